@@ -200,6 +200,122 @@ int pcc_copy_intervals(pcc_ctx *ctx, uint32_t *d_out, size_t count, void *hip_st
 int pcc_set_profiling(pcc_ctx *ctx, int enabled);
 int pcc_last_timings(pcc_ctx *ctx, float *h_ms);
 
+/* ---- Training ----------------------------------------------------------
+ * The operators of a training step of the codec's networks: a pixel's causal
+ * context as a row of inputs, the layers' products and their backward pass,
+ * the code length with its gradient (the loss Eq. (5)), the optimizer.  They
+ * work on rows of several networks of one shape at once: rows
+ * [offsets[g], offsets[g+1]) belong to network ("group") g, whose weights are
+ * the g-th of a stacked tensor.
+ *
+ * These functions belong to no pcc_ctx.  They launch on hip_stream, on the
+ * device that is current at the call, which all pointers belong to; they are
+ * asynchronous, allocate nothing, keep nothing, use no memory but their
+ * arguments and may be captured into a HIP graph.  Types are PCC_BF16,
+ * PCC_FP16 and PCC_FP32.  ld... is the distance between rows in elements, at
+ * least the row's length and at most 2^22.  Outputs must not overlap inputs. */
+
+#define PCC_BF16 0
+#define PCC_FP16 1
+#define PCC_FP32 2
+#define PCC_ACT_RELU 0  /* the blob's activation ids */
+#define PCC_ACT_LEAKY 1 /* slope 0.01 */
+#define PCC_ACT_NONE 2
+#define PCC_MAX_GROUPS 65535
+#define PCC_MAX_FEATURES 65536
+
+/* Causal contexts of all pixels: row p of d_x (bf16) is the network input of
+ * pixel p = (image * H + r) * W + c, value / 256 (exact), 0 outside the image,
+ * in the order of the blob's first layer; `nbhd` and `delay` as in the blob
+ * ((10, 2), (12, 3) or (12, 1)).  Columns 3 nbhd .. width - 1 are set to 0, so
+ * that rows can be padded to a multiple of eight; columns from `width` on are
+ * left as they are. */
+int pcc_contexts(const uint8_t *d_img, int n, int H, int W, int nbhd, int delay,
+                 void *d_x, int width, size_t ldx, void *hip_stream);
+
+/* y_i = act(W_g x_i + b_g) for the rows i of each group g, sums in fp32.
+ *   d_x [rows][in] and d_w [groups][out][in] (contiguous) of `type` bf16 or
+ *   fp16; d_bias [groups][out] fp32 or NULL; d_offsets [groups + 1] int64 on
+ *   the device, rising, within 0..rows.  d_y [rows][out] of `type` or fp32;
+ *   rows of no group are neither read nor written. */
+int pcc_grouped_linear(const void *d_x, size_t ldx, const void *d_w, const float *d_bias,
+                       const int64_t *d_offsets, int groups, size_t rows, int in, int out,
+                       int type, int act, void *d_y, int y_type, size_t ldy, void *hip_stream);
+
+/* Its backward pass.  d_dz [rows][out] is the gradient before this layer's
+ * activation; `x_act` is the activation that made x (PCC_ACT_NONE if none did):
+ *   d_dx [rows][in]         (W_g^T dz_i) * x_act'(x_i): the gradient before the
+ *                           activation of the layer in front, its dz; or NULL
+ *   d_dw [groups][out][in]  sum of dz_i x_i^T over the group's rows, fp32, or NULL
+ *   d_db [groups][out]      sum of dz_i, fp32, or NULL (wants d_dw too)
+ * Groups without rows get zeros in d_dw and d_db.  Sums are taken in an order
+ * that depends on the arguments alone: the same call gives the same bits.
+ * d_workspace: pcc_grouped_linear_grad_workspace_bytes(...) bytes, aligned to
+ * 16, that no other call running at the same time uses (two captured graphs
+ * that may run at once need one each); PCC_E_SCRATCH if it is smaller. */
+size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, int out);
+int pcc_grouped_linear_grad(const void *d_dz, size_t lddz, const void *d_x, size_t ldx, const void *d_w,
+                            const int64_t *d_offsets, int groups, size_t rows, int in, int out,
+                            int type, int x_act, void *d_dx, size_t lddx, float *d_dw, float *d_db,
+                            void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Code length of given pixels under given head outputs, and its gradient.
+ * With p(x) the probability of Eq. (1)-(4) (open tails; `dist` 0 Gaussian, 1
+ * logistic; log-sigma clamped to -8..4, NaN as -8), the coder's integer rule
+ * gives level x the share (65280 p(x) + 1) / 65536 but for rounding down to
+ * whole counts, so
+ *   d_bits[i] = - sum over R, G, B of log2((65280 p + 1) / 65536)
+ *   d_grad[i][12 K] = scale * weight[i] * d bits[i] / d params[i], of grad_type,
+ *                     rounded to nearest; 0 for a log-sigma beyond the clamp
+ * (Eq. (5) is the mean of d_bits: scale = 1 / count.)
+ *   d_params [count][12 K] fp32 (K 3, 5 or 7), d_rgb [count][3], d_weight
+ *   [count] fp32 or NULL (all 1).  A pixel of weight 0 (padding) is not looked
+ *   at: its bits and gradients are 0 whatever its parameters hold.
+ * Either of d_bits and d_grad may be NULL.  d_grad may be d_params where
+ * grad_type is PCC_FP32 and the ld are equal. */
+int pcc_mixture_loss(const float *d_params, size_t ldp, const uint8_t *d_rgb, const float *d_weight, size_t count,
+                     int K, int dist, float scale, float *d_bits, void *d_grad, int grad_type, size_t ldg,
+                     void *hip_stream);
+
+/* AdamW over many tensors in one launch.  With t = *d_step + 1, written back:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g g,
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, and the 16-bit copy of the new param where there is one (what the
+ * products read and a blob holds).
+ * States in 32 bits: m, v fp32 [n].  States in 8 bits: m and the root of v as
+ * e4m3 codes [n] and an fp32 scale for each 256 elements [ceil(n / 256)]; the
+ * scale is the block's largest magnitude / 448, codes are rounded up or down by
+ * a fixed sequence of place in the block and t, in proportion to what is
+ * cut off (to the nearest, a v that changes by 0.1 % a step would never
+ * move); a v above 0 never gets the code of 0.  The update itself uses the
+ * moments before they are rounded. */
+typedef struct {
+    float *d_param;
+    const void *d_grad;
+    void *d_copy;               /* or NULL */
+    void *d_m, *d_v;
+    float *d_m_scale, *d_v_scale; /* 8-bit states, else NULL */
+    size_t n;                   /* elements; 0 is allowed */
+} pcc_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *d_lr; /* device; used in place of lr if not NULL: a captured step then follows a schedule */
+} pcc_adamw_hyper;
+
+typedef struct pcc_adamw pcc_adamw;
+
+/* Lay out the list of tensors (host array, copied) on device `hip_device`.  The
+ * tensors stay the caller's and must outlive the plan.  Allocates device memory
+ * and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
+ * PCC_BF16 or PCC_FP16; state_bits 32 or 8. */
+int pcc_adamw_create(pcc_adamw **out, const pcc_adamw_tensor *h_tensors, int count, int grad_type, int copy_type,
+                     int state_bits, int hip_device);
+void pcc_adamw_destroy(pcc_adamw *plan);
+/* One step.  Asynchronous, allocates nothing; may be captured.  d_step: int64 on
+ * the device, the number of steps taken so far.  One step of a plan at a time. */
+int pcc_adamw_step(pcc_adamw *plan, const pcc_adamw_hyper *h_hyper, int64_t *d_step, void *hip_stream);
+
 const char *pcc_strerror(int code);
 
 #ifdef __cplusplus

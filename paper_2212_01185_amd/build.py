@@ -7,7 +7,8 @@ import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SRC = os.path.join(_HERE, "csrc", "pcc.hip")
+SRC = os.path.join(_HERE, "csrc", "pcc.hip")                # the codec
+TRAIN_SRC = os.path.join(_HERE, "csrc", "pcc_train.hip")    # the operators of a training step
 LIB = os.path.join(_HERE, "libpcc.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -25,14 +26,14 @@ FLAGS = [
 ]
 
 
-def build(verbose: bool = False, extra=(), lib: str = LIB, src: str = SRC) -> str:
+def build(verbose: bool = False, extra=(), lib: str = LIB, src=(SRC, TRAIN_SRC)) -> str:
     """Compile the library to `lib` (default: libpcc.so next to the package).  `extra` are more hipcc flags, e.g.
     -DPCC_PHASE_TIMING for the measurement build that counts the decode step's cycles per phase.  `src` is another HIP
-    source to compile with the library's flags."""
+    source, or several, to compile with the library's flags."""
     LIB = lib
     os.makedirs(os.path.dirname(os.path.abspath(LIB)), exist_ok=True)
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + list(extra) + ["-o", tmp, src]
+    cmd = [HIPCC] + FLAGS + list(extra) + ["-o", tmp] + ([src] if isinstance(src, str) else list(src))
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -1,0 +1,290 @@
+// Host side of the training operators of include/pcc.h, and the contexts' kernel.
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "pcc.h"
+#include "train_adamw.h"
+#include "train_grouped.h"
+#include "train_loss.h"
+
+using namespace pcc_train;
+
+namespace {
+
+// The status of a launch.  An error that another call left is not this one's: it is taken away before.
+template <class F>
+int launch(F&& f) {
+    (void)hipGetLastError();
+    f();
+    return hipGetLastError() == hipSuccess ? PCC_OK : PCC_E_HIP;
+}
+
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) return;
+        ok = hipSetDevice(dev) == hipSuccess;
+    }
+    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
+};
+
+constexpr size_t kMaxLd = (size_t)1 << 22;
+constexpr size_t kMaxRows = (size_t)1 << 40;
+
+bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+size_t size_of(int type) { return type == PCC_FP32 ? 4 : 2; }
+
+// ---------------------------------------------------------------------------
+// Contexts.  A thread writes eight neighbouring values (16 bytes) of one row; the bytes that it gathers were read by its
+// neighbours too and come from the cache, so the output sets the time.
+// ---------------------------------------------------------------------------
+// Network input i of pixel (r, c): the byte of which pixel, or none.
+struct Tap { int dr, dc; };
+__host__ __device__ constexpr Tap tap_of(int nbhd, int delay, int j) {
+    const int run = nbhd == 10 ? 4 : 5;
+    Tap t = j < run ? Tap{-2, j - 2} : j < 2 * run ? Tap{-1, j - run - 2} : Tap{0, j - 2 * run - 2};
+    // diagonal order: (r-2,c+2), (r-1,c+1), (r-1,c+2) are not decoded when (r,c) is; the pixel above stands in
+    if (delay == 1 && ((t.dr == -2 && t.dc == 2) || (t.dr == -1 && t.dc >= 1))) t = {-1, 0};
+    return t;
+}
+
+template <int NBHD, int DELAY>
+__global__ __launch_bounds__(256) void contexts_kernel(const uint8_t* __restrict__ img, uint64_t pixels, int H, int W, u16* __restrict__ x,
+                                                       int width, size_t ldx, int chunks, int wide) {
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint64_t p = id / chunks;
+    const int i0 = (int)(id % chunks) * 8;
+    if (p >= pixels) return;
+    const int c = (int)(p % W), r = (int)(p / W % H);
+    u16x8 v;
+    for (int e = 0; e < 8; ++e) {
+        const int i = i0 + e;
+        float f = 0.0f;
+        if (i < 3 * NBHD) {
+            const Tap t = tap_of(NBHD, DELAY, i / 3);
+            if (r + t.dr >= 0 && c + t.dc >= 0 && c + t.dc < W) f = (float)img[3 * (int64_t)(p + (int64_t)t.dr * W + t.dc) + i % 3] * (1.0f / 256.0f);
+        }
+        v[e] = to16<Bf16>(f);     // exact: eight significant bits
+    }
+    u16* to = x + p * ldx + i0;
+    if (wide && i0 + 8 <= width) *reinterpret_cast<u16x8*>(to) = v;
+    else for (int e = 0; e < 8; ++e) if (i0 + e < width) to[e] = v[e];
+}
+
+// ---------------------------------------------------------------------------
+// Grouped products.
+// ---------------------------------------------------------------------------
+bool features_ok(int in, int out, int groups, size_t rows) {
+    return in >= 1 && out >= 1 && in <= PCC_MAX_FEATURES && out <= PCC_MAX_FEATURES && groups >= 1 && groups <= PCC_MAX_GROUPS && rows <= kMaxRows;
+}
+bool ld_ok(size_t ld, int features) { return ld >= (size_t)features && ld <= kMaxLd; }
+
+// Rows of a chunk of the weights' gradient.  A chunk's sums go to the workspace and are added up by another kernel, so
+// there are no more chunks than fill the chip, and none of less than 256 rows.
+int weights_log2(size_t rows, int in, int out) {
+    const size_t tiles = ((size_t)in + kTile - 1) / kTile * (((size_t)out + kTile - 1) / kTile);
+    const size_t want = std::max<size_t>(1, 512 / tiles);
+    int log2 = 8;
+    while (((size_t)1 << log2) * want < rows) ++log2;
+    return log2;
+}
+
+template <class T, int MODE>
+int launch_tiles(Grouped& a, hipStream_t st) {
+    a.tiles_m = (uint32_t)(((MODE == kForward ? a.out : a.in) + kTile - 1) / kTile);
+    a.tiles_n = (uint32_t)((a.out + kTile - 1) / kTile);
+    const uint64_t chunks = ((uint64_t)a.rows >> a.log2) + a.groups, blocks = chunks * a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
+    if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    return launch([&] { hipLaunchKernelGGL((grouped_tile_kernel<T, MODE>), dim3((uint32_t)blocks), dim3(kTileThreads), 0, st, a); });
+}
+
+}  // namespace
+
+struct pcc_adamw {
+    int device = 0;
+    int grad_type = 0, copy_type = 0, state_bits = 32;
+    uint32_t n_pieces = 0;
+    uint8_t* d_table = nullptr;     // ticket, tensors, pieces
+    AdamwTensor* d_tensors = nullptr;
+    AdamwPiece* d_pieces = nullptr;
+};
+
+extern "C" {
+
+int pcc_contexts(const uint8_t* d_img, int n, int H, int W, int nbhd, int delay, void* d_x, int width, size_t ldx, void* hip_stream) {
+    if (!d_img || !d_x || n < 1 || H < 1 || W < 1 || (size_t)H * W > (size_t)1 << 31) return PCC_E_ARG;
+    const uint64_t pixels = (uint64_t)n * H * W;
+    if (!((nbhd == 10 && delay == 2) || (nbhd == 12 && (delay == 3 || delay == 1)))) return PCC_E_ARG;
+    if (width < 3 * nbhd || width > PCC_MAX_FEATURES || !ld_ok(ldx, width) || !aligned(d_x, 2)) return PCC_E_ARG;
+    const int chunks = (width + 7) / 8, wide = aligned(d_x, 16) && ldx % 8 == 0;
+    const uint64_t blocks = (pixels * chunks + 255) / 256;
+    if (pixels > kMaxRows || blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    auto go = [&](auto kernel) {
+        return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, (hipStream_t)hip_stream, d_img, pixels, H, W, (u16*)d_x, width, ldx, chunks, wide); });
+    };
+    return nbhd == 10 ? go(contexts_kernel<10, 2>) : delay == 3 ? go(contexts_kernel<12, 3>) : go(contexts_kernel<12, 1>);
+}
+
+int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float* d_bias, const int64_t* d_offsets, int groups,
+                       size_t rows, int in, int out, int type, int act, void* d_y, int y_type, size_t ldy, void* hip_stream) {
+    if (!d_x || !d_w || !d_offsets || !d_y || !features_ok(in, out, groups, rows) || !ld_ok(ldx, in) || !ld_ok(ldy, out)) return PCC_E_ARG;
+    if ((type != PCC_BF16 && type != PCC_FP16) || (y_type != type && y_type != PCC_FP32) || act < PCC_ACT_RELU || act > PCC_ACT_NONE) return PCC_E_ARG;
+    if (!aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_bias, 4) || !aligned(d_offsets, 8) || !aligned(d_y, size_of(y_type))) return PCC_E_ARG;
+    if (rows == 0) return PCC_OK;
+    Grouped a = {};
+    a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.bias = d_bias; a.off = d_offsets; a.y = d_y;
+    a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = act;
+    a.y32 = y_type == PCC_FP32;
+    a.log2 = 7;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return type == PCC_BF16 ? launch_tiles<Bf16, kForward>(a, st) : launch_tiles<Fp16, kForward>(a, st);
+}
+
+size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, int out) {
+    if (!features_ok(in, out, groups, rows)) return 0;
+    const int log2 = weights_log2(rows, in, out);
+    if (rows <= (size_t)1 << log2) return 0;
+    return ((rows >> log2) + groups) * ((size_t)in * out + out) * sizeof(float);
+}
+
+int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size_t ldx, const void* d_w, const int64_t* d_offsets,
+                            int groups, size_t rows, int in, int out, int type, int x_act, void* d_dx, size_t lddx, float* d_dw,
+                            float* d_db, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if (!d_dz || !d_x || !d_offsets || (!d_dx && !d_dw) || (d_dx && !d_w) || (d_db && !d_dw)) return PCC_E_ARG;
+    if (!features_ok(in, out, groups, rows) || !ld_ok(lddz, out) || !ld_ok(ldx, in) || (d_dx && !ld_ok(lddx, in))) return PCC_E_ARG;
+    if ((type != PCC_BF16 && type != PCC_FP16) || x_act < PCC_ACT_RELU || x_act > PCC_ACT_NONE) return PCC_E_ARG;
+    if (!aligned(d_dz, 2) || !aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_offsets, 8) || !aligned(d_dx, 2) || !aligned(d_dw, 4) ||
+        !aligned(d_db, 4)) return PCC_E_ARG;
+    const size_t need = d_dw ? pcc_grouped_linear_grad_workspace_bytes(rows, groups, in, out) : 0;
+    if (need && (!d_workspace || workspace_bytes < need)) return PCC_E_SCRATCH;
+    if (need && !aligned(d_workspace, 16)) return PCC_E_ARG;
+    hipStream_t st = (hipStream_t)hip_stream;
+    Grouped a = {};
+    a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.dz = (const u16*)d_dz; a.off = d_offsets; a.y = d_dx; a.dw = d_dw; a.db = d_db;
+    a.ldx = ldx; a.lddz = lddz; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = x_act;
+    a.partial = (float*)d_workspace;
+    if (d_dx && rows) {
+        a.log2 = 7;
+        const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kBackward>(a, st) : launch_tiles<Fp16, kBackward>(a, st);
+        if (rc != PCC_OK) return rc;
+    }
+    if (d_dw) {
+        a.log2 = weights_log2(rows, in, out);
+        int rc = type == PCC_BF16 ? launch_tiles<Bf16, kWeights>(a, st) : launch_tiles<Fp16, kWeights>(a, st);
+        if (rc != PCC_OK || !need) return rc;
+        const size_t values = (size_t)in * out + out;
+        return launch([&] {
+            hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)std::min<size_t>((values + 255) / 256, 1024), groups), dim3(256), 0, st, a);
+        });
+    }
+    return PCC_OK;
+}
+
+int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, const float* d_weight, size_t count, int K, int dist,
+                     float scale, float* d_bits, void* d_grad, int grad_type, size_t ldg, void* hip_stream) {
+    if (!d_params || !d_rgb || (!d_bits && !d_grad) || (K != 3 && K != 5 && K != 7) || (dist != 0 && dist != 1)) return PCC_E_ARG;
+    if (!ld_ok(ldp, 12 * K) || (d_grad && (!ld_ok(ldg, 12 * K) || grad_type < PCC_BF16 || grad_type > PCC_FP32))) return PCC_E_ARG;
+    if (!aligned(d_params, 4) || !aligned(d_weight, 4) || !aligned(d_bits, 4) || (d_grad && !aligned(d_grad, size_of(grad_type)))) return PCC_E_ARG;
+    if (count == 0) return PCC_OK;
+    const size_t blocks = (count + 255) / 256;
+    if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    auto go = [&](auto kernel) {
+        return launch([&] {
+            hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, (hipStream_t)hip_stream, d_params, ldp, d_rgb, d_weight, count, scale,
+                               d_bits, d_grad, grad_type, ldg);
+        });
+    };
+    if (dist == 0) return K == 3 ? go(mixture_loss_kernel<3, 0>) : K == 5 ? go(mixture_loss_kernel<5, 0>) : go(mixture_loss_kernel<7, 0>);
+    return K == 3 ? go(mixture_loss_kernel<3, 1>) : K == 5 ? go(mixture_loss_kernel<5, 1>) : go(mixture_loss_kernel<7, 1>);
+}
+
+int pcc_adamw_create(pcc_adamw** out, const pcc_adamw_tensor* h_tensors, int count, int grad_type, int copy_type, int state_bits,
+                     int hip_device) {
+    if (!out) return PCC_E_ARG;
+    *out = nullptr;
+    if (!h_tensors || count < 1 || grad_type < PCC_BF16 || grad_type > PCC_FP32 || (copy_type != PCC_BF16 && copy_type != PCC_FP16) ||
+        (state_bits != 8 && state_bits != 32)) return PCC_E_ARG;
+    const size_t state = (size_t)state_bits / 8;
+    uint64_t pieces = 0;
+    for (int i = 0; i < count; ++i) {
+        const pcc_adamw_tensor& s = h_tensors[i];
+        if (s.n == 0) continue;
+        if (!s.d_param || !s.d_grad || !s.d_m || !s.d_v || (state_bits == 8 && (!s.d_m_scale || !s.d_v_scale))) return PCC_E_ARG;
+        if (!aligned(s.d_param, 4) || !aligned(s.d_grad, size_of(grad_type)) || !aligned(s.d_copy, 2) || !aligned(s.d_m, state) || !aligned(s.d_v, state) ||
+            (state_bits == 8 && (!aligned(s.d_m_scale, 4) || !aligned(s.d_v_scale, 4)))) return PCC_E_ARG;
+        if (s.n > (size_t)1 << 40) return PCC_E_ARG;
+        pieces += (s.n + kPiece - 1) / kPiece;
+    }
+    if (pieces > 0x7FFFFFFFull) return PCC_E_ARG;
+    std::vector<uint8_t> table;
+    const size_t at_pieces = 64 + (size_t)count * sizeof(AdamwTensor);
+    try {
+        table.assign(at_pieces + (size_t)pieces * sizeof(AdamwPiece), 0);
+    } catch (const std::bad_alloc&) {
+        return PCC_E_INTERNAL;
+    }
+    AdamwTensor* tensors = reinterpret_cast<AdamwTensor*>(table.data() + 64);
+    AdamwPiece* list = reinterpret_cast<AdamwPiece*>(table.data() + at_pieces);
+    for (int i = 0; i < count; ++i) {
+        const pcc_adamw_tensor& s = h_tensors[i];
+        tensors[i] = {s.d_param, s.d_grad, (u16*)s.d_copy, s.d_m, s.d_v, s.d_m_scale, s.d_v_scale, s.n,
+                      aligned(s.d_param, 16) && aligned(s.d_grad, 4 * size_of(grad_type)) && aligned(s.d_copy, 8) && aligned(s.d_m, 4 * state) && aligned(s.d_v, 4 * state), 0};
+        for (size_t k = 0; k * kPiece < s.n; ++k) *list++ = {(uint32_t)i, (uint32_t)k};
+    }
+    DeviceGuard guard(hip_device);
+    if (!guard.ok) { (void)hipGetLastError(); return PCC_E_HIP; }
+    pcc_adamw* plan = new (std::nothrow) pcc_adamw();
+    if (!plan) return PCC_E_INTERNAL;
+    plan->device = hip_device;
+    plan->grad_type = grad_type;
+    plan->copy_type = copy_type;
+    plan->state_bits = state_bits;
+    plan->n_pieces = (uint32_t)pieces;
+    if (hipMalloc((void**)&plan->d_table, table.size()) != hipSuccess ||
+        hipMemcpy(plan->d_table, table.data(), table.size(), hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipGetLastError();
+        pcc_adamw_destroy(plan);
+        return PCC_E_HIP;
+    }
+    plan->d_tensors = reinterpret_cast<AdamwTensor*>(plan->d_table + 64);
+    plan->d_pieces = reinterpret_cast<AdamwPiece*>(plan->d_table + at_pieces);
+    *out = plan;
+    return PCC_OK;
+}
+
+void pcc_adamw_destroy(pcc_adamw* plan) {
+    if (!plan) return;
+    DeviceGuard guard(plan->device);
+    if (plan->d_table) (void)hipFree(plan->d_table);
+    delete plan;
+}
+
+int pcc_adamw_step(pcc_adamw* plan, const pcc_adamw_hyper* h, int64_t* d_step, void* hip_stream) {
+    if (!plan || !h || !d_step || !aligned(d_step, 8) || !aligned(h->d_lr, 4)) return PCC_E_ARG;
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0 && h->eps >= 0.0)) return PCC_E_ARG;
+    DeviceGuard guard(plan->device);
+    if (!guard.ok) return PCC_E_HIP;
+    AdamwArgs a = {};
+    a.tensors = plan->d_tensors;
+    a.pieces = plan->d_pieces;
+    a.n_pieces = plan->n_pieces;
+    a.ticket = reinterpret_cast<uint32_t*>(plan->d_table);
+    a.step = d_step;
+    a.d_lr = h->d_lr;
+    a.lr = h->lr; a.beta1 = h->beta1; a.beta2 = h->beta2; a.weight_decay = h->weight_decay;
+    a.b1 = (float)h->beta1; a.rest1 = (float)(1.0 - h->beta1); a.b2 = (float)h->beta2; a.rest2 = (float)(1.0 - h->beta2); a.eps = (float)h->eps;
+    const uint32_t blocks = std::max<uint32_t>(1, std::min<uint32_t>(plan->n_pieces, 2048));
+    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kAdamwThreads), 0, (hipStream_t)hip_stream, a); }); };
+    auto with_grad = [&](auto copy, auto bits) {
+        constexpr int C = decltype(copy)::value, B = decltype(bits)::value;
+        return plan->grad_type == PCC_FP32 ? go(adamw_kernel<PCC_FP32, C, B>) : plan->grad_type == PCC_BF16 ? go(adamw_kernel<PCC_BF16, C, B>) : go(adamw_kernel<PCC_FP16, C, B>);
+    };
+    auto with_copy = [&](auto bits) {
+        return plan->copy_type == PCC_BF16 ? with_grad(std::integral_constant<int, PCC_BF16>{}, bits) : with_grad(std::integral_constant<int, PCC_FP16>{}, bits);
+    };
+    return plan->state_bits == 8 ? with_copy(std::integral_constant<int, 8>{}) : with_copy(std::integral_constant<int, 32>{});
+}
+
+}  // extern "C"

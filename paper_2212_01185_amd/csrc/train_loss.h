@@ -1,0 +1,179 @@
+// Code length of a pixel under the mixture its head outputs describe, and its gradient.
+//
+// For a component with a = (x - 1/2)/256 and b = (x + 1/2)/256 in units of its width, q = F(b) - F(a) is its probability of
+// level x, and with the density f:  dq/dmu = (f(a) - f(b)) / sigma,  dq/dlog sigma = a f(a) - b f(b).
+// A difference of two values of F next to each other loses what a code length needs (the coder's rule adds one count of
+// 65,536, so q matters down to 1e-5 and below), so nothing here subtracts two such values:
+//   - the component is mirrored so that its middle m is right of the mean, and upper tails are used: near = m - h,
+//     far = m + h, half a level is h = 1 / (512 sigma)
+//   - logistic: S(z) = 1 / (1 + e^z);  S(near) - S(far) = S(near) (1 - S(far)) (1 - e^-2h),
+//     f(near) - f(far) = q (1 - S(near) - S(far))
+//   - Gaussian, levels narrow against the curvature (2h (m + 1) < 1/2): the derivatives of the density are Hermite
+//     polynomials, q = 2h f(m) (1 + He2 D2/24 + He4 D4/1920), f(near) - f(far) = 2h f(m) (He1 + He3 D2/24 + He5 D4/1920) with
+//     D = 2h; what is left out is below D^6 (m + 1)^6 / 322,560 < 5e-8
+//   - Gaussian, else: tails as f(z) R(z), Mills' ratio R a polynomial in 1 / (1 + z/4) (fitted: 4e-8 apart, 4e-7 in fp32);
+//     the two differ by a factor of e^(1/2) at least, or lie near the mean
+//   - near f(near) - far f(far) = m (f(near) - f(far)) - h (f(near) + f(far))
+#pragma once
+
+#include "train_device.h"
+
+namespace pcc_train {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+
+// e^v by the hardware's 2^x: v log2(e) as a rounded product and what the rounding and the constant's own left out (without it
+// e^-8 is 3e-7 off, and a distance in widths of that component with it).
+__device__ __forceinline__ float exp_of(float v) {
+    const float t = v * kLog2e;
+    const float rest = __builtin_fmaf(v, kLog2e, -t) + v * 1.925962989e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return t > -126.0f && t < 128.0f ? __builtin_fmaf(e, rest * kLn2, e) : e;
+}
+
+// Q(z) / f(z) of the standard normal distribution, z >= 0.
+__device__ __forceinline__ float mills(float z) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, z, 1.0f));
+    float p = 4.959281161e-02f;
+    p = __builtin_fmaf(p, t, -2.027588040e-01f);
+    p = __builtin_fmaf(p, t, 2.396807224e-01f);
+    p = __builtin_fmaf(p, t, -7.955849171e-02f);
+    p = __builtin_fmaf(p, t, 1.597021073e-01f);
+    p = __builtin_fmaf(p, t, 1.478174478e-01f);
+    p = __builtin_fmaf(p, t, 2.045509815e-01f);
+    p = __builtin_fmaf(p, t, 2.342851609e-01f);
+    p = __builtin_fmaf(p, t, 2.500021756e-01f);
+    p = __builtin_fmaf(p, t, 2.499999851e-01f);
+    return p * t;
+}
+
+struct Bin {
+    float q;        // probability of the level
+    float d_mu;     // f(a) - f(b)
+    float d_ls;     // a f(a) - b f(b)
+};
+
+// mid: the level's middle, h: half a level, both in widths of the component; first, last: the level is 0, 255 (open ends).
+template <int DIST>
+__device__ __forceinline__ Bin bin_of(float mid, float h, bool first, bool last) {
+    const bool mirrored = mid < 0.0f;
+    const float m = fabsf(mid), near = m - h, far = m + h;
+    const bool open_near = mirrored ? last : first, open_far = mirrored ? first : last;
+    float q, diff, sum;     // diff, sum: f(near) -+ f(far)
+    if (DIST == 1) {
+        const float en = exp_of(near), ef = exp_of(-far);
+        const float sn = open_near ? 1.0f : __builtin_amdgcn_rcpf(1.0f + en);
+        const float sf = open_far ? 0.0f : ef * __builtin_amdgcn_rcpf(1.0f + ef);
+        const float d = 2.0f * h;
+        const float gap = d < 0.1f ? d * __builtin_fmaf(d, __builtin_fmaf(d, __builtin_fmaf(d, -1.0f / 24.0f, 1.0f / 6.0f), -0.5f), 1.0f)
+                                   : 1.0f - exp_of(-d);
+        const float both = 1.0f - sn - sf;
+        if (open_near || open_far) {
+            q = open_near ? __builtin_amdgcn_rcpf(1.0f + ef) : sn;
+            const float fn = open_near ? 0.0f : sn * (1.0f - sn), ff = sf * (1.0f - sf);
+            diff = fn - ff;
+            sum = fn + ff;
+        } else {
+            q = sn * (1.0f - sf) * gap;
+            diff = q * both;
+            sum = __builtin_fmaf(sn, 1.0f - sn, sf * (1.0f - sf));
+        }
+    } else {
+        const float c = 0.39894228040143268f, d = 2.0f * h;
+        if (d * (m + 1.0f) < 0.5f && !open_near && !open_far) {
+            const float f = c * exp_of(-0.5f * m * m), z2 = m * m, d2 = d * d * (1.0f / 24.0f), d4 = d * d * d * d * (1.0f / 1920.0f);
+            const float he2 = z2 - 1.0f, he4 = __builtin_fmaf(z2, z2 - 6.0f, 3.0f), he6 = __builtin_fmaf(z2, __builtin_fmaf(z2, z2 - 15.0f, 45.0f), -15.0f);
+            const float he3 = m * (z2 - 3.0f), he5 = m * __builtin_fmaf(z2, z2 - 10.0f, 15.0f);
+            const float df = d * f;
+            Bin b;
+            b.q = df * __builtin_fmaf(he4, d4, __builtin_fmaf(he2, d2, 1.0f));
+            const float dm = df * __builtin_fmaf(he5, d4, __builtin_fmaf(he3, d2, m));
+            b.d_mu = mirrored ? -dm : dm;
+            b.d_ls = df * __builtin_fmaf(he6, d4, __builtin_fmaf(he4, d2, he2));
+            return b;
+        }
+        const float fn = open_near ? 0.0f : c * exp_of(-0.5f * near * near), ff = open_far ? 0.0f : c * exp_of(-0.5f * far * far);
+        const float tn = fn * mills(fabsf(near)), tail_near = open_near ? 1.0f : near < 0.0f ? 1.0f - tn : tn;
+        const float tail_far = open_far ? 0.0f : ff * mills(far);
+        q = tail_near - tail_far;
+        diff = fn - ff;
+        sum = fn + ff;
+    }
+    return {q, mirrored ? -diff : diff, __builtin_fmaf(m, diff, -(h * sum))};
+}
+
+// One channel: returns its bits and puts the gradient in place of the channel's 3 K outputs (logits, means, log-sigmas).  shift: what
+// the coupling adds to the means.  A level's distance from a mean is taken in 64 bits: in 32 the sum of mean and coupling is rounded
+// by 3e-8, a ten-thousandth of the narrowest component's width.
+template <int K, int DIST>
+__device__ __forceinline__ float channel_loss(float (&o)[3 * K], const double (&shift)[K], int level, float factor) {
+    float top = o[0];
+#pragma unroll
+    for (int k = 1; k < K; ++k) top = fmaxf(top, o[k]);
+    float pi[K], total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) { pi[k] = exp_of(o[k] - top); total += pi[k]; }
+    const float inverse = __builtin_amdgcn_rcpf(total);
+    const double x = (double)level * (1.0 / 256.0);
+    float p = 0.0f, q[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        pi[k] *= inverse;
+        const float raw = o[2 * K + k];
+        const bool inside = raw >= -8.0f && raw <= 4.0f;
+        const float ls = raw > 4.0f ? 4.0f : raw >= -8.0f ? raw : -8.0f;
+        const float width = exp_of(-ls);
+        const Bin b = bin_of<DIST>((float)(x - (double)o[K + k] - shift[k]) * width, width * (1.0f / 512.0f), level == 0, level == 255);
+        q[k] = b.q;
+        p = __builtin_fmaf(pi[k], b.q, p);
+        o[K + k] = pi[k] * b.d_mu * width;
+        o[2 * K + k] = inside ? pi[k] * b.d_ls : 0.0f;
+    }
+    const float counts = __builtin_fmaf(65280.0f, p, 1.0f);
+    const float outer = factor * (-65280.0f / kLn2) * __builtin_amdgcn_rcpf(counts);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        o[k] = outer * pi[k] * (q[k] - p);
+        o[K + k] *= outer;
+        o[2 * K + k] *= outer;
+    }
+    return 16.0f - __builtin_amdgcn_logf(counts);
+}
+
+template <int K, int DIST>
+__global__ __launch_bounds__(256) void mixture_loss_kernel(const float* params, size_t ldp, const uint8_t* __restrict__ rgb,
+                                                           const float* __restrict__ weight, size_t count, float scale,
+                                                           float* __restrict__ bits, void* grad, int grad_type, size_t ldg) {
+    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= count) return;
+    const float wt = weight ? weight[i] : 1.0f;
+    float out[12 * K], sum = 0.0f;
+    if (wt == 0.0f) {
+        for (int j = 0; j < 12 * K; ++j) out[j] = 0.0f;
+    } else {
+        const float* o = params + i * ldp;
+        const int r = rgb[3 * i], g = rgb[3 * i + 1], b = rgb[3 * i + 2];
+        const float rh = (float)r * (1.0f / 256.0f), gh = (float)g * (1.0f / 256.0f);
+        for (int c = 0; c < 3; ++c) {
+            float ch[3 * K];
+            double shift[K];
+            for (int j = 0; j < 3 * K; ++j) ch[j] = o[3 * K * c + j];
+            for (int k = 0; k < K; ++k)
+                shift[k] = c == 0 ? 0.0 : c == 1 ? (double)o[9 * K + k] * rh : __builtin_fma((double)o[11 * K + k], (double)gh, (double)o[10 * K + k] * rh);
+            sum += channel_loss<K, DIST>(ch, shift, c == 0 ? r : c == 1 ? g : b, wt * scale);
+            for (int j = 0; j < 3 * K; ++j) out[3 * K * c + j] = ch[j];
+            for (int k = 0; k < K; ++k) {
+                if (c == 1) out[9 * K + k] = ch[K + k] * rh;
+                if (c == 2) { out[10 * K + k] = ch[K + k] * rh; out[11 * K + k] = ch[K + k] * gh; }
+            }
+        }
+    }
+    if (bits) bits[i] = sum;
+    if (!grad) return;
+    for (int j = 0; j < 12 * K; ++j) {
+        if (grad_type == PCC_FP32) static_cast<float*>(grad)[i * ldg + j] = out[j];
+        else static_cast<u16*>(grad)[i * ldg + j] = grad_type == PCC_BF16 ? to16<Bf16>(out[j]) : to16<Fp16>(out[j]);
+    }
+}
+
+}  // namespace pcc_train

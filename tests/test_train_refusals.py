@@ -1,0 +1,115 @@
+"""Arguments that the training operators refuse, before anything touches a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2212_01185_amd import binding
+
+P = 4096                 # stands for a device pointer: a refused call never follows it
+ARG, SCRATCH = binding.PCC_E_ARG, binding.PCC_E_SCRATCH
+
+
+def call(name, defaults, **changes):
+    args = dict(defaults)
+    assert set(changes) <= set(args)
+    args.update(changes)
+    return getattr(binding.load(), name)(*args.values())
+
+
+CONTEXTS = dict(img=P, n=1, H=4, W=4, nbhd=10, delay=2, x=P, width=32, ldx=32, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(img=None), dict(x=None), dict(n=0), dict(H=-1), dict(W=0), dict(nbhd=11), dict(delay=3), dict(nbhd=12),
+                                     dict(width=29), dict(ldx=31), dict(width=70000, ldx=70000), dict(ldx=1 << 23), dict(x=P + 1),
+                                     dict(H=1 << 20, W=1 << 20), dict(n=1 << 30, H=1 << 15, W=1 << 15)])
+def test_contexts(changes):
+    assert call("pcc_contexts", CONTEXTS, **changes) == ARG
+
+
+LINEAR = dict(x=P, ldx=32, w=P, bias=P, off=P, groups=2, rows=8, fan_in=32, fan_out=16, type=0, act=0, y=P, y_type=0, ldy=16, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(x=None), dict(w=None), dict(off=None), dict(y=None), dict(groups=0), dict(groups=65536), dict(fan_in=0),
+                                     dict(fan_out=0), dict(fan_in=70000, ldx=70000), dict(ldx=31), dict(ldy=15), dict(ldx=1 << 23), dict(type=2),
+                                     dict(type=3), dict(y_type=1), dict(type=1, y_type=0), dict(act=3), dict(act=-1), dict(x=P + 1), dict(w=P + 1),
+                                     dict(bias=P + 2), dict(off=P + 4), dict(y=P + 1), dict(y_type=2, y=P + 2), dict(rows=1 << 41)])
+def test_grouped_linear(changes):
+    assert call("pcc_grouped_linear", LINEAR, **changes) == ARG
+
+
+def test_grouped_linear_without_rows_does_nothing():
+    assert call("pcc_grouped_linear", LINEAR, rows=0) == binding.PCC_OK
+
+
+GRAD = dict(dz=P, lddz=16, x=P, ldx=32, w=P, off=P, groups=2, rows=8, fan_in=32, fan_out=16, type=0, x_act=0, dx=P, lddx=32, dw=P, db=P,
+            workspace=None, workspace_bytes=0, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(dz=None), dict(x=None), dict(off=None), dict(w=None), dict(dx=None, dw=None, db=None), dict(dw=None),
+                                     dict(groups=0), dict(fan_in=0), dict(lddz=15), dict(ldx=31), dict(lddx=31), dict(type=2), dict(x_act=3),
+                                     dict(dz=P + 1), dict(dw=P + 2), dict(db=P + 2), dict(off=P + 4), dict(dx=P + 1),
+                                     dict(rows=100000, workspace=P + 8, workspace_bytes=1 << 30)])
+def test_grouped_linear_grad(changes):
+    assert call("pcc_grouped_linear_grad", GRAD, **changes) == ARG
+
+
+def test_grouped_linear_grad_wants_its_workspace():
+    need = binding.load().pcc_grouped_linear_grad_workspace_bytes(100000, 2, 32, 16)
+    assert need > 0
+    assert call("pcc_grouped_linear_grad", GRAD, rows=100000) == SCRATCH
+    assert call("pcc_grouped_linear_grad", GRAD, rows=100000, workspace=P, workspace_bytes=need - 1) == SCRATCH
+    assert binding.load().pcc_grouped_linear_grad_workspace_bytes(100000, 0, 32, 16) == 0
+
+
+LOSS = dict(params=P, ldp=60, rgb=P, weight=None, count=4, K=5, dist=0, scale=1.0, bits=P, grad=P, grad_type=2, ldg=60, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(params=None), dict(rgb=None), dict(bits=None, grad=None), dict(K=4), dict(K=0), dict(dist=2), dict(dist=-1),
+                                     dict(ldp=59), dict(ldg=59), dict(grad_type=3), dict(grad_type=-1), dict(params=P + 2), dict(weight=P + 1),
+                                     dict(bits=P + 2), dict(grad=P + 2), dict(grad=P + 1, grad_type=0), dict(ldp=1 << 23)])
+def test_mixture_loss(changes):
+    assert call("pcc_mixture_loss", LOSS, **changes) == ARG
+
+
+def test_mixture_loss_of_nothing():
+    assert call("pcc_mixture_loss", LOSS, count=0) == binding.PCC_OK
+
+
+def _plan(count=1, grad_type=2, copy_type=0, bits=32, device=0, out=True, table=True, **tensor):
+    t = (binding._AdamwTensor * max(1, count))()
+    for row in t:
+        for name in ("d_param", "d_grad", "d_copy", "d_m", "d_v", "d_m_scale", "d_v_scale"):
+            setattr(row, name, tensor.get(name, P))
+        row.n = tensor.get("n", 10)
+    h = C.c_void_p()
+    return binding.load().pcc_adamw_create(C.byref(h) if out else None, t if table else None, count, grad_type, copy_type, bits, device)
+
+
+@pytest.mark.parametrize("changes", [dict(count=0), dict(grad_type=3), dict(copy_type=2), dict(bits=16), dict(out=False), dict(table=False),
+                                     dict(d_param=None), dict(d_grad=None), dict(d_m=None), dict(d_v=None), dict(d_param=P + 2), dict(d_grad=P + 1),
+                                     dict(d_copy=P + 1), dict(d_m=P + 2), dict(bits=8, d_m_scale=None), dict(bits=8, d_v_scale=P + 2), dict(n=1 << 41)])
+def test_adamw_create(changes):
+    assert _plan(**changes) == ARG
+
+
+def test_adamw_step_without_a_plan():
+    hyper = binding._AdamwHyper(1e-3, 0.9, 0.999, 1e-8, 0.0, None)
+    assert binding.load().pcc_adamw_step(None, C.byref(hyper), P, None) == ARG
+    binding.load().pcc_adamw_destroy(None)
+
+
+def test_python_arguments():
+    x, w, off = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(1, 3, 8, dtype=torch.bfloat16), torch.tensor([0, 4])
+    for bad in (lambda: binding.pcc_contexts(torch.zeros(1, 2, 2, 3, dtype=torch.uint8)),         # not on a GPU
+                lambda: binding.pcc_grouped_linear(x, w, None, off),
+                lambda: binding.pcc_grouped_linear(x.float(), w, None, off),
+                lambda: binding.pcc_grouped_linear(x.t(), w, None, off),
+                lambda: binding.pcc_mixture_loss(torch.zeros(4, 60), torch.zeros(4, 3, dtype=torch.uint8)),
+                lambda: binding.AdamW([], []),
+                lambda: binding.AdamW([torch.zeros(3)], []),
+                lambda: binding.AdamW([torch.zeros(3)], [torch.zeros(3)], state_bits=16),
+                lambda: binding.AdamW([torch.zeros(3)], [torch.zeros(3)], betas=(1.0, 0.9)),
+                lambda: binding.AdamW([torch.zeros(3)], [torch.zeros(3)])):
+        with pytest.raises(ValueError):
+            bad()
