@@ -91,13 +91,23 @@ int weights_log2(size_t rows, int in, int out) {
     return log2;
 }
 
+// Rows of an operand can be read in pieces of 16 bytes, which have to begin at a multiple of four.
+bool even_rows(const void* p, size_t ld) { return aligned(p, 4) && ld % 2 == 0; }
+
 template <class T, int MODE>
 int launch_tiles(Grouped& a, hipStream_t st) {
     a.tiles_m = (uint32_t)(((MODE == kForward ? a.out : a.in) + kTile - 1) / kTile);
     a.tiles_n = (uint32_t)((a.out + kTile - 1) / kTile);
     const uint64_t chunks = ((uint64_t)a.rows >> a.log2) + a.groups, blocks = chunks * a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
-    if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
-    return launch([&] { hipLaunchKernelGGL((grouped_tile_kernel<T, MODE>), dim3((uint32_t)blocks), dim3(kTileThreads), 0, st, a); });
+    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    const bool wide = (MODE == kBackward || even_rows(a.x, a.ldx)) && (MODE == kForward || even_rows(a.dz, a.lddz)) &&
+                      (MODE == kWeights || even_rows(a.w, (size_t)a.in));
+    a.wide_x = aligned(a.x, 8) && a.ldx % 4 == 0;
+    a.wide_out = MODE == kWeights ? aligned(a.dw, 16) && aligned(a.partial, 16) && ((size_t)a.in * a.out + a.out) % 4 == 0
+                                  : aligned(a.y, a.y32 ? 16 : 8) && a.ldy % 4 == 0;
+    const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);     // a multiple of the dies: see find_chunk
+    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kTileThreads), 0, st, a); }); };
+    return wide ? go(grouped_tile_kernel<T, MODE, true>) : go(grouped_tile_kernel<T, MODE, false>);
 }
 
 }  // namespace

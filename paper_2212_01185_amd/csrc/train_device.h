@@ -66,8 +66,9 @@ __device__ __forceinline__ float times_derivative(float d, float x, int act) {
 struct Chunk {
     int group;          // -1: there is no such chunk
     int64_t lo, hi;     // rows
-    uint32_t first;     // number of the group's first chunk
+    uint32_t id;        // number of the chunk
     uint32_t count;     // chunks of the group
+    uint32_t part;      // tile of the chunk
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -77,38 +78,56 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
     return (int64_t)(((uint64_t)uniform((uint32_t)((uint64_t)v >> 32)) << 32) | uniform((uint32_t)(uint64_t)v));
 }
 
-// All lanes of a wave together; the result is the same in every lane.  With `empty`, a group without rows has one chunk, of no rows.
-__device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t t, bool empty) {
+// Rows of group g and how many chunks they make; with `empty`, a group without rows has one, of no rows.
+__device__ __forceinline__ uint32_t group_chunks(const int64_t* __restrict__ off, int g, int groups, int64_t rows, int log2, bool empty, int64_t& lo, int64_t& hi) {
+    if (g >= groups) { lo = hi = 0; return 0; }
+    lo = clamp64(off[g], 0, rows);
+    hi = clamp64(off[g + 1], lo, rows);
+    const uint32_t n = (uint32_t)((hi - lo + ((int64_t)1 << log2) - 1) >> log2);
+    return empty && n == 0 ? 1 : n;
+}
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
     const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t up = (uint32_t)__shfl_up((int)v, d);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
+
+// Workgroup b's chunk and tile (of `tiles` that each chunk has).  All lanes of a wave together; the result is the same in every lane.
+// The chip's eight dies take workgroups in turn and have an L2 each, so die d gets the d-th eighth of the work, and within a group
+// the chunks of one tile come one after the other: they read the same weights at about the same time.
+__device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t tiles, uint32_t b, bool empty) {
+    const int lane = threadIdx.x & 63;
+    uint32_t total = 0;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+        int64_t lo, hi;
+        uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, empty, lo, hi);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
+        total += uniform(n);
+    }
+    const uint32_t all = total * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
+    if (at >= each || t >= all) return {-1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
-        const int g = g0 + lane;
-        int64_t lo = 0, hi = 0;
-        uint32_t n = 0;
-        if (g < groups) {
-            lo = clamp64(off[g], 0, rows);
-            hi = clamp64(off[g + 1], lo, rows);
-            n = (uint32_t)((hi - lo + ((int64_t)1 << log2) - 1) >> log2);
-            if (empty && n == 0) n = 1;
-        }
-        uint32_t sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t up = (uint32_t)__shfl_up((int)sum, d);
-            if (lane >= d) sum += up;
-        }
-        const uint64_t beyond = __ballot(before + sum > t);
+        int64_t lo, hi;
+        const uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, empty, lo, hi);
+        const uint32_t sum = wave_prefix(n);
+        const uint64_t beyond = __ballot((before + sum) * tiles > t);
         if (beyond) {
-            const int at = __ffsll((unsigned long long)beyond) - 1;
-            const int64_t glo = uniform64(__shfl(lo, at)), ghi = uniform64(__shfl(hi, at));
-            const uint32_t count = uniform((uint32_t)__shfl((int)n, at)), first = before + uniform((uint32_t)__shfl((int)sum, at)) - count;
-            const int64_t clo = glo + ((int64_t)(t - first) << log2);
-            const int64_t chi = clo + ((int64_t)1 << log2);
-            return {g0 + at, clo, chi < ghi ? chi : ghi, first, count};
+            const int found = __ffsll((unsigned long long)beyond) - 1;
+            const int64_t glo = uniform64(__shfl(lo, found)), ghi = uniform64(__shfl(hi, found));
+            const uint32_t count = uniform((uint32_t)__shfl((int)n, found)), first = before + uniform((uint32_t)__shfl((int)sum, found)) - count;
+            const uint32_t in_group = t - first * tiles, chunk = tiles == 1 ? in_group : in_group % count;
+            const int64_t clo = glo + ((int64_t)chunk << log2), chi = clo + ((int64_t)1 << log2);
+            return {g0 + found, clo, chi < ghi ? chi : ghi, first + chunk, count, tiles == 1 ? 0 : in_group / count};
         }
         before += uniform((uint32_t)__shfl((int)sum, 63));
     }
-    return {-1, 0, 0, 0, 0};
+    return {-1, 0, 0, 0, 0, 0};
 }
 
 }  // namespace pcc_train

@@ -30,6 +30,7 @@ struct Grouped {
     int groups, in, out, act;
     int log2;           // rows of a chunk
     int y32;            // y is fp32
+    int wide_out, wide_x;   // four values of a row of the result, of x, can be stored, read in one piece
     uint32_t tiles_m, tiles_n;
 };
 
@@ -59,63 +60,170 @@ struct TileLds {
     }
 };
 
-// Fill a tile from memory, zeros where there is nothing.  base is the value of index 0, k 0.
+typedef __attribute__((address_space(3))) void lds_void;
+
+// An operand in memory, and a workgroup's way through it in steps of 64 k.  Where rows begin at even elements (`wide`), chunks go from
+// memory to LDS without a register, 16 bytes a lane; a chunk that is cut by the end of its row is read value by value, and what lies
+// beyond the operand is zero: such a lane's offset is beyond the buffer's end, for which the load gives zeros.  Rows at
+// odd elements are read value by value.
 template <bool ACROSS>
-__device__ __forceinline__ void stage(u16* lds, const u16* base, size_t ld, int64_t i0, int64_t ni, int64_t k0, int64_t nk) {
+struct Source {
+    const u16* base;            // index i0, k 0
+    size_t ld;
+    int64_t ni, nk;             // indices from i0 on, all k
+    uint32_t offset[4];         // bytes of this lane's chunks from base + the step
+    static constexpr uint32_t kNone = 0x7FFFFF00u;      // beyond the buffer (rows are at most 2^22 values, a tile has 128)
+
+    __device__ void init(const u16* b, size_t stride, int64_t i0, int64_t n_index, int64_t n_k) {
+        base = b + (ACROSS ? (size_t)i0 : (size_t)i0 * stride);
+        ld = stride;
+        ni = n_index - i0;
+        nk = n_k;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        const int t = threadIdx.x + kTileThreads * s;
-        const int r = t / TileLds<ACROSS>::kChunks, c = t % TileLds<ACROSS>::kChunks;
-        const int64_t row = (ACROSS ? k0 : i0) + r, rows = ACROSS ? nk : ni;
-        const int64_t col = (ACROSS ? i0 : k0) + 8 * c, cols = ACROSS ? ni : nk;
-        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row < rows)
-            for (int j = 0; j < 8; ++j)
-                if (col + j < cols) v[j] = base[(size_t)row * ld + (size_t)(col + j)];
-        *reinterpret_cast<u16x8*>(lds + TileLds<ACROSS>::at(r, c)) = v;
+        for (int s = 0; s < 4; ++s) {
+            int r, c;
+            place(s, r, c);
+            const bool there = ACROSS ? 8 * c < ni : r < ni;
+            offset[s] = there ? (uint32_t)(((size_t)r * ld + 8 * c) * 2) : kNone;
+        }
     }
-}
+    __device__ static void place(int s, int& r, int& c) {
+        const int slot = threadIdx.x + kTileThreads * s;
+        r = slot / TileLds<ACROSS>::kChunks;
+        c = (slot % TileLds<ACROSS>::kChunks) ^ (ACROSS ? 2 * (r & 7) : (r & 7));
+    }
+    // Values of a chunk that are there, at k0.
+    __device__ int values(int r, int c, int64_t k0) const {
+        const int64_t n = ACROSS ? (k0 + r < nk ? ni - 8 * c : 0) : (r < ni ? nk - k0 - 8 * c : 0);
+        return n < 0 ? 0 : n > 8 ? 8 : (int)n;
+    }
+    __device__ void one_by_one(u16* lds, int s, int64_t k0, int n) const {
+        int r, c;
+        place(s, r, c);
+        const u16* from = base + (ACROSS ? (size_t)(k0 + r) * ld + 8 * c : (size_t)r * ld + (size_t)k0 + 8 * c);
+        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) v[j] = from[j];
+        *reinterpret_cast<u16x8*>(lds + (threadIdx.x + kTileThreads * s) * 8) = v;
+    }
+    template <bool WIDE>
+    __device__ void stage(u16* lds, int64_t k0) const {
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                int r, c;
+                place(s, r, c);
+                one_by_one(lds, s, k0, values(r, c, k0));
+            }
+        } else {
+            const __amdgpu_buffer_rsrc_t from =
+                __builtin_amdgcn_make_buffer_rsrc((void*)(base + (ACROSS ? (size_t)k0 * ld : (size_t)k0)), 0, (int)kNone, 0x00020000);
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            const bool whole = k0 + kTileK <= nk && (!ACROSS || ni % 8 == 0 || ni >= kTile);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                lds_void* to = (lds_void*)(lds + (64 * wave + kTileThreads * s) * 8);
+                if (whole) {
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, offset[s], 0, 0, 0);
+                } else {
+                    int r, c;
+                    place(s, r, c);
+                    const int n = values(r, c, k0);
+                    if (n == 0 || n == 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, n ? offset[s] : kNone, 0, 0, 0);
+                    else one_by_one(lds, s, k0, n);
+                }
+            }
+        }
+    }
+};
 
 enum Mode { kForward, kBackward, kWeights };
 
-// Four waves, each 64 x 64 of the tile's 128 x 128.
+__device__ __forceinline__ void store_four(float* to, f32x4 v, int left, bool wide) {
+    if (wide && left == 4) { *reinterpret_cast<f32x4*>(to) = v; return; }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) to[e] = v[e];
+}
+
+// Bias and activation, or the activation's derivative, of four neighbouring results of a row, and their store.
 template <class T, int MODE>
-__global__ __launch_bounds__(kTileThreads) void grouped_tile_kernel(Grouped a) {
+__device__ __forceinline__ void finish_four(const Grouped& a, int group, size_t row, int64_t m, f32x4 v, int left) {
+    const bool wide = a.wide_out && left == 4;
+    if (MODE == kForward) {
+        if (a.bias) {
+            const float* bias = a.bias + (size_t)group * a.out + m;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += bias[e < left ? e : 0];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
+    } else if (a.act != PCC_ACT_NONE) {
+        const u16* x = a.x + row * a.ldx + m;
+        u16x4 s = {0, 0, 0, 0};
+        if (a.wide_x && left == 4) s = *reinterpret_cast<const u16x4*>(x);
+        else for (int e = 0; e < 4; ++e) if (e < left) s[e] = x[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = times_derivative(v[e], from16<T>(s[e]), a.act);
+    }
+    const size_t at = row * a.ldy + m;
+    if (a.y32) { store_four(static_cast<float*>(a.y) + at, v, left, wide); return; }
+    u16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = to16<T>(v[e]);
+    u16* y = static_cast<u16*>(a.y) + at;
+    if (wide) *reinterpret_cast<u16x4*>(y) = o;
+    else for (int e = 0; e < 4; ++e) if (e < left) y[e] = o[e];
+}
+
+// Four waves, each 64 x 64 of the tile's 128 x 128.  Two tiles in LDS for each operand: the next step's is filled while this one's is
+// multiplied.
+template <class T, int MODE, bool WIDE>
+__global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a) {
     constexpr bool kPAcross = MODE != kForward, kQAcross = MODE == kWeights;
-    __shared__ __align__(16) u16 lds_p[kTile * kTileK], lds_q[kTile * kTileK];
+    __shared__ __align__(16) u16 lds[2][2][kTile * kTileK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
-    const uint32_t per_chunk = a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
-    const uint32_t id = blockIdx.x / per_chunk, rest = blockIdx.x % per_chunk;
-    const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, id, MODE == kWeights);
+    const uint32_t tiles = a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
+    const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, tiles, blockIdx.x, MODE == kWeights);
     if (ch.group < 0) return;
-    const int64_t m0 = (int64_t)(rest % a.tiles_m) * kTile, n0 = MODE == kWeights ? (int64_t)(rest / a.tiles_m) * kTile : 0;
+    const int64_t m0 = (int64_t)(ch.part % a.tiles_m) * kTile, n0 = MODE == kWeights ? (int64_t)(ch.part / a.tiles_m) * kTile : 0;
     const int64_t n_rows = ch.hi - ch.lo;
     const u16* w = a.w ? a.w + (size_t)ch.group * a.in * a.out : nullptr;
-    const u16* p = MODE == kWeights ? a.x + (size_t)ch.lo * a.ldx : w;
-    const u16* q = MODE == kForward ? a.x + (size_t)ch.lo * a.ldx : a.dz + (size_t)ch.lo * a.lddz;
-    const size_t ldp = MODE == kWeights ? a.ldx : (size_t)a.in, ldq = MODE == kForward ? a.ldx : a.lddz;
     const int64_t np = MODE == kForward ? a.out : a.in, nq = MODE == kWeights ? a.out : n_rows;
     const int64_t nk = MODE == kForward ? a.in : MODE == kBackward ? a.out : n_rows;
+    Source<kPAcross> p;
+    Source<kQAcross> q;
+    p.init(MODE == kWeights ? a.x + (size_t)ch.lo * a.ldx : w, MODE == kWeights ? a.ldx : (size_t)a.in, m0, np, nk);
+    if (MODE == kForward) q.init(a.x + (size_t)ch.lo * a.ldx, a.ldx, n0, nq, nk);
+    else q.init(a.dz + (size_t)ch.lo * a.lddz, a.lddz, n0, nq, nk);
 
     f32x4 acc[4][4] = {}, sums[4] = {};
     const bool with_db = MODE == kWeights && a.db && m0 == 0 && wm == 0;
     u16x8 ones;
     for (int j = 0; j < 8; ++j) ones[j] = T::kOne;
-    for (int64_t k0 = 0; k0 < nk; k0 += kTileK) {
-        stage<kPAcross>(lds_p, p, ldp, m0, np, k0, nk);
-        stage<kQAcross>(lds_q, q, ldq, n0, nq, k0, nk);
+    if (nk > 0) {
+        p.template stage<WIDE>(lds[0][0], 0);
+        q.template stage<WIDE>(lds[0][1], 0);
+    }
+    int now = 0;
+    for (int64_t k0 = 0; k0 < nk; k0 += kTileK, now ^= 1) {
+        __builtin_amdgcn_s_waitcnt(0);      // this step's chunks are in LDS: the barrier alone does not wait for loads that go there
         __syncthreads();
+        if (k0 + kTileK < nk) {
+            p.template stage<WIDE>(lds[now ^ 1][0], k0 + kTileK);
+            q.template stage<WIDE>(lds[now ^ 1][1], k0 + kTileK);
+        }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             u16x8 fp[4], fq[4];
-            for (int i = 0; i < 4; ++i) fp[i] = TileLds<kPAcross>::operand(lds_p, 4 * wm + i, kk, lane);
-            for (int i = 0; i < 4; ++i) fq[i] = TileLds<kQAcross>::operand(lds_q, 4 * wn + i, kk, lane);
+            for (int i = 0; i < 4; ++i) fp[i] = TileLds<kPAcross>::operand(lds[now][0], 4 * wm + i, kk, lane);
+            for (int i = 0; i < 4; ++i) fq[i] = TileLds<kQAcross>::operand(lds[now][1], 4 * wn + i, kk, lane);
             for (int i = 0; i < 4; ++i)
                 for (int j = 0; j < 4; ++j) acc[i][j] = T::mfma(fp[i], fq[j], acc[i][j]);
             if (with_db)
                 for (int j = 0; j < 4; ++j) sums[j] = T::mfma(ones, fq[j], sums[j]);
         }
-        __syncthreads();
     }
 
     float* dw = nullptr;
@@ -126,7 +234,7 @@ __global__ __launch_bounds__(kTileThreads) void grouped_tile_kernel(Grouped a) {
             dw = a.dw + (size_t)ch.group * size;
             db = a.db ? a.db + (size_t)ch.group * a.out : nullptr;
         } else {
-            dw = a.partial + (size_t)id * (size + a.out);
+            dw = a.partial + (size_t)ch.id * (size + a.out);
             db = dw + size;
         }
     }
@@ -136,21 +244,11 @@ __global__ __launch_bounds__(kTileThreads) void grouped_tile_kernel(Grouped a) {
         if (n >= nq) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t m = m0 + 64 * wm + 16 * i + 4 * (lane >> 4) + e;
-                if (m >= np) continue;
-                float v = acc[i][j][e];
-                if (MODE == kWeights) {
-                    dw[(size_t)n * a.in + m] = v;
-                } else {
-                    const size_t at = (size_t)(ch.lo + n) * a.ldy + m;
-                    if (MODE == kForward) v = activate(a.bias ? v + a.bias[(size_t)ch.group * a.out + m] : v, a.act);
-                    else if (a.act != PCC_ACT_NONE) v = times_derivative(v, from16<T>(a.x[(size_t)(ch.lo + n) * a.ldx + m]), a.act);
-                    if (a.y32) static_cast<float*>(a.y)[at] = v;
-                    else static_cast<u16*>(a.y)[at] = to16<T>(v);
-                }
-            }
+            const int64_t m = m0 + 64 * wm + 16 * i + 4 * (lane >> 4);
+            const int left = np - m >= 4 ? 4 : (int)(np - m);
+            if (left <= 0) continue;
+            if (MODE == kWeights) store_four(dw + (size_t)n * a.in + m, acc[i][j], left, a.in % 4 == 0 && a.wide_out);
+            else finish_four<T, MODE>(a, ch.group, (size_t)(ch.lo + n), m, acc[i][j], left);
         }
         if (with_db && lane < 16) db[n] = sums[j][0];
     }
@@ -159,18 +257,12 @@ __global__ __launch_bounds__(kTileThreads) void grouped_tile_kernel(Grouped a) {
 // Chunks' sums to those of their group, in the chunks' order.  A group of one chunk was written where it belongs.
 __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
     const int g = blockIdx.y;
-    // the chunks of groups 0..g-1 come first: the chunk that a search for group g's first one finds
     const int lane = threadIdx.x & 63;
     uint32_t first = 0, count = 0;
     for (int g0 = 0; g0 <= g; g0 += 64) {
-        const int i = g0 + lane;
-        uint32_t n = 0;
-        if (i <= g) {
-            const int64_t lo = clamp64(a.off[i], 0, a.rows), hi = clamp64(a.off[i + 1], lo, a.rows);
-            n = (uint32_t)((hi - lo + ((int64_t)1 << a.log2) - 1) >> a.log2);
-            if (n == 0) n = 1;
-        }
-        if (i == g) count = n;
+        int64_t lo, hi;
+        uint32_t n = group_chunks(a.off, g0 + lane, g + 1, a.rows, a.log2, true, lo, hi);
+        if (g0 + lane == g) count = n;
         for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
         first += n;
     }
