@@ -7,6 +7,7 @@
 #include "train_adamw.h"
 #include "train_grouped.h"
 #include "train_loss.h"
+#include "train_narrow.h"
 
 using namespace pcc_train;
 
@@ -98,16 +99,99 @@ template <class T, int MODE>
 int launch_tiles(Grouped& a, hipStream_t st) {
     a.tiles_m = (uint32_t)(((MODE == kForward ? a.out : a.in) + kTile - 1) / kTile);
     a.tiles_n = (uint32_t)((a.out + kTile - 1) / kTile);
+    a.mult = 1;
     const uint64_t chunks = ((uint64_t)a.rows >> a.log2) + a.groups, blocks = chunks * a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
     if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
     const bool wide = (MODE == kBackward || even_rows(a.x, a.ldx)) && (MODE == kForward || even_rows(a.dz, a.lddz)) &&
                       (MODE == kWeights || even_rows(a.w, (size_t)a.in));
     a.wide_x = aligned(a.x, 8) && a.ldx % 4 == 0;
-    a.wide_out = MODE == kWeights ? aligned(a.dw, 16) && aligned(a.partial, 16) && ((size_t)a.in * a.out + a.out) % 4 == 0
-                                  : aligned(a.y, a.y32 ? 16 : 8) && a.ldy % 4 == 0;
+    a.wide_dw = aligned(a.dw, 16) && aligned(a.partial, 16) && a.out % 4 == 0;
+    a.wide_out = aligned(a.y, a.y32 ? 16 : 8) && a.ldy % 4 == 0;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);     // a multiple of the dies: see find_chunk
     auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kTileThreads), 0, st, a); }); };
     return wide ? go(grouped_tile_kernel<T, MODE, true>) : go(grouped_tile_kernel<T, MODE, false>);
+}
+
+// Chunks of about rows / want rows, in steps of 1/4 to 1/8 of a power of two, and a multiple of `unit` (a power of two).  The
+// number of chunks (with one more for each group's part) is at most `want`, if there are not too many groups for that.
+void chunk_rows(Grouped& a, uint64_t want, int unit_log2) {
+    const uint64_t whole = want > 2 * (uint64_t)a.groups ? want - a.groups : std::max<uint64_t>(want, 1) / 2 + 1;
+    const uint64_t rows = std::max<uint64_t>(((uint64_t)a.rows + whole - 1) / whole, 1);
+    a.log2 = unit_log2;
+    while (a.log2 < 24 && ((uint64_t)8 << a.log2) < rows) ++a.log2;     // rows of a chunk are counted in 32 bits
+    a.mult = (uint32_t)std::min<uint64_t>((rows + ((uint64_t)1 << a.log2) - 1) >> a.log2, 8);
+}
+uint64_t chunk_count(const Grouped& a) { return (uint64_t)a.rows / ((uint64_t)a.mult << a.log2) + a.groups; }
+
+constexpr int kMaxLds = 160 * 1024;
+
+// More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
+template <class K>
+bool allow_lds(K kernel, size_t bytes) {
+    return bytes <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+}
+
+// The forward pass with the weights in LDS: for inputs of up to 192 features, a multiple of eight, in rows that begin at even
+// elements, and weights that leave a compute unit room for two workgroups.
+bool narrow_forward_fits(const Grouped& a) {
+    return a.in <= 192 && a.in % 8 == 0 && even_rows(a.x, a.ldx) && aligned(a.w, 4) && narrow_forward_lds(a.in, a.out) <= kMaxLds / 2;
+}
+
+template <class T>
+int launch_narrow_forward(Grouped& a, hipStream_t st) {
+    chunk_rows(a, 256, 5);
+    a.wide_out = aligned(a.y, 16) && a.ldy % (a.y32 ? 4 : 8) == 0;
+    const uint64_t blocks = chunk_count(a);
+    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
+    const size_t weights = narrow_forward_lds(a.in, a.out), rows = narrow_rows_lds(a.out, a.y32);
+    const int threads = kNarrowThreads;
+    a.staged = even_rows(a.y, a.ldy * (a.y32 ? 2 : 1)) && weights + threads / 64 * rows <= kMaxLds && narrow_row_pieces(a.out, a.y32) <= 64;
+    const size_t lds = weights + (a.staged ? threads / 64 * rows : 0);
+    auto go = [&](auto kernel) {
+        if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
+        return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), lds, st, a); });
+    };
+    switch ((a.in + 31) / 32) {
+        case 1: return go(grouped_narrow_forward_kernel<T, 1>);
+        case 2: return go(grouped_narrow_forward_kernel<T, 2>);
+        case 3: return go(grouped_narrow_forward_kernel<T, 3>);
+        case 4: return go(grouped_narrow_forward_kernel<T, 4>);
+        case 5: return go(grouped_narrow_forward_kernel<T, 5>);
+        default: return go(grouped_narrow_forward_kernel<T, 6>);
+    }
+}
+
+// The backward pass with everything of a step in LDS: for up to 192 features to each side, the inputs a multiple of eight, in
+// rows that begin at even elements.  Returns the rows of a step, 0: not for this call.
+int narrow_backward_rows(const Grouped& a) {
+    if (a.in > 192 || a.out > 192 || a.in % 8 || !a.dw || !even_rows(a.x, a.ldx) || !even_rows(a.dz, a.lddz)) return 0;
+    return narrow_backward_lds(a.in, a.out, 64, a.y != nullptr) <= (size_t)kMaxLds ? 64 : 32;
+}
+uint64_t backward_chunks(Grouped& a) {
+    chunk_rows(a, 256, 6);
+    return chunk_count(a);
+}
+
+template <class T>
+int launch_narrow_backward(Grouped& a, int step_rows, hipStream_t st) {
+    a.step_rows = step_rows;
+    const uint64_t blocks = backward_chunks(a);
+    a.wide_x = 1;
+    a.wide_out = a.y && aligned(a.y, 16) && a.ldy % 8 == 0;
+    a.wide_dw = aligned(a.dw, 16) && aligned(a.partial, 16) && a.out % 4 == 0;
+    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
+    const size_t lds = narrow_backward_lds(a.in, a.out, step_rows, a.y != nullptr);
+    auto go = [&](auto kernel) {
+        if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
+        return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kNarrowThreads), lds, st, a); });
+    };
+    auto with_n = [&](auto mb) {
+        constexpr int M = decltype(mb)::value;
+        return a.out <= 64 ? go(grouped_narrow_backward_kernel<T, M, 1>) : a.out <= 128 ? go(grouped_narrow_backward_kernel<T, M, 2>) : go(grouped_narrow_backward_kernel<T, M, 3>);
+    };
+    return a.in <= 64 ? with_n(std::integral_constant<int, 2>{}) : a.in <= 128 ? with_n(std::integral_constant<int, 4>{}) : with_n(std::integral_constant<int, 6>{});
 }
 
 }  // namespace
@@ -147,16 +231,26 @@ int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.bias = d_bias; a.off = d_offsets; a.y = d_y;
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = act;
     a.y32 = y_type == PCC_FP32;
-    a.log2 = 7;
     hipStream_t st = (hipStream_t)hip_stream;
+    if (narrow_forward_fits(a)) return type == PCC_BF16 ? launch_narrow_forward<Bf16>(a, st) : launch_narrow_forward<Fp16>(a, st);
+    a.log2 = 7;
     return type == PCC_BF16 ? launch_tiles<Bf16, kForward>(a, st) : launch_tiles<Fp16, kForward>(a, st);
 }
 
 size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, int out) {
     if (!features_ok(in, out, groups, rows)) return 0;
+    // enough for either kernel: which one runs depends on the tensors' places too
+    const size_t values = (size_t)in * out + out;
     const int log2 = weights_log2(rows, in, out);
-    if (rows <= (size_t)1 << log2) return 0;
-    return ((rows >> log2) + groups) * ((size_t)in * out + out) * sizeof(float);
+    size_t chunks = rows <= (size_t)1 << log2 ? 0 : (rows >> log2) + groups;
+    if (in <= 192 && out <= 192) {
+        Grouped a = {};
+        a.rows = (int64_t)rows;
+        a.groups = groups;
+        const size_t narrow = backward_chunks(a);
+        if (rows > (size_t)a.mult << a.log2) chunks = std::max(chunks, narrow);
+    }
+    return chunks * values * sizeof(float);
 }
 
 int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size_t ldx, const void* d_w, const int64_t* d_offsets,
@@ -175,21 +269,25 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.dz = (const u16*)d_dz; a.off = d_offsets; a.y = d_dx; a.dw = d_dw; a.db = d_db;
     a.ldx = ldx; a.lddz = lddz; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = x_act;
     a.partial = (float*)d_workspace;
-    if (d_dx && rows) {
-        a.log2 = 7;
-        const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kBackward>(a, st) : launch_tiles<Fp16, kBackward>(a, st);
+    if (const int step = narrow_backward_rows(a)) {
+        const int rc = type == PCC_BF16 ? launch_narrow_backward<Bf16>(a, step, st) : launch_narrow_backward<Fp16>(a, step, st);
+        if (rc != PCC_OK) return rc;
+    } else {
+        if (d_dx && rows) {
+            a.log2 = 7;
+            const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kBackward>(a, st) : launch_tiles<Fp16, kBackward>(a, st);
+            if (rc != PCC_OK) return rc;
+        }
+        if (!d_dw) return PCC_OK;
+        a.log2 = weights_log2(rows, in, out);
+        const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kWeights>(a, st) : launch_tiles<Fp16, kWeights>(a, st);
         if (rc != PCC_OK) return rc;
     }
-    if (d_dw) {
-        a.log2 = weights_log2(rows, in, out);
-        int rc = type == PCC_BF16 ? launch_tiles<Bf16, kWeights>(a, st) : launch_tiles<Fp16, kWeights>(a, st);
-        if (rc != PCC_OK || !need) return rc;
-        const size_t values = (size_t)in * out + out;
-        return launch([&] {
-            hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)std::min<size_t>((values + 255) / 256, 1024), groups), dim3(256), 0, st, a);
-        });
-    }
-    return PCC_OK;
+    if (rows <= (size_t)a.mult << a.log2) return PCC_OK;        // no group can have two chunks
+    const size_t values = (size_t)in * out + out;
+    return launch([&] {
+        hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)std::min<size_t>((values + 255) / 256, 1024), groups), dim3(256), 0, st, a);
+    });
 }
 
 int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, const float* d_weight, size_t count, int K, int dist,

@@ -59,7 +59,7 @@ __device__ __forceinline__ float times_derivative(float d, float x, int act) {
 
 // ---------------------------------------------------------------------------
 // Ragged groups.  off[0..groups] are device data, so no launch knows the groups' sizes: a launch has a workgroup for
-// every chunk of 2^log2 rows that could exist (rows / 2^log2, and one more a group for the parts), and a
+// every chunk of mult * 2^log2 rows that could exist (rows / that, and one more a group for the parts), and a
 // workgroup looks up which rows are its own.  Offsets are clamped to the rows there are and to rising order, so
 // that wrong ones make wrong results but no access outside the tensors.
 // ---------------------------------------------------------------------------
@@ -79,11 +79,11 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
 }
 
 // Rows of group g and how many chunks they make; with `empty`, a group without rows has one, of no rows.
-__device__ __forceinline__ uint32_t group_chunks(const int64_t* __restrict__ off, int g, int groups, int64_t rows, int log2, bool empty, int64_t& lo, int64_t& hi) {
+__device__ __forceinline__ uint32_t group_chunks(const int64_t* __restrict__ off, int g, int groups, int64_t rows, int log2, uint32_t mult, bool empty, int64_t& lo, int64_t& hi) {
     if (g >= groups) { lo = hi = 0; return 0; }
     lo = clamp64(off[g], 0, rows);
     hi = clamp64(off[g + 1], lo, rows);
-    const uint32_t n = (uint32_t)((hi - lo + ((int64_t)1 << log2) - 1) >> log2);
+    const uint32_t n = ((uint32_t)((hi - lo + ((int64_t)1 << log2) - 1) >> log2) + mult - 1) / mult;
     return empty && n == 0 ? 1 : n;
 }
 __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
@@ -99,30 +99,33 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
 // Workgroup b's chunk and tile (of `tiles` that each chunk has).  All lanes of a wave together; the result is the same in every lane.
 // The chip's eight dies take workgroups in turn and have an L2 each, so die d gets the d-th eighth of the work, and within a group
 // the chunks of one tile come one after the other: they read the same weights at about the same time.
-__device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t tiles, uint32_t b, bool empty) {
+__device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t mult, uint32_t tiles, uint32_t b, bool empty) {
     const int lane = threadIdx.x & 63;
     uint32_t total = 0;
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        int64_t lo, hi;
-        uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, empty, lo, hi);
+    if (groups > 64) {                  // else the search itself says it
+        for (int g0 = 0; g0 < groups; g0 += 64) {
+            int64_t lo, hi;
+            uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi);
 #pragma unroll
-        for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
-        total += uniform(n);
+            for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
+            total += uniform(n);
+        }
     }
-    const uint32_t all = total * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
-    if (at >= each || t >= all) return {-1, 0, 0, 0, 0, 0};
     uint32_t before = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
         int64_t lo, hi;
-        const uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, empty, lo, hi);
-        const uint32_t sum = wave_prefix(n);
+        const uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi);
+        const uint32_t sum = groups == 1 ? uniform(n) : wave_prefix(n);
+        if (groups <= 64) total = groups == 1 ? sum : (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+        const uint32_t all = total * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
+        if (at >= each || t >= all) break;
         const uint64_t beyond = __ballot((before + sum) * tiles > t);
         if (beyond) {
             const int found = __ffsll((unsigned long long)beyond) - 1;
             const int64_t glo = uniform64(__shfl(lo, found)), ghi = uniform64(__shfl(hi, found));
             const uint32_t count = uniform((uint32_t)__shfl((int)n, found)), first = before + uniform((uint32_t)__shfl((int)sum, found)) - count;
             const uint32_t in_group = t - first * tiles, chunk = tiles == 1 ? in_group : in_group % count;
-            const int64_t clo = glo + ((int64_t)chunk << log2), chi = clo + ((int64_t)1 << log2);
+            const int64_t size = (int64_t)mult << log2, clo = glo + (int64_t)chunk * size, chi = clo + size;
             return {g0 + found, clo, chi < ghi ? chi : ghi, first + chunk, count, tiles == 1 ? 0 : in_group / count};
         }
         before += uniform((uint32_t)__shfl((int)sum, 63));

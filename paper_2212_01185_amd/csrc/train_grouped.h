@@ -28,9 +28,12 @@ struct Grouped {
     size_t ldx, lddz, ldy;
     int64_t rows;
     int groups, in, out, act;
-    int log2;           // rows of a chunk
+    int log2;           // rows of a chunk: mult * 2^log2
+    uint32_t mult;
     int y32;            // y is fp32
-    int wide_out, wide_x;   // four values of a row of the result, of x, can be stored, read in one piece
+    int staged;         // forward, narrow: outputs go through LDS
+    int step_rows;      // backward, narrow: rows of a step
+    int wide_out, wide_x, wide_dw;  // four values of a row of the result, of x, of dw can be stored, read in one piece
     uint32_t tiles_m, tiles_n;
 };
 
@@ -177,6 +180,28 @@ __device__ __forceinline__ void finish_four(const Grouped& a, int group, size_t 
     else for (int e = 0; e < 4; ++e) if (e < left) y[e] = o[e];
 }
 
+// Eight neighbouring results of a row after the activation, `left` of them there.
+template <class T>
+__device__ __forceinline__ void store_eight(const Grouped& a, size_t at, f32x4 v0, f32x4 v1, int left, int act) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v0[e] = activate(v0[e], act); v1[e] = activate(v1[e], act); }
+    if (a.y32) {
+        float* y = static_cast<float*>(a.y) + at;
+        store_four(y, v0, left < 4 ? left : 4, a.wide_out);
+        if (left > 4) store_four(y + 4, v1, left < 8 ? left - 4 : 4, a.wide_out);
+        return;
+    }
+    u16x8 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { o[e] = to16<T>(v0[e]); o[4 + e] = to16<T>(v1[e]); }
+    u16* y = static_cast<u16*>(a.y) + at;
+    if (a.wide_out && left >= 8) *reinterpret_cast<u16x8*>(y) = o;
+    else
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) y[e] = o[e];
+}
+
 // Four waves, each 64 x 64 of the tile's 128 x 128.  Two tiles in LDS for each operand: the next step's is filled while this one's is
 // multiplied.
 template <class T, int MODE, bool WIDE>
@@ -185,7 +210,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
     __shared__ __align__(16) u16 lds[2][2][kTile * kTileK];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
     const uint32_t tiles = a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
-    const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, tiles, blockIdx.x, MODE == kWeights);
+    const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, a.mult, tiles, blockIdx.x, MODE == kWeights);
     if (ch.group < 0) return;
     const int64_t m0 = (int64_t)(ch.part % a.tiles_m) * kTile, n0 = MODE == kWeights ? (int64_t)(ch.part / a.tiles_m) * kTile : 0;
     const int64_t n_rows = ch.hi - ch.lo;
@@ -247,7 +272,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
             const int64_t m = m0 + 64 * wm + 16 * i + 4 * (lane >> 4);
             const int left = np - m >= 4 ? 4 : (int)(np - m);
             if (left <= 0) continue;
-            if (MODE == kWeights) store_four(dw + (size_t)n * a.in + m, acc[i][j], left, a.in % 4 == 0 && a.wide_out);
+            if (MODE == kWeights) store_four(dw + (size_t)n * a.in + m, acc[i][j], left, a.in % 4 == 0 && a.wide_dw);
             else finish_four<T, MODE>(a, ch.group, (size_t)(ch.lo + n), m, acc[i][j], left);
         }
         if (with_db && lane < 16) db[n] = sums[j][0];
@@ -261,7 +286,7 @@ __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
     uint32_t first = 0, count = 0;
     for (int g0 = 0; g0 <= g; g0 += 64) {
         int64_t lo, hi;
-        uint32_t n = group_chunks(a.off, g0 + lane, g + 1, a.rows, a.log2, true, lo, hi);
+        uint32_t n = group_chunks(a.off, g0 + lane, g + 1, a.rows, a.log2, a.mult, true, lo, hi);
         if (g0 + lane == g) count = n;
         for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
         first += n;
