@@ -105,7 +105,7 @@ int launch_tiles(Grouped& a, hipStream_t st) {
     const bool wide = (MODE == kBackward || even_rows(a.x, a.ldx)) && (MODE == kForward || even_rows(a.dz, a.lddz)) &&
                       (MODE == kWeights || even_rows(a.w, (size_t)a.in));
     a.wide_x = aligned(a.x, 8) && a.ldx % 4 == 0;
-    a.wide_dw = aligned(a.dw, 16) && aligned(a.partial, 16) && a.out % 4 == 0;
+    a.wide_dw = aligned(a.dw, 16) && (size_t)a.in * a.out % 4 == 0;
     a.wide_out = aligned(a.y, a.y32 ? 16 : 8) && a.ldy % 4 == 0;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);     // a multiple of the dies: see find_chunk
     auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kTileThreads), 0, st, a); }); };
@@ -122,8 +122,6 @@ void chunk_rows(Grouped& a, uint64_t want, int unit_log2) {
     a.mult = (uint32_t)std::min<uint64_t>((rows + ((uint64_t)1 << a.log2) - 1) >> a.log2, 8);
 }
 uint64_t chunk_count(const Grouped& a) { return (uint64_t)a.rows / ((uint64_t)a.mult << a.log2) + a.groups; }
-
-constexpr int kMaxLds = 160 * 1024;
 
 // More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
 template <class K>
@@ -162,11 +160,11 @@ int launch_narrow_forward(Grouped& a, hipStream_t st) {
     }
 }
 
-// The backward pass with everything of a step in LDS: for up to 192 features to each side, the inputs a multiple of eight, in
-// rows that begin at even elements.  Returns the rows of a step, 0: not for this call.
-int narrow_backward_rows(const Grouped& a) {
-    if (a.in > 192 || a.out > 192 || a.in % 8 || !a.dw || !even_rows(a.x, a.ldx) || !even_rows(a.dz, a.lddz)) return 0;
-    return narrow_backward_lds(a.in, a.out, 64, a.y != nullptr) <= (size_t)kMaxLds ? 64 : 32;
+// The backward pass in one kernel: for up to 192 features to each side, the inputs a multiple of eight and the outputs of
+// two, in rows that begin at even elements.
+bool narrow_backward_fits(const Grouped& a) {
+    return a.in <= 192 && a.out <= 192 && a.in % 8 == 0 && a.out % 2 == 0 && a.dw && even_rows(a.x, a.ldx) && even_rows(a.dz, a.lddz) &&
+           (!a.y || (aligned(a.w, 4) && aligned(a.y, 4) && a.ldy % 2 == 0));
 }
 uint64_t backward_chunks(Grouped& a) {
     chunk_rows(a, 256, 6);
@@ -174,24 +172,33 @@ uint64_t backward_chunks(Grouped& a) {
 }
 
 template <class T>
-int launch_narrow_backward(Grouped& a, int step_rows, hipStream_t st) {
-    a.step_rows = step_rows;
+int launch_narrow_backward(Grouped& a, hipStream_t st) {
     const uint64_t blocks = backward_chunks(a);
-    a.wide_x = 1;
-    a.wide_out = a.y && aligned(a.y, 16) && a.ldy % 8 == 0;
-    a.wide_dw = aligned(a.dw, 16) && aligned(a.partial, 16) && a.out % 4 == 0;
+    a.wide_out = 1;
+    a.wide_dw = aligned(a.dw, 16) && (size_t)a.in * a.out % 4 == 0;
     if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
-    const size_t lds = narrow_backward_lds(a.in, a.out, step_rows, a.y != nullptr);
-    auto go = [&](auto kernel) {
+    auto go = [&](auto kernel, size_t lds) {
         if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
         return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kNarrowThreads), lds, st, a); });
     };
-    auto with_n = [&](auto mb) {
-        constexpr int M = decltype(mb)::value;
-        return a.out <= 64 ? go(grouped_narrow_backward_kernel<T, M, 1>) : a.out <= 128 ? go(grouped_narrow_backward_kernel<T, M, 2>) : go(grouped_narrow_backward_kernel<T, M, 3>);
+    auto with_out = [&](auto pairs) {
+        constexpr int P = decltype(pairs)::value;
+        switch ((a.out + 31) / 32) {
+            case 1: case 2: return go(grouped_narrow_backward_kernel<T, P, 2>, NarrowBackward<P, 2>::kLds);
+            case 3: return go(grouped_narrow_backward_kernel<T, P, 3>, NarrowBackward<P, 3>::kLds);
+            case 4: return go(grouped_narrow_backward_kernel<T, P, 4>, NarrowBackward<P, 4>::kLds);
+            case 5: return go(grouped_narrow_backward_kernel<T, P, 5>, NarrowBackward<P, 5>::kLds);
+            default: return go(grouped_narrow_backward_kernel<T, P, 6>, NarrowBackward<P, 6>::kLds);
+        }
     };
-    return a.in <= 64 ? with_n(std::integral_constant<int, 2>{}) : a.in <= 128 ? with_n(std::integral_constant<int, 4>{}) : with_n(std::integral_constant<int, 6>{});
+    switch ((a.in + 31) / 32) {
+        case 1: return with_out(std::integral_constant<int, 1>{});
+        case 2: return with_out(std::integral_constant<int, 2>{});
+        case 3: case 4: return with_out(std::integral_constant<int, 4>{});
+        case 5: return with_out(std::integral_constant<int, 5>{});
+        default: return with_out(std::integral_constant<int, 6>{});
+    }
 }
 
 }  // namespace
@@ -240,7 +247,7 @@ int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float
 size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, int out) {
     if (!features_ok(in, out, groups, rows)) return 0;
     // enough for either kernel: which one runs depends on the tensors' places too
-    const size_t values = (size_t)in * out + out;
+    const size_t values = partial_values(in, out);
     const int log2 = weights_log2(rows, in, out);
     size_t chunks = rows <= (size_t)1 << log2 ? 0 : (rows >> log2) + groups;
     if (in <= 192 && out <= 192) {
@@ -269,8 +276,8 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.dz = (const u16*)d_dz; a.off = d_offsets; a.y = d_dx; a.dw = d_dw; a.db = d_db;
     a.ldx = ldx; a.lddz = lddz; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = x_act;
     a.partial = (float*)d_workspace;
-    if (const int step = narrow_backward_rows(a)) {
-        const int rc = type == PCC_BF16 ? launch_narrow_backward<Bf16>(a, step, st) : launch_narrow_backward<Fp16>(a, step, st);
+    if (narrow_backward_fits(a)) {
+        const int rc = type == PCC_BF16 ? launch_narrow_backward<Bf16>(a, st) : launch_narrow_backward<Fp16>(a, st);
         if (rc != PCC_OK) return rc;
     } else {
         if (d_dx && rows) {
@@ -286,7 +293,7 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
     if (rows <= (size_t)a.mult << a.log2) return PCC_OK;        // no group can have two chunks
     const size_t values = (size_t)in * out + out;
     return launch([&] {
-        hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)std::min<size_t>((values + 255) / 256, 1024), groups), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)((values + 63) / 64), groups), dim3(256), 0, st, a);
     });
 }
 

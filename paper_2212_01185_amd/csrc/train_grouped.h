@@ -32,7 +32,6 @@ struct Grouped {
     uint32_t mult;
     int y32;            // y is fp32
     int staged;         // forward, narrow: outputs go through LDS
-    int step_rows;      // backward, narrow: rows of a step
     int wide_out, wide_x, wide_dw;  // four values of a row of the result, of x, of dw can be stored, read in one piece
     uint32_t tiles_m, tiles_n;
 };
@@ -140,6 +139,9 @@ struct Source {
         }
     }
 };
+
+// Values of a chunk's sums in the workspace: dw, db, and up to a multiple of four.
+__host__ __device__ constexpr size_t partial_values(int in, int out) { return ((size_t)in * out + out + 3) / 4 * 4; }
 
 enum Mode { kForward, kBackward, kWeights };
 
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
             dw = a.dw + (size_t)ch.group * size;
             db = a.db ? a.db + (size_t)ch.group * a.out : nullptr;
         } else {
-            dw = a.partial + (size_t)ch.id * (size + a.out);
+            dw = a.partial + (size_t)ch.id * partial_values(a.in, a.out);
             db = dw + size;
         }
     }
@@ -279,10 +281,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
     }
 }
 
-// Chunks' sums to those of their group, in the chunks' order.  A group of one chunk was written where it belongs.
+// Chunks' sums to those of their group, always in the same order.  A group of one chunk was written where it belongs.  A workgroup has 64
+// values; 16 slices of its threads sum every 16th chunk, so that as many loads are on their way, then the slices are summed.
 __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
-    const int g = blockIdx.y;
-    const int lane = threadIdx.x & 63;
+    __shared__ __align__(16) f32x4 slices[16][16];
+    const int g = blockIdx.y, lane = threadIdx.x & 63;
     uint32_t first = 0, count = 0;
     for (int g0 = 0; g0 <= g; g0 += 64) {
         int64_t lo, hi;
@@ -294,12 +297,24 @@ __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
     for (int d = 32; d; d >>= 1) count += (uint32_t)__shfl_xor((int)count, d);
     first -= count;
     if (count <= 1) return;
-    const size_t size = (size_t)a.in * a.out, all = size + (a.db ? a.out : 0);
-    for (size_t e = (size_t)blockIdx.x * blockDim.x + threadIdx.x; e < all; e += (size_t)gridDim.x * blockDim.x) {
-        float s = 0.0f;
-        for (uint32_t c = 0; c < count; ++c) s += a.partial[(size_t)(first + c) * (size + a.out) + e];
-        if (e < size) a.dw[(size_t)g * size + e] = s;
-        else a.db[(size_t)g * a.out + (e - size)] = s;
+    const size_t size = (size_t)a.in * a.out, all = size + a.out, stride = partial_values(a.in, a.out);
+    const int quad = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const size_t e0 = (size_t)blockIdx.x * 64 + 4 * quad;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (e0 < all) {
+        const float* from = a.partial + (size_t)first * stride + e0;
+#pragma unroll 4
+        for (uint32_t c = slice; c < count; c += 16) s += *reinterpret_cast<const f32x4*>(from + (size_t)c * stride);
+    }
+    slices[slice][quad] = s;
+    __syncthreads();
+    if (slice != 0 || e0 >= all) return;
+    for (int i = 1; i < 16; ++i) s += slices[i][quad];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const size_t e = e0 + j;
+        if (e < size) a.dw[(size_t)g * size + e] = s[j];
+        else if (e < all && a.db) a.db[(size_t)g * a.out + (e - size)] = s[j];
     }
 }
 

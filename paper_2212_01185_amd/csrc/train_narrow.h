@@ -146,204 +146,201 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_forward_kernel(
 
 // ---------------------------------------------------------------------------
 // Backward, all of it in one pass over dz and x: every row of both is read once.  A workgroup of eight waves takes a chunk of
-// one group's rows in steps of 64 (32 where LDS has no room for more); a step's rows of dz and x go to LDS, the next step's on
-// the way while this one's are multiplied.  From there dz is read along for dx, and dz and x across for dw, whose sums stay in
-// registers to the chunk's end (the waves have a part of dw each: halves of the inputs, quarters of the outputs).
+// one group's rows in steps of 64 (32 where LDS has no room for more); a step's rows of dz and x go to LDS by registers, the
+// next step's on the way while this one's are multiplied (loads that go to LDS by themselves would be waited for before every
+// ds_read_b64_tr_b16: the compiler cannot tell which of them it must see).  From there dz is read along for dx, and dz and x
+// across for dw, whose sums stay in registers to the chunk's end (the waves have a part of dw each: halves of the inputs,
+// quarters of the outputs).
 // A row in LDS has its chunks of 8 values, zeros up to a multiple of four chunks, and two more of nothing: a distance of 2 modulo 4
 // chunks puts the 32-byte pieces of eight rows, which ds_read_b64_tr_b16 reads together, into different banks.
 // ---------------------------------------------------------------------------
-__host__ __device__ constexpr int narrow_chunks(int features) { return (features + 31) / 32 * 4 + 2; }
-__host__ __device__ constexpr size_t narrow_backward_lds(int in, int out, int rows, bool dx) {
-    const size_t weights = dx ? ((size_t)in + 31) / 32 * 2 * (((size_t)out + 31) / 32) * 1024 : 0;
-    return weights + 2 * (size_t)rows * (narrow_chunks(in) + narrow_chunks(out)) * 16;
-}
+constexpr int kMaxLds = 160 * 1024;
 
-// A thread's part in bringing a step's rows to LDS.
-struct NarrowSource {
-    static constexpr uint32_t kSkip = 0xFFFFFFFFu, kNone = 0x7FFFFF00u;
-    uint32_t offset[4];
-    const u16* base;
-    size_t ld;
-    int chunks, cut;        // chunks of a row in LDS; values of the chunk that the row's end cuts
-    int features;
+// PAIRS, KBS: inputs, outputs in units of 32.
+template <int PAIRS, int KBS>
+struct NarrowBackward {
+    static constexpr int kXChunks = 4 * PAIRS + 2, kZChunks = 4 * KBS + 2;      // of a row in LDS
+    static constexpr size_t kWeights = (size_t)PAIRS * 2 * KBS * 1024;          // w^T as operands
+    static constexpr size_t tiles(int rows) { return 2 * (size_t)rows * (kXChunks + kZChunks) * 16; }
+    static constexpr int kRows = kWeights + tiles(64) <= kMaxLds ? 64 : 32;
+    static constexpr size_t kLds = kWeights + tiles(kRows);
+    static_assert(kLds <= kMaxLds, "LDS");
+    static constexpr int kXLoads = (kRows * 4 * PAIRS + kNarrowThreads - 1) / kNarrowThreads;
+    static constexpr int kZLoads = (kRows * 4 * KBS + kNarrowThreads - 1) / kNarrowThreads;
+    static constexpr int kNB = (KBS + 1) / 2;       // blocks of 16 outputs of a wave
+    static constexpr int kWRows = 32 * (int)(tiles(kRows) / ((size_t)32 * kXChunks * 16) < KBS ? tiles(kRows) / ((size_t)32 * kXChunks * 16) : KBS);
+};
 
-    __device__ void init(const u16* b, size_t stride, int n_features, int rows) {
-        base = b;
-        ld = stride;
-        features = n_features;
-        chunks = narrow_chunks(n_features);
-        cut = n_features % 8;
+// A thread's chunks of `rows` rows of 32 * UNITS features (zeros where there is nothing), in registers between memory and LDS.
+template <int UNITS, int LOADS>
+struct RowPieces {
+    u32x4 v[LOADS];
+    __device__ void load(const u16* base, size_t ld, int features, int rows, int left) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int slot = threadIdx.x + kNarrowThreads * s, r = slot / chunks, c = slot - r * chunks;
-            offset[s] = r < rows && 8 * c + 8 <= n_features ? (uint32_t)(((size_t)r * ld + 8 * c) * 2) : kSkip;
+        for (int s = 0; s < LOADS; ++s) {
+            const int slot = threadIdx.x + kNarrowThreads * s, r = slot / (4 * UNITS), c = slot % (4 * UNITS), there = features - 8 * c;
+            u32x4 u = {0, 0, 0, 0};
+            if (r < left && r < rows && there > 0) {
+                const u16* from = base + (size_t)r * ld + 8 * c;
+                if (there >= 8) __builtin_memcpy(&u, from, 16);
+                else {                              // the chunk that the row's end cuts: features are even
+                    const uint32_t* words = reinterpret_cast<const uint32_t*>(from);
+                    u[0] = words[0];
+                    if (there > 2) u[1] = words[1];
+                    if (there > 4) u[2] = words[2];
+                }
+            }
+            v[s] = u;
         }
     }
-    // Zeros in what no load writes: the chunks behind a row's last.
-    __device__ void clear(u16* lds, int rows) const {
-        const int first = features / 8, last = (features + 31) / 32 * 4;
-        for (int i = threadIdx.x; i < rows * (last - first); i += kNarrowThreads) {
-            const int r = i / (last - first), c = first + i - r * (last - first);
-            *reinterpret_cast<u16x8*>(lds + (r * chunks + c) * 8) = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
-        }
-    }
-    // Rows r0 .. of the chunk, `left` of them there; zeros for the others.
-    __device__ void stage(u16* lds, int64_t r0, int left) const {
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)r0 * ld), 0, (int)kNone, 0x00020000);
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __device__ void store(u16* lds, int rows) const {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            if (offset[s] == kSkip) continue;
-            const bool there = (int)((threadIdx.x + kNarrowThreads * s) / (uint32_t)chunks) < left;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void*)(lds + (64 * wave + kNarrowThreads * s) * 8), 16, there ? offset[s] : kNone, 0, 0, 0);
+        for (int s = 0; s < LOADS; ++s) {
+            const int slot = threadIdx.x + kNarrowThreads * s, r = slot / (4 * UNITS), c = slot % (4 * UNITS);
+            if (r < rows) *reinterpret_cast<u32x4*>(lds + (r * (4 * UNITS + 2) + c) * 8) = v[s];
         }
-    }
-    // The chunk that the row's end cuts, of row threadIdx.x.
-    __device__ u16x8 cut_chunk(int64_t r0, int left) const {
-        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-        if ((int)threadIdx.x < left) {
-            const u16* from = base + (size_t)(r0 + threadIdx.x) * ld + features - cut;
-#pragma unroll
-            for (int j = 0; j < 7; ++j)
-                if (j < cut) v[j] = from[j];
-        }
-        return v;
     }
 };
 
-// Operand of 16 indices (chunk columns 2 i, 2 i + 1) and 32 rows from 32 kk on, read across.
-__device__ __forceinline__ u16x8 across(const u16* lds, int chunks, int i, int kk, int lane) {
+__device__ __forceinline__ u16x8 read_across(const u16* at, int row_values) {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int r = 32 * kk + 8 * (lane >> 4) + ((lane & 15) >> 2), at = (r * chunks + 2 * i + ((lane & 3) >> 1)) * 8 + 4 * (lane & 1);
-    const u16x4 a = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at)));
-    const u16x4 b = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at + 4 * chunks * 8)));
-    u16x8 v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[j + 4] = b[j]; }
-    return v;
+    const u16x4 a = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at));
+    const u16x4 b = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 4 * row_values)));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// MB, NB: blocks of 16 inputs, outputs that a wave may have of dw.
-template <class T, int MB, int NB>
+template <class T, int PAIRS, int KBS>
 __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_backward_kernel(Grouped a) {
+    using L = NarrowBackward<PAIRS, KBS>;
+    constexpr int kRows = L::kRows, kXRow = L::kXChunks * 8, kZRow = L::kZChunks * 8, NB = L::kNB;
     extern __shared__ __align__(16) u16 lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, a.mult, 1, blockIdx.x, true);
     if (ch.group < 0) return;
-    const int n = (int)(ch.hi - ch.lo), rows = a.step_rows;
-    const int pairs = (a.in + 31) / 32, kbs = (a.out + 31) / 32;
-    u16* tiles = lds + (a.y ? (size_t)pairs * 2 * kbs * 512 : 0);
-    const int z_size = rows * narrow_chunks(a.out) * 8, x_size = rows * narrow_chunks(a.in) * 8;
-    NarrowSource z, x;
-    z.init(a.dz + (size_t)ch.lo * a.lddz, a.lddz, a.out, rows);
-    x.init(a.x + (size_t)ch.lo * a.ldx, a.ldx, a.in, rows);
-    auto z_tile = [&](int b) { return tiles + b * (z_size + x_size); };
-    auto x_tile = [&](int b) { return tiles + b * (z_size + x_size) + z_size; };
-    const bool cuts = z.cut != 0 && (int)threadIdx.x < rows;
-    const int cut_at = ((int)threadIdx.x * z.chunks + a.out / 8) * 8;
-    if (n > 0) {
-        z.stage(z_tile(0), 0, n);
-        x.stage(x_tile(0), 0, n);
-    }
-    for (int b = 0; b < 2; ++b) { z.clear(z_tile(b), rows); x.clear(x_tile(b), rows); }
-    __syncthreads();
-    if (cuts) *reinterpret_cast<u16x8*>(z_tile(0) + cut_at) = z.cut_chunk(0, n);
+    const int n = (int)(ch.hi - ch.lo);
+    const u16* dz = a.dz + (size_t)ch.lo * a.lddz;
+    const u16* x = a.x + (size_t)ch.lo * a.ldx;
+    u16* tiles = lds + L::kWeights / 2;
+    RowPieces<KBS, L::kZLoads> z_next;
+    RowPieces<PAIRS, L::kXLoads> x_next;
+    z_next.load(dz, a.lddz, a.out, kRows, n);
+    x_next.load(x, a.ldx, a.in, kRows, n);
 
+    // a lane's place when 32 rows are read across: row 8 quad + (lane % 16) / 4 (and four below it), column 4 (lane % 4) of 16
+    const int across_row = 8 * quad + (col >> 2), across_col = 4 * (lane & 3);
     if (a.y) {
         // w^T as operands: inputs are dealt to two blocks of a pair as the forward kernel deals its outputs
         const u16* w = a.w + (size_t)ch.group * a.in * a.out;
-        for (int slot = threadIdx.x; slot < pairs * 2 * kbs * 64; slot += kNarrowThreads) {
-            const int m = slot & 15, q = (slot >> 4) & 3, k = slot / 64 % kbs, b = slot / 64 / kbs;
-            const int f = 32 * (b >> 1) + 8 * (m >> 2) + 4 * (b & 1) + (m & 3), o = 32 * k + 8 * q;
-            u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (f < a.in && o + j < a.out) v[j] = w[(size_t)(o + j) * a.in + f];
-            *reinterpret_cast<u16x8*>(lds + slot * 8) = v;
+        for (int o0 = 0; o0 < 32 * KBS; o0 += L::kWRows) {
+            for (int i = threadIdx.x; i < L::kWRows * 4 * PAIRS; i += kNarrowThreads) {
+                const int o = i / (4 * PAIRS), c = i % (4 * PAIRS);
+                u32x4 v = {0, 0, 0, 0};
+                if (o0 + o < a.out && 8 * c < a.in) __builtin_memcpy(&v, w + (size_t)(o0 + o) * a.in + 8 * c, 16);
+                *reinterpret_cast<u32x4*>(tiles + o * kXRow + 8 * c) = v;
+            }
+            __syncthreads();
+            for (int i = wave; i < L::kWRows / 32 * 2 * PAIRS; i += 8) {
+                const int k = i / (2 * PAIRS), b = i % (2 * PAIRS);
+                if (o0 / 32 + k < KBS) {
+                    const u16x8 v = read_across(tiles + (32 * k + across_row) * kXRow + 32 * (b >> 1) + 2 * across_col + 4 * (b & 1), kXRow);
+                    *reinterpret_cast<u16x8*>(lds + ((b * KBS + o0 / 32 + k) * 64 + lane) * 8) = v;
+                }
+            }
+            __syncthreads();
         }
     }
+    z_next.store(tiles, kRows);
+    x_next.store(tiles + kRows * kZRow, kRows);
 
-    const int m_blocks = (a.in + 15) / 16, n_blocks = (a.out + 15) / 16, m_each = (m_blocks + 1) / 2, n_each = (n_blocks + 3) / 4;
-    const int mb0 = (wave & 1) * m_each, nb0 = (wave >> 1) * n_each;
-    const int mbs = m_blocks - mb0 < m_each ? m_blocks - mb0 : m_each, nbs = n_blocks - nb0 < n_each ? n_blocks - nb0 : n_each;
-    f32x4 acc[MB][NB] = {}, sums[NB] = {};
+    // blocks of 16 of dw; the last of a wave's may be another's as well (and is not stored)
+    const int mb0 = (wave & 1) * PAIRS, nb0 = (wave >> 1) * NB;
+    f32x4 acc[PAIRS][NB] = {}, sums[NB] = {};
     u16x8 ones;
     for (int j = 0; j < 8; ++j) ones[j] = T::kOne;
     const bool with_db = a.db && (wave & 1) == 0;
-    const int row_tiles = rows / 16, my_tile = wave % row_tiles, pair0 = wave / row_tiles, pair_step = 8 / row_tiles;
+    constexpr int kRowTiles = kRows / 16, kPairStep = 8 / kRowTiles;
+    const int my_row = 16 * (wave % kRowTiles) + col, pair0 = wave / kRowTiles;
 
     int now = 0;
-    for (int r0 = 0; r0 < n; r0 += rows, now ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0);          // this step's rows are in LDS, and the chunks that a thread wrote
+    for (int r0 = 0; r0 < n; r0 += kRows, now ^= 1) {
         __syncthreads();
-        const u16* zt = z_tile(now);
-        const u16* xt = x_tile(now);
-        u16x8 cut = {0, 0, 0, 0, 0, 0, 0, 0};
-        const bool more = r0 + rows < n;
+        const u16* zt = tiles + now * kRows * (kZRow + kXRow);
+        const u16* xt = zt + kRows * kZRow;
+        const bool more = r0 + kRows < n;
         if (more) {
-            z.stage(z_tile(now ^ 1), r0 + rows, n - r0 - rows);
-            x.stage(x_tile(now ^ 1), r0 + rows, n - r0 - rows);
-            if (cuts) cut = z.cut_chunk(r0 + rows, n - r0 - rows);
+            z_next.load(dz + (size_t)(r0 + kRows) * a.lddz, a.lddz, a.out, kRows, n - r0 - kRows);
+            x_next.load(x + (size_t)(r0 + kRows) * a.ldx, a.ldx, a.in, kRows, n - r0 - kRows);
         }
         if (a.y) {
-            const int r = 16 * my_tile + col;
-            u16x8 q[2 * NB];
+            u16x8 q[KBS];
 #pragma unroll
-            for (int k = 0; k < 2 * NB; ++k)
-                if (k < kbs) q[k] = *reinterpret_cast<const u16x8*>(zt + (r * z.chunks + 4 * k + quad) * 8);
-            for (int pair = pair0; pair < pairs; pair += pair_step) {
+            for (int k = 0; k < KBS; ++k) q[k] = *reinterpret_cast<const u16x8*>(zt + my_row * kZRow + 32 * k + 8 * quad);
+#pragma unroll
+            for (int j = 0; j < (PAIRS + kPairStep - 1) / kPairStep; ++j) {
+                const int pair = pair0 + j * kPairStep;
+                if (pair >= PAIRS) break;
                 f32x4 d0 = {}, d1 = {};
-                const u16* p = lds + (size_t)pair * 2 * kbs * 512 + lane * 8;
+                const u16* p = lds + (size_t)pair * 2 * KBS * 512 + lane * 8;
 #pragma unroll
-                for (int k = 0; k < 2 * NB; ++k) {
-                    if (k >= kbs) continue;
+                for (int k = 0; k < KBS; ++k) {
                     d0 = T::mfma(*reinterpret_cast<const u16x8*>(p + k * 512), q[k], d0);
-                    d1 = T::mfma(*reinterpret_cast<const u16x8*>(p + (kbs + k) * 512), q[k], d1);
+                    d1 = T::mfma(*reinterpret_cast<const u16x8*>(p + (KBS + k) * 512), q[k], d1);
                 }
                 const int f = 32 * pair + 8 * quad;
                 if (a.act != PCC_ACT_NONE) {
-                    const u16x8 s = *reinterpret_cast<const u16x8*>(xt + (r * x.chunks + 4 * pair + quad) * 8);
+                    const u16x8 s = *reinterpret_cast<const u16x8*>(xt + my_row * kXRow + f);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         d0[e] = times_derivative(d0[e], from16<T>(s[e]), a.act);
                         d1[e] = times_derivative(d1[e], from16<T>(s[4 + e]), a.act);
                     }
                 }
-                if (r0 + r < n && f < a.in) store_eight<T>(a, (size_t)(ch.lo + r0 + r) * a.ldy + f, d0, d1, 8, PCC_ACT_NONE);
+                if (r0 + my_row < n && f < a.in) {
+                    u16x8 o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { o[e] = to16<T>(d0[e]); o[4 + e] = to16<T>(d1[e]); }
+                    u16* to = static_cast<u16*>(a.y) + (size_t)(ch.lo + r0 + my_row) * a.ldy + f;
+                    if (a.wide_out) __builtin_memcpy(to, &o, 16);
+                    else for (int e = 0; e < 8; ++e) to[e] = o[e];
+                }
             }
         }
-        for (int kk = 0; kk < rows / 32; ++kk) {
+#pragma unroll
+        for (int kk = 0; kk < kRows / 32; ++kk) {
             u16x8 q[NB];
 #pragma unroll
-            for (int j = 0; j < NB; ++j)
-                if (j < nbs) q[j] = across(zt, z.chunks, nb0 + j, kk, lane);
+            for (int j = 0; j < NB; ++j) {
+                const int nb = nb0 + j < 2 * KBS ? nb0 + j : 2 * KBS - 1;
+                q[j] = read_across(zt + (32 * kk + across_row) * kZRow + 16 * nb + across_col, kZRow);
+            }
 #pragma unroll
-            for (int i = 0; i < MB; ++i) {
-                if (i >= mbs) continue;
-                const u16x8 p = across(xt, x.chunks, mb0 + i, kk, lane);
+            for (int i = 0; i < PAIRS; ++i) {
+                const u16x8 p = read_across(xt + (32 * kk + across_row) * kXRow + 16 * (mb0 + i) + across_col, kXRow);
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
-                    if (j < nbs) acc[i][j] = T::mfma(p, q[j], acc[i][j]);
+                for (int j = 0; j < NB; ++j) acc[i][j] = T::mfma(p, q[j], acc[i][j]);
             }
             if (with_db)
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
-                    if (j < nbs) sums[j] = T::mfma(ones, q[j], sums[j]);
+                for (int j = 0; j < NB; ++j) sums[j] = T::mfma(ones, q[j], sums[j]);
         }
-        if (more && cuts) *reinterpret_cast<u16x8*>(z_tile(now ^ 1) + cut_at) = cut;
+        if (more) {
+            u16* to = tiles + (now ^ 1) * kRows * (kZRow + kXRow);
+            z_next.store(to, kRows);
+            x_next.store(to + kRows * kZRow, kRows);
+        }
     }
 
     const size_t size = (size_t)a.in * a.out;
-    float* dw = ch.count == 1 ? a.dw + (size_t)ch.group * size : a.partial + (size_t)ch.id * (size + a.out);
+    float* dw = ch.count == 1 ? a.dw + (size_t)ch.group * size : a.partial + (size_t)ch.id * partial_values(a.in, a.out);
     float* db = ch.count == 1 ? a.db + (a.db ? (size_t)ch.group * a.out : 0) : dw + size;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         const int o = 16 * (nb0 + j) + col;
-        if (j >= nbs || o >= a.out) continue;
+        if (o >= a.out) continue;
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
+        for (int i = 0; i < PAIRS; ++i) {
             const int f = 16 * (mb0 + i) + 4 * quad;
-            if (i < mbs && f < a.in) store_four(dw + (size_t)o * a.in + f, acc[i][j], 4, a.wide_dw);
+            if (f < a.in) store_four(dw + (size_t)o * a.in + f, acc[i][j], 4, a.wide_dw);
         }
         if (with_db && quad == 0) db[o] = sums[j][0];
     }
