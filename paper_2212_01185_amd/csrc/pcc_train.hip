@@ -83,22 +83,33 @@ bool features_ok(int in, int out, int groups, size_t rows) {
 bool ld_ok(size_t ld, int features) { return ld >= (size_t)features && ld <= kMaxLd; }
 
 // Rows of a chunk of the weights' gradient.  A chunk's sums go to the workspace and are added up by another kernel, so
-// there are no more chunks than fill the chip, and none of less than 256 rows.
-int weights_log2(size_t rows, int in, int out) {
-    const size_t tiles = ((size_t)in + kTile - 1) / kTile * (((size_t)out + kTile - 1) / kTile);
-    const size_t want = std::max<size_t>(1, 512 / tiles);
+// there are no more chunks than fill the chip (512 workgroups at a time), none of less than 256 rows, and where the groups fill it by themselves
+// only a group of twice the mean or more is cut.
+int weights_log2(size_t rows, int groups, int in, int out) {
+    const size_t tiles = ((size_t)in + 127) / 128 * (((size_t)out + 127) / 128), want = std::max<size_t>(1, 512 / tiles);
+    const size_t least = want > (size_t)groups ? (rows + want - 1) / want : 2 * (rows / groups);
     int log2 = 8;
-    while (((size_t)1 << log2) * want < rows) ++log2;
+    while (((size_t)1 << log2) < least) ++log2;
     return log2;
+}
+// Chunks that can be in groups of more than one: such a group of n has more than (n - 1) chunks' rows, n/2 at least.
+size_t shared_chunks(size_t rows, int groups, size_t chunk) {
+    return rows <= chunk ? 0 : std::min(rows / chunk + groups, 2 * (rows / chunk));
 }
 
 // Rows of an operand can be read in pieces of 16 bytes, which have to begin at a multiple of four.
 bool even_rows(const void* p, size_t ld) { return aligned(p, 4) && ld % 2 == 0; }
 
-template <class T, int MODE>
-int launch_tiles(Grouped& a, hipStream_t st) {
-    a.tiles_m = (uint32_t)(((MODE == kForward ? a.out : a.in) + kTile - 1) / kTile);
-    a.tiles_n = (uint32_t)((a.out + kTile - 1) / kTile);
+// More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
+template <class K>
+bool allow_lds(K kernel, size_t bytes) {
+    return bytes <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+}
+
+template <class T, int MODE, int TILE>
+int launch_tiles_of(Grouped& a, hipStream_t st) {
+    a.tiles_m = (uint32_t)(((MODE == kForward ? a.out : a.in) + TILE - 1) / TILE);
+    a.tiles_n = (uint32_t)((a.out + TILE - 1) / TILE);
     a.mult = 1;
     const uint64_t chunks = ((uint64_t)a.rows >> a.log2) + a.groups, blocks = chunks * a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
     if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
@@ -108,8 +119,27 @@ int launch_tiles(Grouped& a, hipStream_t st) {
     a.wide_dw = aligned(a.dw, 16) && (size_t)a.in * a.out % 4 == 0;
     a.wide_out = aligned(a.y, a.y32 ? 16 : 8) && a.ldy % 4 == 0;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);     // a multiple of the dies: see find_chunk
-    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kTileThreads), 0, st, a); }); };
-    return wide ? go(grouped_tile_kernel<T, MODE, true>) : go(grouped_tile_kernel<T, MODE, false>);
+    const size_t lds = 4 * (size_t)TILE * kTileK * sizeof(u16);
+    auto go = [&](auto kernel) {
+        if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
+        return launch([&] { hipLaunchKernelGGL(kernel, dim3(grid), dim3(tile_threads(TILE)), lds, st, a); });
+    };
+    return wide ? go(grouped_tile_kernel<T, MODE, true, TILE>) : go(grouped_tile_kernel<T, MODE, false, TILE>);
+}
+
+template <class T, int MODE>
+int launch_tiles(Grouped& a, hipStream_t st) {
+    if (MODE != kWeights) a.log2 = 7;
+    return launch_tiles_of<T, MODE, 128>(a, st);
+}
+// Forward: tiles of 256 where the groups have the rows for them and there are as many as compute units, else of 128.  us with 128 and
+// 256: four groups of 2,048 rows, 2048 to 2048, 88 and 71; sixteen of 512, 1024 to 4096, 131 and 131; 64 of five, 1024 to 1024, 28 and 34.
+template <class T>
+int launch_forward_tiles(Grouped& a, hipStream_t st) {
+    const uint64_t of_256 = ((uint64_t)a.rows / 256 + a.groups) * ((a.out + 255) / 256);
+    if (a.rows / a.groups < 512 || of_256 < 256) return launch_tiles<T, kForward>(a, st);
+    a.log2 = 8;
+    return launch_tiles_of<T, kForward, 256>(a, st);
 }
 
 // Chunks of about rows / want rows, in steps of 1/4 to 1/8 of a power of two, and a multiple of `unit` (a power of two).  The
@@ -122,12 +152,6 @@ void chunk_rows(Grouped& a, uint64_t want, int unit_log2) {
     a.mult = (uint32_t)std::min<uint64_t>((rows + ((uint64_t)1 << a.log2) - 1) >> a.log2, 8);
 }
 uint64_t chunk_count(const Grouped& a) { return (uint64_t)a.rows / ((uint64_t)a.mult << a.log2) + a.groups; }
-
-// More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
-template <class K>
-bool allow_lds(K kernel, size_t bytes) {
-    return bytes <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
-}
 
 // The forward pass with the weights in LDS: for inputs of up to 192 features, a multiple of eight, in rows that begin at even
 // elements, and weights that leave a compute unit room for two workgroups.
@@ -240,24 +264,21 @@ int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float
     a.y32 = y_type == PCC_FP32;
     hipStream_t st = (hipStream_t)hip_stream;
     if (narrow_forward_fits(a)) return type == PCC_BF16 ? launch_narrow_forward<Bf16>(a, st) : launch_narrow_forward<Fp16>(a, st);
-    a.log2 = 7;
-    return type == PCC_BF16 ? launch_tiles<Bf16, kForward>(a, st) : launch_tiles<Fp16, kForward>(a, st);
+    return type == PCC_BF16 ? launch_forward_tiles<Bf16>(a, st) : launch_forward_tiles<Fp16>(a, st);
 }
 
 size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, int out) {
     if (!features_ok(in, out, groups, rows)) return 0;
     // enough for either kernel: which one runs depends on the tensors' places too
-    const size_t values = partial_values(in, out);
-    const int log2 = weights_log2(rows, in, out);
-    size_t chunks = rows <= (size_t)1 << log2 ? 0 : (rows >> log2) + groups;
+    size_t chunks = shared_chunks(rows, groups, (size_t)1 << weights_log2(rows, groups, in, out));
     if (in <= 192 && out <= 192) {
         Grouped a = {};
         a.rows = (int64_t)rows;
         a.groups = groups;
-        const size_t narrow = backward_chunks(a);
-        if (rows > (size_t)a.mult << a.log2) chunks = std::max(chunks, narrow);
+        backward_chunks(a);
+        chunks = std::max(chunks, shared_chunks(rows, groups, (size_t)a.mult << a.log2));
     }
-    return chunks * values * sizeof(float);
+    return chunks * partial_values(in, out) * sizeof(float);
 }
 
 int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size_t ldx, const void* d_w, const int64_t* d_offsets,
@@ -276,24 +297,24 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.dz = (const u16*)d_dz; a.off = d_offsets; a.y = d_dx; a.dw = d_dw; a.db = d_db;
     a.ldx = ldx; a.lddz = lddz; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = x_act;
     a.partial = (float*)d_workspace;
+    a.shared_max = (uint32_t)std::min<size_t>(need / (partial_values(in, out) * sizeof(float)), 0xFFFFFFFFu);
     if (narrow_backward_fits(a)) {
         const int rc = type == PCC_BF16 ? launch_narrow_backward<Bf16>(a, st) : launch_narrow_backward<Fp16>(a, st);
         if (rc != PCC_OK) return rc;
     } else {
         if (d_dx && rows) {
-            a.log2 = 7;
             const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kBackward>(a, st) : launch_tiles<Fp16, kBackward>(a, st);
             if (rc != PCC_OK) return rc;
         }
         if (!d_dw) return PCC_OK;
-        a.log2 = weights_log2(rows, in, out);
+        a.log2 = weights_log2(rows, groups, in, out);
         const int rc = type == PCC_BF16 ? launch_tiles<Bf16, kWeights>(a, st) : launch_tiles<Fp16, kWeights>(a, st);
         if (rc != PCC_OK) return rc;
     }
     if (rows <= (size_t)a.mult << a.log2) return PCC_OK;        // no group can have two chunks
-    const size_t values = (size_t)in * out + out;
+    const size_t parts = (partial_values(in, out) + 63) / 64;
     return launch([&] {
-        hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)((values + 63) / 64), groups), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(grouped_reduce_kernel, dim3((uint32_t)std::min<size_t>(parts, std::max(4, 4096 / groups)), groups), dim3(256), 0, st, a);
     });
 }
 

@@ -66,7 +66,7 @@ __device__ __forceinline__ float times_derivative(float d, float x, int act) {
 struct Chunk {
     int group;          // -1: there is no such chunk
     int64_t lo, hi;     // rows
-    uint32_t id;        // number of the chunk
+    uint32_t shared;    // number of the chunk among those of groups that have more than one
     uint32_t count;     // chunks of the group
     uint32_t part;      // tile of the chunk
 };
@@ -86,6 +86,11 @@ __device__ __forceinline__ uint32_t group_chunks(const int64_t* __restrict__ off
     const uint32_t n = ((uint32_t)((hi - lo + ((int64_t)1 << log2) - 1) >> log2) + mult - 1) / mult;
     return empty && n == 0 ? 1 : n;
 }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += (uint32_t)__shfl_xor((int)v, d);
+    return uniform(v);
+}
 __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -97,6 +102,7 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
 }
 
 // Workgroup b's chunk and tile (of `tiles` that each chunk has).  All lanes of a wave together; the result is the same in every lane.
+// `shared` is only found with `empty`, for sums.
 // The chip's eight dies take workgroups in turn and have an L2 each, so die d gets the d-th eighth of the work, and within a group
 // the chunks of one tile come one after the other: they read the same weights at about the same time.
 __device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t mult, uint32_t tiles, uint32_t b, bool empty) {
@@ -105,13 +111,10 @@ __device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int
     if (groups > 64) {                  // else the search itself says it
         for (int g0 = 0; g0 < groups; g0 += 64) {
             int64_t lo, hi;
-            uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi);
-#pragma unroll
-            for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
-            total += uniform(n);
+            total += wave_sum(group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi));
         }
     }
-    uint32_t before = 0;
+    uint32_t before = 0, shared = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
         int64_t lo, hi;
         const uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi);
@@ -126,9 +129,11 @@ __device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int
             const uint32_t count = uniform((uint32_t)__shfl((int)n, found)), first = before + uniform((uint32_t)__shfl((int)sum, found)) - count;
             const uint32_t in_group = t - first * tiles, chunk = tiles == 1 ? in_group : in_group % count;
             const int64_t size = (int64_t)mult << log2, clo = glo + (int64_t)chunk * size, chi = clo + size;
-            return {g0 + found, clo, chi < ghi ? chi : ghi, first + chunk, count, tiles == 1 ? 0 : in_group / count};
+            if (empty && groups > 1) shared += wave_sum(n > 1 && lane < found ? n : 0);
+            return {g0 + found, clo, chi < ghi ? chi : ghi, shared + chunk, count, tiles == 1 ? 0 : in_group / count};
         }
         before += uniform((uint32_t)__shfl((int)sum, 63));
+        if (empty) shared += wave_sum(n > 1 ? n : 0);
     }
     return {-1, 0, 0, 0, 0, 0};
 }

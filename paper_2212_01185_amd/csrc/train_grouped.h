@@ -28,6 +28,7 @@ struct Grouped {
     size_t ldx, lddz, ldy;
     int64_t rows;
     int groups, in, out, act;
+    uint32_t shared_max;    // chunks of sums that the workspace has room for
     int log2;           // rows of a chunk: mult * 2^log2
     uint32_t mult;
     int y32;            // y is fp32
@@ -36,48 +37,51 @@ struct Grouped {
     uint32_t tiles_m, tiles_n;
 };
 
-constexpr int kTile = 128, kTileK = 64, kTileThreads = 256;
+constexpr int kTileK = 64;
+__host__ __device__ constexpr int tile_threads(int tile) { return 2 * tile; }
 
-// An operand's tile in LDS, 16 KB.  Chunks of 8 values; chunk c of row r stands at slot c ^ swizzle(r) of the row, so that the
+// An operand's tile in LDS, TILE (128, 256) indices and 64 k.  Chunks of 8 values; chunk c of row r stands at slot c ^ swizzle(r) of the row, so that the
 // rows that are read together lie in different banks.
-//   along: rows are the operand's 128 indices, 64 k each (8 chunks)
-//   across: rows are the 64 k, 128 indices each (16 chunks)
-template <bool ACROSS>
+//   along: rows are the operand's indices, 64 k each (8 chunks)
+//   across: rows are the 64 k, TILE indices each (16 or 32 chunks)
+template <bool ACROSS, int TILE>
 struct TileLds {
-    static constexpr int kChunks = ACROSS ? 16 : 8;
+    static constexpr int kChunks = ACROSS ? TILE / 8 : 8;
     __device__ static int at(int r, int c) { return (r * kChunks + (c ^ (ACROSS ? (2 * (r & 7)) : (r & 7)))) * 8; }
     // The MFMA operand of indices 16 i .. +15, k 32 kk .. +31.
     __device__ static u16x8 operand(const u16* lds, int i, int kk, int lane) {
         if constexpr (!ACROSS) {
             return *reinterpret_cast<const u16x8*>(lds + at(16 * i + (lane & 15), 4 * kk + (lane >> 4)));
         } else {
-            u16x8 v;
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
             const int r = 32 * kk + 8 * (lane >> 4) + ((lane & 15) >> 2), c = 2 * i + ((lane & 3) >> 1), e = 4 * (lane & 1);
             const u16x4 a = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(r, c) + e)));
             const u16x4 b = __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(r + 4, c) + e)));
-            for (int j = 0; j < 4; ++j) { v[j] = a[j]; v[j + 4] = b[j]; }
-            return v;
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
     }
 };
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-// An operand in memory, and a workgroup's way through it in steps of 64 k.  Where rows begin at even elements (`wide`), chunks go from
-// memory to LDS without a register, 16 bytes a lane; a chunk that is cut by the end of its row is read value by value, and what lies
-// beyond the operand is zero: such a lane's offset is beyond the buffer's end, for which the load gives zeros.  Rows at
-// odd elements are read value by value.
-template <bool ACROSS>
+// An operand in memory, and a workgroup's way through it in steps of 64 k.  Where rows begin at even elements (WIDE), chunks go 16
+// bytes a lane: by themselves, without a register, if all operands are read along (the compiler waits for all such loads
+// before a ds_read_b64_tr_b16, of which it cannot tell what it must see), else by registers.  A chunk that is cut by the end of its row is
+// read value by value, and what lies beyond the operand is zero (a lane's offset beyond the buffer's end loads zeros).  Rows
+// at odd elements are read value by value.
+template <bool ACROSS, int TILE>
 struct Source {
+    static constexpr int kThreads = tile_threads(TILE);
     const u16* base;            // index i0, k 0
     size_t ld;
     int64_t ni, nk;             // indices from i0 on, all k
     uint32_t offset[4];         // bytes of this lane's chunks from base + the step
-    static constexpr uint32_t kNone = 0x7FFFFF00u;      // beyond the buffer (rows are at most 2^22 values, a tile has 128)
+    u32x4 held[4];              // chunks on their way by registers
+    static constexpr uint32_t kNone = 0xFFFFFF00u;      // beyond the buffer (rows are at most 2^22 values, a tile has 256)
 
     __device__ void init(const u16* b, size_t stride, int64_t i0, int64_t n_index, int64_t n_k) {
-        base = b + (ACROSS ? (size_t)i0 : (size_t)i0 * stride);
+        const u16* from = b + (ACROSS ? (size_t)i0 : (size_t)i0 * stride);
+        base = reinterpret_cast<const u16*>(uniform64(reinterpret_cast<int64_t>(from)));
         ld = stride;
         ni = n_index - i0;
         nk = n_k;
@@ -90,53 +94,69 @@ struct Source {
         }
     }
     __device__ static void place(int s, int& r, int& c) {
-        const int slot = threadIdx.x + kTileThreads * s;
-        r = slot / TileLds<ACROSS>::kChunks;
-        c = (slot % TileLds<ACROSS>::kChunks) ^ (ACROSS ? 2 * (r & 7) : (r & 7));
+        const int slot = threadIdx.x + kThreads * s;
+        r = slot / TileLds<ACROSS, TILE>::kChunks;
+        c = (slot % TileLds<ACROSS, TILE>::kChunks) ^ (ACROSS ? 2 * (r & 7) : (r & 7));
     }
     // Values of a chunk that are there, at k0.
     __device__ int values(int r, int c, int64_t k0) const {
         const int64_t n = ACROSS ? (k0 + r < nk ? ni - 8 * c : 0) : (r < ni ? nk - k0 - 8 * c : 0);
         return n < 0 ? 0 : n > 8 ? 8 : (int)n;
     }
-    __device__ void one_by_one(u16* lds, int s, int64_t k0, int n) const {
-        int r, c;
-        place(s, r, c);
+    __device__ u32x4 one_by_one(int r, int c, int64_t k0, int n) const {
         const u16* from = base + (ACROSS ? (size_t)(k0 + r) * ld + 8 * c : (size_t)r * ld + (size_t)k0 + 8 * c);
         u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) v[j] = from[j];
-        *reinterpret_cast<u16x8*>(lds + (threadIdx.x + kTileThreads * s) * 8) = v;
+        return __builtin_bit_cast(u32x4, v);
     }
-    template <bool WIDE>
+    __device__ __amdgpu_buffer_rsrc_t buffer(int64_t k0) const {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (ACROSS ? (size_t)k0 * ld : (size_t)k0)), 0, (int)kNone, 0x00020000);
+    }
+    // All chunks of the step are there, or not at all for every k.
+    __device__ bool whole(int64_t k0) const { return k0 + kTileK <= nk && (!ACROSS || ni % 8 == 0 || ni >= TILE); }
+
+    // Straight to LDS.
     __device__ void stage(u16* lds, int64_t k0) const {
-        if constexpr (!WIDE) {
+        const __amdgpu_buffer_rsrc_t from = buffer(k0);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const bool all = whole(k0);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 4; ++s) {
+            lds_void* to = (lds_void*)(lds + (64 * wave + kThreads * s) * 8);
+            if (all) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, offset[s], 0, 0, 0);
+            } else {
                 int r, c;
                 place(s, r, c);
-                one_by_one(lds, s, k0, values(r, c, k0));
-            }
-        } else {
-            const __amdgpu_buffer_rsrc_t from =
-                __builtin_amdgcn_make_buffer_rsrc((void*)(base + (ACROSS ? (size_t)k0 * ld : (size_t)k0)), 0, (int)kNone, 0x00020000);
-            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-            const bool whole = k0 + kTileK <= nk && (!ACROSS || ni % 8 == 0 || ni >= kTile);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                lds_void* to = (lds_void*)(lds + (64 * wave + kTileThreads * s) * 8);
-                if (whole) {
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, offset[s], 0, 0, 0);
-                } else {
-                    int r, c;
-                    place(s, r, c);
-                    const int n = values(r, c, k0);
-                    if (n == 0 || n == 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, n ? offset[s] : kNone, 0, 0, 0);
-                    else one_by_one(lds, s, k0, n);
-                }
+                const int n = values(r, c, k0);
+                if (n == 0 || n == 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, n ? offset[s] : kNone, 0, 0, 0);
+                else *reinterpret_cast<u32x4*>(lds + (threadIdx.x + kThreads * s) * 8) = one_by_one(r, c, k0, n);
             }
         }
+    }
+    // To registers, and from there to LDS.
+    template <bool WIDE>
+    __device__ void fetch(int64_t k0) {
+        const __amdgpu_buffer_rsrc_t from = buffer(k0);
+        if (WIDE && whole(k0)) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) held[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, offset[s], 0, 0));
+            return;
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            int r, c;
+            place(s, r, c);
+            const int n = values(r, c, k0);
+            if (WIDE && (n == 0 || n == 8)) held[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, n ? offset[s] : kNone, 0, 0));
+            else held[s] = one_by_one(r, c, k0, n);
+        }
+    }
+    __device__ void put(u16* lds) const {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) *reinterpret_cast<u32x4*>(lds + (threadIdx.x + kThreads * s) * 8) = held[s];
     }
 };
 
@@ -204,52 +224,95 @@ __device__ __forceinline__ void store_eight(const Grouped& a, size_t at, f32x4 v
             if (e < left) y[e] = o[e];
 }
 
-// Four waves, each 64 x 64 of the tile's 128 x 128.  Two tiles in LDS for each operand: the next step's is filled while this one's is
-// multiplied.
-template <class T, int MODE, bool WIDE>
-__global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a) {
+// TILE x TILE results of a workgroup: 128 by four waves with 64 x 64 each, 256 by eight with 128 x 64.  Two tiles in LDS for each
+// operand: the next step's is filled while this one's is multiplied.
+template <class T, int MODE, bool WIDE, int TILE>
+__global__ __launch_bounds__(tile_threads(TILE), 2) void grouped_tile_kernel(Grouped a) {
     constexpr bool kPAcross = MODE != kForward, kQAcross = MODE == kWeights;
-    __shared__ __align__(16) u16 lds[2][2][kTile * kTileK];
+    constexpr int kTile = TILE, MI = TILE / 32;
+    using P = TileLds<kPAcross, TILE>;
+    using Q = TileLds<kQAcross, TILE>;
+    extern __shared__ __align__(16) u16 lds_all[];
+    auto lds = [&](int buffer, int operand) { return lds_all + (2 * buffer + operand) * TILE * kTileK; };
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave & 1, wn = wave >> 1;
     const uint32_t tiles = a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
     const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, a.mult, tiles, blockIdx.x, MODE == kWeights);
-    if (ch.group < 0) return;
+    if (ch.group < 0 || (MODE == kWeights && ch.count > 1 && ch.shared >= a.shared_max)) return;     // (the second only with offsets that fall)
     const int64_t m0 = (int64_t)(ch.part % a.tiles_m) * kTile, n0 = MODE == kWeights ? (int64_t)(ch.part / a.tiles_m) * kTile : 0;
     const int64_t n_rows = ch.hi - ch.lo;
     const u16* w = a.w ? a.w + (size_t)ch.group * a.in * a.out : nullptr;
     const int64_t np = MODE == kForward ? a.out : a.in, nq = MODE == kWeights ? a.out : n_rows;
     const int64_t nk = MODE == kForward ? a.in : MODE == kBackward ? a.out : n_rows;
-    Source<kPAcross> p;
-    Source<kQAcross> q;
+    Source<kPAcross, TILE> p;
+    Source<kQAcross, TILE> q;
     p.init(MODE == kWeights ? a.x + (size_t)ch.lo * a.ldx : w, MODE == kWeights ? a.ldx : (size_t)a.in, m0, np, nk);
     if (MODE == kForward) q.init(a.x + (size_t)ch.lo * a.ldx, a.ldx, n0, nq, nk);
     else q.init(a.dz + (size_t)ch.lo * a.lddz, a.lddz, n0, nq, nk);
 
-    f32x4 acc[4][4] = {}, sums[4] = {};
+    f32x4 acc[MI][4] = {}, sums[4] = {};
     const bool with_db = MODE == kWeights && a.db && m0 == 0 && wm == 0;
     u16x8 ones;
     for (int j = 0; j < 8; ++j) ones[j] = T::kOne;
+    constexpr bool kStraight = WIDE && MODE == kForward;
     if (nk > 0) {
-        p.template stage<WIDE>(lds[0][0], 0);
-        q.template stage<WIDE>(lds[0][1], 0);
+        if constexpr (kStraight) {
+            p.stage(lds(0, 0), 0);
+            q.stage(lds(0, 1), 0);
+        } else {
+            p.template fetch<WIDE>(0);
+            q.template fetch<WIDE>(0);
+            p.put(lds(0, 0));
+            q.put(lds(0, 1));
+        }
     }
     int now = 0;
     for (int64_t k0 = 0; k0 < nk; k0 += kTileK, now ^= 1) {
-        __builtin_amdgcn_s_waitcnt(0);      // this step's chunks are in LDS: the barrier alone does not wait for loads that go there
+        if (kStraight) __builtin_amdgcn_s_waitcnt(0);       // the barrier alone does not wait for loads that go to LDS
         __syncthreads();
-        if (k0 + kTileK < nk) {
-            p.template stage<WIDE>(lds[now ^ 1][0], k0 + kTileK);
-            q.template stage<WIDE>(lds[now ^ 1][1], k0 + kTileK);
+        const bool more = k0 + kTileK < nk;
+        if (more) {
+            if constexpr (kStraight) {
+                p.stage(lds(now ^ 1, 0), k0 + kTileK);
+                q.stage(lds(now ^ 1, 1), k0 + kTileK);
+            } else {
+                p.template fetch<WIDE>(k0 + kTileK);
+                q.template fetch<WIDE>(k0 + kTileK);
+            }
         }
+        // Groups of four products that share P's block i of half kk.  P's blocks are read two groups ahead and Q's of the second half
+        // during the first, each between two groups: read where they are needed, every group would wait for LDS.
+        const u16* tp = lds(now, 0);
+        const u16* tq = lds(now, 1);
+        u16x8 fq[2][4], fp[2 * MI];
+        auto read_q = [&](int kk, int j) { fq[kk][j] = Q::operand(tq, 4 * wn + j, kk, lane); };
+        auto read_p = [&](int g) { fp[g] = P::operand(tp, MI * wm + g % MI, g / MI, lane); };
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u16x8 fp[4], fq[4];
-            for (int i = 0; i < 4; ++i) fp[i] = TileLds<kPAcross>::operand(lds[now][0], 4 * wm + i, kk, lane);
-            for (int i = 0; i < 4; ++i) fq[i] = TileLds<kQAcross>::operand(lds[now][1], 4 * wn + i, kk, lane);
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) acc[i][j] = T::mfma(fp[i], fq[j], acc[i][j]);
-            if (with_db)
-                for (int j = 0; j < 4; ++j) sums[j] = T::mfma(ones, fq[j], sums[j]);
+        for (int j = 0; j < 4; ++j) read_q(0, j);
+        read_p(0);
+        read_p(1);
+        constexpr int kP = kPAcross ? 2 : 1, kQ = kQAcross ? 2 : 1;     // LDS instructions of an operand
+        __builtin_amdgcn_sched_group_barrier(0x100, 4 * kQ + 2 * kP, 0);
+#pragma unroll
+        for (int g = 0; g < 2 * MI; ++g) {
+            const int kk = g / MI, i = g % MI;
+            if (g + 2 < 2 * MI) {
+                read_p(g + 2);
+                __builtin_amdgcn_sched_group_barrier(0x100, kP, 0);
+            }
+            if (kk == 0 && i < 4) {
+                read_q(1, i);
+                __builtin_amdgcn_sched_group_barrier(0x100, kQ, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = T::mfma(fp[g], fq[kk][j], acc[i][j]);
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
+        if (with_db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sums[j] = T::mfma(ones, fq[1][j], T::mfma(ones, fq[0][j], sums[j]));
+        if (!kStraight && more) {
+            p.put(lds(now ^ 1, 0));
+            q.put(lds(now ^ 1, 1));
         }
     }
 
@@ -261,7 +324,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
             dw = a.dw + (size_t)ch.group * size;
             db = a.db ? a.db + (size_t)ch.group * a.out : nullptr;
         } else {
-            dw = a.partial + (size_t)ch.id * partial_values(a.in, a.out);
+            dw = a.partial + (size_t)ch.shared * partial_values(a.in, a.out);
             db = dw + size;
         }
     }
@@ -270,8 +333,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
         const int64_t n = n0 + 64 * wn + 16 * j + (lane & 15);
         if (n >= nq) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t m = m0 + 64 * wm + 16 * i + 4 * (lane >> 4);
+        for (int i = 0; i < MI; ++i) {
+            const int64_t m = m0 + 16 * MI * wm + 16 * i + 4 * (lane >> 4);
             const int left = np - m >= 4 ? 4 : (int)(np - m);
             if (left <= 0) continue;
             if (MODE == kWeights) store_four(dw + (size_t)n * a.in + m, acc[i][j], left, a.in % 4 == 0 && a.wide_dw);
@@ -286,35 +349,36 @@ __global__ __launch_bounds__(kTileThreads, 2) void grouped_tile_kernel(Grouped a
 __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
     __shared__ __align__(16) f32x4 slices[16][16];
     const int g = blockIdx.y, lane = threadIdx.x & 63;
-    uint32_t first = 0, count = 0;
-    for (int g0 = 0; g0 <= g; g0 += 64) {
-        int64_t lo, hi;
-        uint32_t n = group_chunks(a.off, g0 + lane, g + 1, a.rows, a.log2, a.mult, true, lo, hi);
-        if (g0 + lane == g) count = n;
-        for (int d = 32; d; d >>= 1) n += (uint32_t)__shfl_xor((int)n, d);
-        first += n;
-    }
-    for (int d = 32; d; d >>= 1) count += (uint32_t)__shfl_xor((int)count, d);
-    first -= count;
+    int64_t lo, hi;
+    const uint32_t count = uniform(group_chunks(a.off, g, a.groups, a.rows, a.log2, a.mult, true, lo, hi));
     if (count <= 1) return;
+    uint32_t first = 0;
+    for (int g0 = 0; g0 < g; g0 += 64) {
+        const uint32_t n = group_chunks(a.off, g0 + lane, g, a.rows, a.log2, a.mult, true, lo, hi);
+        first += wave_sum(n > 1 ? n : 0);
+    }
+    if (first + count > a.shared_max) return;
     const size_t size = (size_t)a.in * a.out, all = size + a.out, stride = partial_values(a.in, a.out);
     const int quad = threadIdx.x & 15, slice = threadIdx.x >> 4;
-    const size_t e0 = (size_t)blockIdx.x * 64 + 4 * quad;
-    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (e0 < all) {
-        const float* from = a.partial + (size_t)first * stride + e0;
+    for (size_t e0 = (size_t)blockIdx.x * 64 + 4 * quad; e0 - 4 * quad < all; e0 += (size_t)gridDim.x * 64) {
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e0 < all) {
+            const float* from = a.partial + (size_t)first * stride + e0;
 #pragma unroll 4
-        for (uint32_t c = slice; c < count; c += 16) s += *reinterpret_cast<const f32x4*>(from + (size_t)c * stride);
-    }
-    slices[slice][quad] = s;
-    __syncthreads();
-    if (slice != 0 || e0 >= all) return;
-    for (int i = 1; i < 16; ++i) s += slices[i][quad];
+            for (uint32_t c = slice; c < count; c += 16) s += *reinterpret_cast<const f32x4*>(from + (size_t)c * stride);
+        }
+        slices[slice][quad] = s;
+        __syncthreads();
+        if (slice == 0 && e0 < all) {
+            for (int i = 1; i < 16; ++i) s += slices[i][quad];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const size_t e = e0 + j;
-        if (e < size) a.dw[(size_t)g * size + e] = s[j];
-        else if (e < all && a.db) a.db[(size_t)g * a.out + (e - size)] = s[j];
+            for (int j = 0; j < 4; ++j) {
+                const size_t e = e0 + j;
+                if (e < size) a.dw[(size_t)g * size + e] = s[j];
+                else if (e < all && a.db) a.db[(size_t)g * a.out + (e - size)] = s[j];
+            }
+        }
+        __syncthreads();
     }
 }
 

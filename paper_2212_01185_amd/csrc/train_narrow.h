@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_backward_kernel
     extern __shared__ __align__(16) u16 lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const Chunk ch = find_chunk(a.off, a.groups, a.rows, a.log2, a.mult, 1, blockIdx.x, true);
-    if (ch.group < 0) return;
+    if (ch.group < 0 || (ch.count > 1 && ch.shared >= a.shared_max)) return;    // (the second only with offsets that fall)
     const int n = (int)(ch.hi - ch.lo);
     const u16* dz = a.dz + (size_t)ch.lo * a.lddz;
     const u16* x = a.x + (size_t)ch.lo * a.ldx;
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_backward_kernel
     }
 
     const size_t size = (size_t)a.in * a.out;
-    float* dw = ch.count == 1 ? a.dw + (size_t)ch.group * size : a.partial + (size_t)ch.id * partial_values(a.in, a.out);
+    float* dw = ch.count == 1 ? a.dw + (size_t)ch.group * size : a.partial + (size_t)ch.shared * partial_values(a.in, a.out);
     float* db = ch.count == 1 ? a.db + (a.db ? (size_t)ch.group * a.out : 0) : dw + size;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {

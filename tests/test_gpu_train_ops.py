@@ -45,7 +45,7 @@ def test_contexts_are_what_the_oracle_gathers(orc, orc_diagonal, orc_paper):
 
 # (in, out): the codec's layers, odd ones, more than a tile
 SHAPES = [(32, 160), (160, 160), (160, 128), (128, 60), (40, 128), (128, 36), (128, 84), (192, 192), (64, 64), (1, 1), (7, 13), (30, 33),
-          (130, 257), (520, 136), (256, 520), (2, 300), (264, 40), (250, 6)]
+          (130, 257), (520, 136), (320, 520), (256, 520), (2, 300), (264, 40), (250, 6)]
 # rows of the groups, and rows of no group behind them
 GROUPS = [([1], 0), ([0, 3, 0, 130, 1], 5), ([127, 129], 0), ([0, 0], 3), ([333], 1)]
 
@@ -163,6 +163,20 @@ def test_offsets_that_make_no_sense_stay_inside():
         torch.cuda.synchronize()
         for t in (guard, dx):
             assert (t[:10] == 5).all() and (t[210:] == 5).all()
+
+
+@pytest.mark.parametrize("fan_in,fan_out", [(48, 24), (200, 264)])
+def test_falling_offsets_over_many_rows_stay_in_the_workspace(fan_in, fan_out):
+    """Groups that overlap have more chunks than the workspace has room for: their sums are nobody's, what lies behind it is not touched."""
+    rows, groups = 60000, 20
+    x, dz = torch.ones(rows, fan_in, dtype=BF16, device="cuda"), torch.ones(rows, fan_out, dtype=BF16, device="cuda")
+    w = torch.ones(groups, fan_out, fan_in, dtype=BF16, device="cuda")
+    off = torch.tensor([0, rows] * 10 + [0]).cuda()
+    need = binding.load().pcc_grouped_linear_grad_workspace_bytes(rows, groups, fan_in, fan_out)
+    space = torch.full((need + (1 << 20),), 77, dtype=torch.uint8, device="cuda")
+    binding.pcc_grouped_linear_grad(dz, x, w, off, workspace=space[:need])
+    torch.cuda.synchronize()
+    assert need > 0 and (space[need:] == 77).all()
 
 
 def test_many_groups():
