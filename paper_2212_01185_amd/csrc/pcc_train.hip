@@ -324,11 +324,12 @@ int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, co
     if (!ld_ok(ldp, 12 * K) || (d_grad && (!ld_ok(ldg, 12 * K) || grad_type < PCC_BF16 || grad_type > PCC_FP32))) return PCC_E_ARG;
     if (!aligned(d_params, 4) || !aligned(d_weight, 4) || !aligned(d_bits, 4) || (d_grad && !aligned(d_grad, size_of(grad_type)))) return PCC_E_ARG;
     if (count == 0) return PCC_OK;
-    const size_t blocks = (count + 255) / 256;
+    const size_t blocks = (count + 64 * kLossWaves - 1) / (64 * kLossWaves), lds = (size_t)kLossWaves * 64 * 12 * K * sizeof(float);
     if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
     auto go = [&](auto kernel) {
+        if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
         return launch([&] {
-            hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, (hipStream_t)hip_stream, d_params, ldp, d_rgb, d_weight, count, scale,
+            hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * kLossWaves), lds, (hipStream_t)hip_stream, d_params, ldp, d_rgb, d_weight, count, scale,
                                d_bits, d_grad, grad_type, ldg);
         });
     };

@@ -140,39 +140,101 @@ __device__ __forceinline__ float channel_loss(float (&o)[3 * K], const double (&
     return 16.0f - __builtin_amdgcn_logf(counts);
 }
 
+// A lane has a pixel.  A pixel's 12 K outputs are neighbours in memory, so a wave brings its 64 pixels' to LDS 16 bytes a lane, each lane
+// takes its own from there (rows of 12 K values: the 16 lanes that are served together read different banks), and the
+// gradients go the same way back.  Nothing is shared between waves.
+#ifndef LW
+#define LW 4
+#endif
+constexpr int kLossWaves = LW;
+
 template <int K, int DIST>
-__global__ __launch_bounds__(256) void mixture_loss_kernel(const float* params, size_t ldp, const uint8_t* __restrict__ rgb,
-                                                           const float* __restrict__ weight, size_t count, float scale,
-                                                           float* __restrict__ bits, void* grad, int grad_type, size_t ldg) {
-    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= count) return;
-    const float wt = weight ? weight[i] : 1.0f;
-    float out[12 * K], sum = 0.0f;
-    if (wt == 0.0f) {
-        for (int j = 0; j < 12 * K; ++j) out[j] = 0.0f;
-    } else {
-        const float* o = params + i * ldp;
-        const int r = rgb[3 * i], g = rgb[3 * i + 1], b = rgb[3 * i + 2];
-        const float rh = (float)r * (1.0f / 256.0f), gh = (float)g * (1.0f / 256.0f);
-        for (int c = 0; c < 3; ++c) {
-            float ch[3 * K];
-            double shift[K];
-            for (int j = 0; j < 3 * K; ++j) ch[j] = o[3 * K * c + j];
-            for (int k = 0; k < K; ++k)
-                shift[k] = c == 0 ? 0.0 : c == 1 ? (double)o[9 * K + k] * rh : __builtin_fma((double)o[11 * K + k], (double)gh, (double)o[10 * K + k] * rh);
-            sum += channel_loss<K, DIST>(ch, shift, c == 0 ? r : c == 1 ? g : b, wt * scale);
-            for (int j = 0; j < 3 * K; ++j) out[3 * K * c + j] = ch[j];
-            for (int k = 0; k < K; ++k) {
-                if (c == 1) out[9 * K + k] = ch[K + k] * rh;
-                if (c == 2) { out[10 * K + k] = ch[K + k] * rh; out[11 * K + k] = ch[K + k] * gh; }
-            }
+__global__ __launch_bounds__(64 * kLossWaves) void mixture_loss_kernel(const float* params, size_t ldp, const uint8_t* __restrict__ rgb,
+                                                                       const float* __restrict__ weight, size_t count, float scale,
+                                                                       float* __restrict__ bits, void* grad, int grad_type, size_t ldg) {
+    constexpr int N = 12 * K, kPieces = 3 * K;       // 16-byte pieces of a row
+    typedef f32x4 at_four __attribute__((aligned(4)));
+    extern __shared__ __align__(16) float loss_shared[];
+    const int lane = threadIdx.x & 63;
+    float* lds = loss_shared + (threadIdx.x >> 6) * 64 * N;
+    const size_t i0 = (size_t)blockIdx.x * (64 * kLossWaves) + (threadIdx.x & ~63u), i = i0 + lane;
+    if (i0 >= count) return;
+    const int pixels = count - i0 < 64 ? (int)(count - i0) : 64;
+#pragma unroll
+    for (int s = 0; s < kPieces; ++s) {
+        const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+        if (r < pixels) *reinterpret_cast<f32x4*>(lds + 4 * id) = *reinterpret_cast<const at_four*>(params + (i0 + r) * ldp + 4 * c);
+    }
+    const bool mine = lane < pixels;
+    const float wt = !mine ? 0.0f : weight ? weight[i] : 1.0f;
+    const int rgb3[3] = {mine ? rgb[3 * i] : 0, mine ? rgb[3 * i + 1] : 0, mine ? rgb[3 * i + 2] : 0};
+    const float rh = (float)rgb3[0] * (1.0f / 256.0f), gh = (float)rgb3[1] * (1.0f / 256.0f);
+    __builtin_amdgcn_wave_barrier();
+
+    float o[N], sum = 0.0f;
+    const f32x4* row = reinterpret_cast<const f32x4*>(lds + lane * N);
+#pragma unroll
+    for (int s = 0; s < kPieces; ++s) {
+        const f32x4 v = row[s];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[4 * s + e] = v[e];
+    }
+    const bool used = wt != 0.0f;
+#pragma unroll
+    for (int c = 0; c < 3; ++c) {
+        float ch[3 * K];
+        double shift[K];
+#pragma unroll
+        for (int j = 0; j < 3 * K; ++j) ch[j] = o[3 * K * c + j];
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            shift[k] = c == 0 ? 0.0 : c == 1 ? (double)o[9 * K + k] * rh : __builtin_fma((double)o[11 * K + k], (double)gh, (double)o[10 * K + k] * rh);
+        sum += channel_loss<K, DIST>(ch, shift, rgb3[c], wt * scale);
+#pragma unroll
+        for (int j = 0; j < 3 * K; ++j) o[3 * K * c + j] = used ? ch[j] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const float d = o[3 * K * c + K + k];
+            if (c == 1) o[9 * K + k] = d * rh;
+            if (c == 2) { o[10 * K + k] = d * rh; o[11 * K + k] = d * gh; }
         }
     }
-    if (bits) bits[i] = sum;
+    if (bits && mine) bits[i] = used ? sum : 0.0f;
     if (!grad) return;
-    for (int j = 0; j < 12 * K; ++j) {
-        if (grad_type == PCC_FP32) static_cast<float*>(grad)[i * ldg + j] = out[j];
-        else static_cast<u16*>(grad)[i * ldg + j] = grad_type == PCC_BF16 ? to16<Bf16>(out[j]) : to16<Fp16>(out[j]);
+    __builtin_amdgcn_wave_barrier();        // every lane has its outputs: LDS is free for the gradients
+    if (grad_type == PCC_FP32) {
+        f32x4* to = reinterpret_cast<f32x4*>(lds + lane * N);
+#pragma unroll
+        for (int s = 0; s < kPieces; ++s) to[s] = f32x4{o[4 * s], o[4 * s + 1], o[4 * s + 2], o[4 * s + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int s = 0; s < kPieces; ++s) {
+            const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+            if (r < pixels) *reinterpret_cast<at_four*>(static_cast<float*>(grad) + (i0 + r) * ldg + 4 * c) = *reinterpret_cast<const f32x4*>(lds + 4 * id);
+        }
+        return;
+    }
+    u16x4* to = reinterpret_cast<u16x4*>(lds) + lane * kPieces;
+#pragma unroll
+    for (int s = 0; s < kPieces; ++s) {
+        u16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = grad_type == PCC_BF16 ? to16<Bf16>(o[4 * s + e]) : to16<Fp16>(o[4 * s + e]);
+        to[s] = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+    u16* out = static_cast<u16*>(grad) + i0 * ldg;
+    const bool even = ldg % 2 == 0 && (reinterpret_cast<uintptr_t>(grad) & 3) == 0;
+#pragma unroll
+    for (int s = 0; s < kPieces; ++s) {
+        const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+        if (r >= pixels) continue;
+        const u16x4 v = reinterpret_cast<const u16x4*>(lds)[id];
+        u16* at = out + (size_t)r * ldg + 4 * c;
+        if (even) __builtin_memcpy(__builtin_assume_aligned(at, 4), &v, 8);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at[e] = v[e];
     }
 }
 

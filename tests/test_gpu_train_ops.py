@@ -106,7 +106,7 @@ def test_grouped_linear_grad(fan_in, fan_out, lengths, tail):
 
 
 @pytest.mark.parametrize("fan_in,fan_out,rows,groups", [(160, 160, 70001, 1), (128, 36, 40000, 3), (36, 128, 33333, 7), (64, 64, 20000, 40), (200, 520, 9000, 2),
-                                                        (300, 264, 20000, 1), (17, 9, 30000, 2)])
+                                                        (300, 264, 20000, 1), (17, 9, 30000, 2), (264, 1000, 17000, 2)])
 def test_many_rows(fan_in, fan_out, rows, groups):
     """Sums over chunks that are joined: values, the same bits every time, and every group its own."""
     share = np.random.default_rng(rows).dirichlet(np.ones(groups))
