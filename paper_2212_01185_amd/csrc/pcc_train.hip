@@ -1,10 +1,11 @@
-// Host side of the training operators of include/pcc.h, and the contexts' kernel.
+// Host side of the training operators of include/pcc.h.
 #include <algorithm>
 #include <new>
 #include <vector>
 
 #include "pcc.h"
 #include "train_adamw.h"
+#include "train_contexts.h"
 #include "train_grouped.h"
 #include "train_loss.h"
 #include "train_narrow.h"
@@ -36,43 +37,6 @@ constexpr size_t kMaxRows = (size_t)1 << 40;
 
 bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 size_t size_of(int type) { return type == PCC_FP32 ? 4 : 2; }
-
-// ---------------------------------------------------------------------------
-// Contexts.  A thread writes eight neighbouring values (16 bytes) of one row; the bytes that it gathers were read by its
-// neighbours too and come from the cache, so the output sets the time.
-// ---------------------------------------------------------------------------
-// Network input i of pixel (r, c): the byte of which pixel, or none.
-struct Tap { int dr, dc; };
-__host__ __device__ constexpr Tap tap_of(int nbhd, int delay, int j) {
-    const int run = nbhd == 10 ? 4 : 5;
-    Tap t = j < run ? Tap{-2, j - 2} : j < 2 * run ? Tap{-1, j - run - 2} : Tap{0, j - 2 * run - 2};
-    // diagonal order: (r-2,c+2), (r-1,c+1), (r-1,c+2) are not decoded when (r,c) is; the pixel above stands in
-    if (delay == 1 && ((t.dr == -2 && t.dc == 2) || (t.dr == -1 && t.dc >= 1))) t = {-1, 0};
-    return t;
-}
-
-template <int NBHD, int DELAY>
-__global__ __launch_bounds__(256) void contexts_kernel(const uint8_t* __restrict__ img, uint64_t pixels, int H, int W, u16* __restrict__ x,
-                                                       int width, size_t ldx, int chunks, int wide) {
-    const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint64_t p = id / chunks;
-    const int i0 = (int)(id % chunks) * 8;
-    if (p >= pixels) return;
-    const int c = (int)(p % W), r = (int)(p / W % H);
-    u16x8 v;
-    for (int e = 0; e < 8; ++e) {
-        const int i = i0 + e;
-        float f = 0.0f;
-        if (i < 3 * NBHD) {
-            const Tap t = tap_of(NBHD, DELAY, i / 3);
-            if (r + t.dr >= 0 && c + t.dc >= 0 && c + t.dc < W) f = (float)img[3 * (int64_t)(p + (int64_t)t.dr * W + t.dc) + i % 3] * (1.0f / 256.0f);
-        }
-        v[e] = to16<Bf16>(f);     // exact: eight significant bits
-    }
-    u16* to = x + p * ldx + i0;
-    if (wide && i0 + 8 <= width) *reinterpret_cast<u16x8*>(to) = v;
-    else for (int e = 0; e < 8; ++e) if (i0 + e < width) to[e] = v[e];
-}
 
 // ---------------------------------------------------------------------------
 // Grouped products.
@@ -243,11 +207,11 @@ int pcc_contexts(const uint8_t* d_img, int n, int H, int W, int nbhd, int delay,
     const uint64_t pixels = (uint64_t)n * H * W;
     if (!((nbhd == 10 && delay == 2) || (nbhd == 12 && (delay == 3 || delay == 1)))) return PCC_E_ARG;
     if (width < 3 * nbhd || width > PCC_MAX_FEATURES || !ld_ok(ldx, width) || !aligned(d_x, 2)) return PCC_E_ARG;
-    const int chunks = (width + 7) / 8, wide = aligned(d_x, 16) && ldx % 8 == 0;
-    const uint64_t blocks = (pixels * chunks + 255) / 256;
+    const uint64_t blocks = (pixels + kContextThreads - 1) / kContextThreads;
     if (pixels > kMaxRows || blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    const int wide = aligned(d_x, 4) && ldx % 2 == 0 && width % 8 == 0 && width <= kContextWidth;
     auto go = [&](auto kernel) {
-        return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(256), 0, (hipStream_t)hip_stream, d_img, pixels, H, W, (u16*)d_x, width, ldx, chunks, wide); });
+        return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(kContextThreads), 0, (hipStream_t)hip_stream, d_img, pixels, H, W, (u16*)d_x, width, ldx, wide); });
     };
     return nbhd == 10 ? go(contexts_kernel<10, 2>) : delay == 3 ? go(contexts_kernel<12, 3>) : go(contexts_kernel<12, 1>);
 }
@@ -330,11 +294,16 @@ int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, co
         if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
         return launch([&] {
             hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(64 * kLossWaves), lds, (hipStream_t)hip_stream, d_params, ldp, d_rgb, d_weight, count, scale,
-                               d_bits, d_grad, grad_type, ldg);
+                               d_bits, d_grad, ldg);
         });
     };
-    if (dist == 0) return K == 3 ? go(mixture_loss_kernel<3, 0>) : K == 5 ? go(mixture_loss_kernel<5, 0>) : go(mixture_loss_kernel<7, 0>);
-    return K == 3 ? go(mixture_loss_kernel<3, 1>) : K == 5 ? go(mixture_loss_kernel<5, 1>) : go(mixture_loss_kernel<7, 1>);
+    auto with_type = [&](auto k, auto f) {
+        constexpr int N = decltype(k)::value, F = decltype(f)::value;
+        const int type = d_grad ? grad_type : PCC_FP32;
+        return type == PCC_BF16 ? go(mixture_loss_kernel<N, F, PCC_BF16>) : type == PCC_FP16 ? go(mixture_loss_kernel<N, F, PCC_FP16>) : go(mixture_loss_kernel<N, F, PCC_FP32>);
+    };
+    auto with_dist = [&](auto k) { return dist == 0 ? with_type(k, std::integral_constant<int, 0>{}) : with_type(k, std::integral_constant<int, 1>{}); };
+    return K == 3 ? with_dist(std::integral_constant<int, 3>{}) : K == 5 ? with_dist(std::integral_constant<int, 5>{}) : with_dist(std::integral_constant<int, 7>{});
 }
 
 int pcc_adamw_create(pcc_adamw** out, const pcc_adamw_tensor* h_tensors, int count, int grad_type, int copy_type, int state_bits,

@@ -16,20 +16,23 @@
 //   - near f(near) - far f(far) = m (f(near) - f(far)) - h (f(near) + f(far))
 #pragma once
 
+#include <type_traits>
+
 #include "train_device.h"
 
 namespace pcc_train {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 
-// e^v by the hardware's 2^x: v log2(e) as a rounded product and what the rounding and the constant's own left out (without it
-// e^-8 is 3e-7 off, and a distance in widths of that component with it).
-__device__ __forceinline__ float exp_of(float v) {
-    const float t = v * kLog2e;
-    const float rest = __builtin_fmaf(v, kLog2e, -t) + v * 1.925962989e-8f;
-    const float e = __builtin_amdgcn_exp2f(t);
-    return t > -126.0f && t < 128.0f ? __builtin_fmaf(e, rest * kLn2, e) : e;
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+// The same for |v| <= 8, with what the rounding of v log2(e) and of the constant left out: without it e^-8 is 3e-7 off, and a
+// distance in widths of that component with it.
+__device__ __forceinline__ float exp_exact(float v) {
+    const float t = v * kLog2e, e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, __builtin_fmaf(v, 1.925962989e-8f, __builtin_fmaf(v, kLog2e, -t)) * kLn2, e);
 }
+// f(z) of the standard normal distribution.
+__device__ __forceinline__ float normal_density(float z) { return 0.39894228040143268f * __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e)); }
 
 // Q(z) / f(z) of the standard normal distribution, z >= 0.
 __device__ __forceinline__ float mills(float z) {
@@ -53,10 +56,15 @@ struct Bin {
     float d_ls;     // a f(a) - b f(b)
 };
 
+// v, or -v where `sign` is negative.
+__device__ __forceinline__ float with_sign(float v, float sign) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) ^ (__builtin_bit_cast(uint32_t, sign) & 0x80000000u));
+}
+
 // mid: the level's middle, h: half a level, both in widths of the component; first, last: the level is 0, 255 (open ends).
 template <int DIST>
 __device__ __forceinline__ Bin bin_of(float mid, float h, bool first, bool last) {
-    const bool mirrored = mid < 0.0f;
+    const bool mirrored = __builtin_signbit(mid);
     const float m = fabsf(mid), near = m - h, far = m + h;
     const bool open_near = mirrored ? last : first, open_far = mirrored ? first : last;
     float q, diff, sum;     // diff, sum: f(near) -+ f(far)
@@ -79,27 +87,27 @@ __device__ __forceinline__ Bin bin_of(float mid, float h, bool first, bool last)
             sum = __builtin_fmaf(sn, 1.0f - sn, sf * (1.0f - sf));
         }
     } else {
-        const float c = 0.39894228040143268f, d = 2.0f * h;
+        const float d = 2.0f * h;
         if (d * (m + 1.0f) < 0.5f && !open_near && !open_far) {
-            const float f = c * exp_of(-0.5f * m * m), z2 = m * m, d2 = d * d * (1.0f / 24.0f), d4 = d * d * d * d * (1.0f / 1920.0f);
+            const float f = normal_density(m), z2 = m * m, d2 = d * d * (1.0f / 24.0f), d4 = d * d * d * d * (1.0f / 1920.0f);
             const float he2 = z2 - 1.0f, he4 = __builtin_fmaf(z2, z2 - 6.0f, 3.0f), he6 = __builtin_fmaf(z2, __builtin_fmaf(z2, z2 - 15.0f, 45.0f), -15.0f);
             const float he3 = m * (z2 - 3.0f), he5 = m * __builtin_fmaf(z2, z2 - 10.0f, 15.0f);
             const float df = d * f;
             Bin b;
             b.q = df * __builtin_fmaf(he4, d4, __builtin_fmaf(he2, d2, 1.0f));
             const float dm = df * __builtin_fmaf(he5, d4, __builtin_fmaf(he3, d2, m));
-            b.d_mu = mirrored ? -dm : dm;
+            b.d_mu = with_sign(dm, mid);
             b.d_ls = df * __builtin_fmaf(he6, d4, __builtin_fmaf(he4, d2, he2));
             return b;
         }
-        const float fn = open_near ? 0.0f : c * exp_of(-0.5f * near * near), ff = open_far ? 0.0f : c * exp_of(-0.5f * far * far);
+        const float fn = open_near ? 0.0f : normal_density(near), ff = open_far ? 0.0f : normal_density(far);
         const float tn = fn * mills(fabsf(near)), tail_near = open_near ? 1.0f : near < 0.0f ? 1.0f - tn : tn;
         const float tail_far = open_far ? 0.0f : ff * mills(far);
         q = tail_near - tail_far;
         diff = fn - ff;
         sum = fn + ff;
     }
-    return {q, mirrored ? -diff : diff, __builtin_fmaf(m, diff, -(h * sum))};
+    return {q, with_sign(diff, mid), __builtin_fmaf(m, diff, -(h * sum))};
 }
 
 // One channel: returns its bits and puts the gradient in place of the channel's 3 K outputs (logits, means, log-sigmas).  shift: what
@@ -122,7 +130,7 @@ __device__ __forceinline__ float channel_loss(float (&o)[3 * K], const double (&
         const float raw = o[2 * K + k];
         const bool inside = raw >= -8.0f && raw <= 4.0f;
         const float ls = raw > 4.0f ? 4.0f : raw >= -8.0f ? raw : -8.0f;
-        const float width = exp_of(-ls);
+        const float width = exp_exact(-ls);
         const Bin b = bin_of<DIST>((float)(x - (double)o[K + k] - shift[k]) * width, width * (1.0f / 512.0f), level == 0, level == 255);
         q[k] = b.q;
         p = __builtin_fmaf(pi[k], b.q, p);
@@ -143,27 +151,34 @@ __device__ __forceinline__ float channel_loss(float (&o)[3 * K], const double (&
 // A lane has a pixel.  A pixel's 12 K outputs are neighbours in memory, so a wave brings its 64 pixels' to LDS 16 bytes a lane, each lane
 // takes its own from there (rows of 12 K values: the 16 lanes that are served together read different banks), and the
 // gradients go the same way back.  Nothing is shared between waves.
-#ifndef LW
-#define LW 4
-#endif
-constexpr int kLossWaves = LW;
+// One wave is a workgroup (2048x1365 pixels, K = 5: 202 us; four are 208).
+constexpr int kLossWaves = 1;
 
-template <int K, int DIST>
+// GRAD: the gradients' type.
+template <int K, int DIST, int GRAD>
 __global__ __launch_bounds__(64 * kLossWaves) void mixture_loss_kernel(const float* params, size_t ldp, const uint8_t* __restrict__ rgb,
                                                                        const float* __restrict__ weight, size_t count, float scale,
-                                                                       float* __restrict__ bits, void* grad, int grad_type, size_t ldg) {
+                                                                       float* __restrict__ bits, void* grad, size_t ldg) {
     constexpr int N = 12 * K, kPieces = 3 * K;       // 16-byte pieces of a row
     typedef f32x4 at_four __attribute__((aligned(4)));
+    typedef u16x4 at_four_16 __attribute__((aligned(4)));
     extern __shared__ __align__(16) float loss_shared[];
     const int lane = threadIdx.x & 63;
     float* lds = loss_shared + (threadIdx.x >> 6) * 64 * N;
-    const size_t i0 = (size_t)blockIdx.x * (64 * kLossWaves) + (threadIdx.x & ~63u), i = i0 + lane;
+    const size_t i0 = (size_t)blockIdx.x * (64 * kLossWaves) + uniform(threadIdx.x & ~63u), i = i0 + lane;
     if (i0 >= count) return;
     const int pixels = count - i0 < 64 ? (int)(count - i0) : 64;
+    const float* from = params + i0 * ldp;
+    // 64 whole rows one behind the other are one piece of memory; else every piece has its row looked up
+    const bool in_line = pixels == 64 && ldp == (size_t)N, out_line = pixels == 64 && ldg == (size_t)N;
+    if (in_line) {
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
-        const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
-        if (r < pixels) *reinterpret_cast<f32x4*>(lds + 4 * id) = *reinterpret_cast<const at_four*>(params + (i0 + r) * ldp + 4 * c);
+        for (int s = 0; s < kPieces; ++s) *reinterpret_cast<f32x4*>(lds + 4 * (lane + 64 * s)) = *reinterpret_cast<const at_four*>(from + 4 * (lane + 64 * s));
+    } else {
+        for (int s = 0; s < kPieces; ++s) {
+            const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+            if (r < pixels) *reinterpret_cast<f32x4*>(lds + 4 * id) = *reinterpret_cast<const at_four*>(from + (size_t)r * ldp + 4 * c);
+        }
     }
     const bool mine = lane < pixels;
     const float wt = !mine ? 0.0f : weight ? weight[i] : 1.0f;
@@ -179,7 +194,6 @@ __global__ __launch_bounds__(64 * kLossWaves) void mixture_loss_kernel(const flo
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[4 * s + e] = v[e];
     }
-    const bool used = wt != 0.0f;
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
         float ch[3 * K];
@@ -191,50 +205,58 @@ __global__ __launch_bounds__(64 * kLossWaves) void mixture_loss_kernel(const flo
             shift[k] = c == 0 ? 0.0 : c == 1 ? (double)o[9 * K + k] * rh : __builtin_fma((double)o[11 * K + k], (double)gh, (double)o[10 * K + k] * rh);
         sum += channel_loss<K, DIST>(ch, shift, rgb3[c], wt * scale);
 #pragma unroll
-        for (int j = 0; j < 3 * K; ++j) o[3 * K * c + j] = used ? ch[j] : 0.0f;
+        for (int j = 0; j < 3 * K; ++j) o[3 * K * c + j] = ch[j];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const float d = o[3 * K * c + K + k];
+            const float d = ch[K + k];
             if (c == 1) o[9 * K + k] = d * rh;
             if (c == 2) { o[10 * K + k] = d * rh; o[11 * K + k] = d * gh; }
         }
     }
-    if (bits && mine) bits[i] = used ? sum : 0.0f;
+    if (__ballot(wt == 0.0f)) {             // pixels that do not count, whatever their outputs were
+        if (wt == 0.0f) sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[j] = wt == 0.0f ? 0.0f : o[j];
+    }
+    if (bits && mine) bits[i] = sum;
     if (!grad) return;
     __builtin_amdgcn_wave_barrier();        // every lane has its outputs: LDS is free for the gradients
-    if (grad_type == PCC_FP32) {
+    if constexpr (GRAD == PCC_FP32) {
         f32x4* to = reinterpret_cast<f32x4*>(lds + lane * N);
 #pragma unroll
         for (int s = 0; s < kPieces; ++s) to[s] = f32x4{o[4 * s], o[4 * s + 1], o[4 * s + 2], o[4 * s + 3]};
         __builtin_amdgcn_wave_barrier();
+        float* out = static_cast<float*>(grad) + i0 * ldg;
+        if (out_line) {
 #pragma unroll
-        for (int s = 0; s < kPieces; ++s) {
-            const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
-            if (r < pixels) *reinterpret_cast<at_four*>(static_cast<float*>(grad) + (i0 + r) * ldg + 4 * c) = *reinterpret_cast<const f32x4*>(lds + 4 * id);
+            for (int s = 0; s < kPieces; ++s) *reinterpret_cast<at_four*>(out + 4 * (lane + 64 * s)) = *reinterpret_cast<const f32x4*>(lds + 4 * (lane + 64 * s));
+        } else {
+            for (int s = 0; s < kPieces; ++s) {
+                const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+                if (r < pixels) *reinterpret_cast<at_four*>(out + (size_t)r * ldg + 4 * c) = *reinterpret_cast<const f32x4*>(lds + 4 * id);
+            }
         }
-        return;
-    }
-    u16x4* to = reinterpret_cast<u16x4*>(lds) + lane * kPieces;
+    } else {
+        using T = std::conditional_t<GRAD == PCC_BF16, Bf16, Fp16>;
+        u16x4* to = reinterpret_cast<u16x4*>(lds) + lane * kPieces;
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
-        u16x4 v;
+        for (int s = 0; s < kPieces; ++s) to[s] = u16x4{to16<T>(o[4 * s]), to16<T>(o[4 * s + 1]), to16<T>(o[4 * s + 2]), to16<T>(o[4 * s + 3])};
+        __builtin_amdgcn_wave_barrier();
+        u16* out = static_cast<u16*>(grad) + i0 * ldg;
+        const u16x4* held = reinterpret_cast<const u16x4*>(lds);
+        const bool even = ldg % 2 == 0 && (reinterpret_cast<uintptr_t>(grad) & 3) == 0;
+        if (out_line && even) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = grad_type == PCC_BF16 ? to16<Bf16>(o[4 * s + e]) : to16<Fp16>(o[4 * s + e]);
-        to[s] = v;
-    }
-    __builtin_amdgcn_wave_barrier();
-    u16* out = static_cast<u16*>(grad) + i0 * ldg;
-    const bool even = ldg % 2 == 0 && (reinterpret_cast<uintptr_t>(grad) & 3) == 0;
-#pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
-        const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
-        if (r >= pixels) continue;
-        const u16x4 v = reinterpret_cast<const u16x4*>(lds)[id];
-        u16* at = out + (size_t)r * ldg + 4 * c;
-        if (even) __builtin_memcpy(__builtin_assume_aligned(at, 4), &v, 8);
-        else
-#pragma unroll
-            for (int e = 0; e < 4; ++e) at[e] = v[e];
+            for (int s = 0; s < kPieces; ++s) *reinterpret_cast<at_four_16*>(out + 4 * (lane + 64 * s)) = held[lane + 64 * s];
+        } else {
+            for (int s = 0; s < kPieces; ++s) {
+                const int id = lane + 64 * s, r = id / kPieces, c = id % kPieces;
+                if (r >= pixels) continue;
+                u16* at = out + (size_t)r * ldg + 4 * c;
+                if (even) *reinterpret_cast<at_four_16*>(at) = held[id];
+                else for (int e = 0; e < 4; ++e) at[e] = held[id][e];
+            }
+        }
     }
 }
 
