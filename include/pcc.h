@@ -277,7 +277,7 @@ int pcc_mixture_loss(const float *d_params, size_t ldp, const uint8_t *d_rgb, co
                      int K, int dist, float scale, float *d_bits, void *d_grad, int grad_type, size_t ldg,
                      void *hip_stream);
 
-/* AdamW over many tensors in one launch.  With t = *d_step + 1, written back:
+/* AdamW over many tensors, all in one launch.  With t = *d_step + 1, written back:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g g,
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in fp32, and the 16-bit copy of the new param where there is one (what the

@@ -248,22 +248,29 @@ _TYPES = {torch.bfloat16: PCC_BF16, torch.float16: PCC_FP16, torch.float32: PCC_
 def _check(what: str, t, dtypes, shape, device=None, rows: bool = False):
     """A tensor argument: of one of `dtypes`, of `shape` (None: any size), on a GPU (`device`), contiguous or with `rows` a matrix
     whose rows are.  Returns the distance of its rows."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)):
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or (t.shape != shape and (
+            t.dim() != len(shape) or any(s is not None and s != n for s, n in zip(shape, t.shape)))):
         raise ValueError("%s must be a tensor %s of %s" % (what, list("?" if s is None else s for s in shape), " or ".join(str(d) for d in dtypes)))
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError("%s must be on %s" % (what, device or "a GPU"))
     if rows:
-        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        n, width = t.shape
+        apart, step = t.stride()
+        if (width > 1 and step != 1) or (n > 1 and apart < width):
             raise ValueError("%s must have contiguous rows that do not overlap" % what)
-        return max(int(t.stride(0)), int(t.shape[1])) if t.shape[0] > 1 else int(t.shape[1])
+        return apart if n > 1 else width
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % what)
     return 0
 
 
 def _call(what: str, device, *args) -> None:
-    with torch.cuda.device(device):
-        rc = getattr(load(), what)(*args, C.c_void_p(torch.cuda.current_stream(device).cuda_stream))
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = getattr(_lib or load(), what)(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(_lib or load(), what)(*args, stream)
     if rc != PCC_OK:
         raise PccError(rc, what)
 
@@ -328,7 +335,7 @@ def pcc_grouped_linear_grad(dz: torch.Tensor, x: torch.Tensor, w: torch.Tensor, 
     _check("dw", dw, (torch.float32,), tuple(w.shape), x.device)
     _check("db", db, (torch.float32,), (groups, n_out), x.device)
     if workspace is None:
-        need = int(load().pcc_grouped_linear_grad_workspace_bytes(rows, groups, n_in, n_out))
+        need = int((_lib or load()).pcc_grouped_linear_grad_workspace_bytes(rows, groups, n_in, n_out))
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
     else:
         _check("workspace", workspace, (torch.uint8,), (None,), x.device)
