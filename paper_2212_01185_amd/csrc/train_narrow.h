@@ -286,6 +286,11 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_backward_kernel
                     d0 = T::mfma(*reinterpret_cast<const u16x8*>(p + k * 512), q[k], d0);
                     d1 = T::mfma(*reinterpret_cast<const u16x8*>(p + (KBS + k) * 512), q[k], d1);
                 }
+                // the products' results are complete on both sides of the branch: eight wait states, which the compiler counts on its own
+                // in straight-line code only
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_nop 7");
+                __builtin_amdgcn_sched_barrier(0);
                 const int f = 32 * pair + 8 * quad;
                 if (a.act != PCC_ACT_NONE) {
                     const u16x8 s = *reinterpret_cast<const u16x8*>(xt + my_row * kXRow + f);
