@@ -213,7 +213,8 @@ int pcc_last_timings(pcc_ctx *ctx, float *h_ms);
  * asynchronous, allocate nothing, keep nothing, use no memory but their
  * arguments and may be captured into a HIP graph.  Types are PCC_BF16,
  * PCC_FP16 and PCC_FP32.  ld... is the distance between rows in elements, at
- * least the row's length and at most 2^22.  Outputs must not overlap inputs. */
+ * least the row's length and at most 2^22.  Outputs must not overlap inputs.
+ * Without any rows the pointers to rows may be NULL. */
 
 #define PCC_BF16 0
 #define PCC_FP16 1
@@ -306,7 +307,8 @@ typedef struct {
 typedef struct pcc_adamw pcc_adamw;
 
 /* Lay out the list of tensors (host array, copied) on device `hip_device`.  The
- * tensors stay the caller's and must outlive the plan.  Allocates device memory
+ * tensors stay the caller's and must outlive the plan; what a step writes must not
+ * overlap (PCC_E_ARG).  Allocates device memory
  * and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
  * PCC_BF16 or PCC_FP16; state_bits 32 or 8. */
 int pcc_adamw_create(pcc_adamw **out, const pcc_adamw_tensor *h_tensors, int count, int grad_type, int copy_type,

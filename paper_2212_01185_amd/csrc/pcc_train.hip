@@ -1,6 +1,7 @@
 // Host side of the training operators of include/pcc.h.
 #include <algorithm>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "pcc.h"
@@ -219,7 +220,7 @@ int pcc_contexts(const uint8_t* d_img, int n, int H, int W, int nbhd, int delay,
 
 int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float* d_bias, const int64_t* d_offsets, int groups,
                        size_t rows, int in, int out, int type, int act, void* d_y, int y_type, size_t ldy, void* hip_stream) {
-    if (!d_x || !d_w || !d_offsets || !d_y || !features_ok(in, out, groups, rows) || !ld_ok(ldx, in) || !ld_ok(ldy, out)) return PCC_E_ARG;
+    if ((rows && (!d_x || !d_y)) || !d_w || !d_offsets || !features_ok(in, out, groups, rows) || !ld_ok(ldx, in) || !ld_ok(ldy, out)) return PCC_E_ARG;
     if ((type != PCC_BF16 && type != PCC_FP16) || (y_type != type && y_type != PCC_FP32) || act < PCC_ACT_RELU || act > PCC_ACT_NONE) return PCC_E_ARG;
     if (!aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_bias, 4) || !aligned(d_offsets, 8) || !aligned(d_y, size_of(y_type))) return PCC_E_ARG;
     if (rows == 0) return PCC_OK;
@@ -249,7 +250,7 @@ size_t pcc_grouped_linear_grad_workspace_bytes(size_t rows, int groups, int in, 
 int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size_t ldx, const void* d_w, const int64_t* d_offsets,
                             int groups, size_t rows, int in, int out, int type, int x_act, void* d_dx, size_t lddx, float* d_dw,
                             float* d_db, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
-    if (!d_dz || !d_x || !d_offsets || (!d_dx && !d_dw) || (d_dx && !d_w) || (d_db && !d_dw)) return PCC_E_ARG;
+    if ((rows && (!d_dz || !d_x)) || !d_offsets || (rows && !d_dx && !d_dw) || (d_dx && !d_w) || (d_db && !d_dw)) return PCC_E_ARG;
     if (!features_ok(in, out, groups, rows) || !ld_ok(lddz, out) || !ld_ok(ldx, in) || (d_dx && !ld_ok(lddx, in))) return PCC_E_ARG;
     if ((type != PCC_BF16 && type != PCC_FP16) || x_act < PCC_ACT_RELU || x_act > PCC_ACT_NONE) return PCC_E_ARG;
     if (!aligned(d_dz, 2) || !aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_offsets, 8) || !aligned(d_dx, 2) || !aligned(d_dw, 4) ||
@@ -285,7 +286,7 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
 
 int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, const float* d_weight, size_t count, int K, int dist,
                      float scale, float* d_bits, void* d_grad, int grad_type, size_t ldg, void* hip_stream) {
-    if (!d_params || !d_rgb || (!d_bits && !d_grad) || (K != 3 && K != 5 && K != 7) || (dist != 0 && dist != 1)) return PCC_E_ARG;
+    if ((count && (!d_params || !d_rgb || (!d_bits && !d_grad))) || (K != 3 && K != 5 && K != 7) || (dist != 0 && dist != 1)) return PCC_E_ARG;
     if (!ld_ok(ldp, 12 * K) || (d_grad && (!ld_ok(ldg, 12 * K) || grad_type < PCC_BF16 || grad_type > PCC_FP32))) return PCC_E_ARG;
     if (!aligned(d_params, 4) || !aligned(d_weight, 4) || !aligned(d_bits, 4) || (d_grad && !aligned(d_grad, size_of(grad_type)))) return PCC_E_ARG;
     if (count == 0) return PCC_OK;
@@ -332,6 +333,22 @@ int pcc_adamw_create(pcc_adamw** out, const pcc_adamw_tensor* h_tensors, int cou
     const size_t at_pieces = 64 + (size_t)count * sizeof(AdamwTensor);
     try {
         table.assign(at_pieces + (size_t)pieces * sizeof(AdamwPiece), 0);
+        // what a step writes is written once: a tensor that is listed twice, or shares bytes with another, has no result
+        std::vector<std::pair<uintptr_t, uintptr_t>> written;
+        auto add = [&](const void* p, size_t bytes) { if (p && bytes) written.emplace_back((uintptr_t)p, (uintptr_t)p + bytes); };
+        for (int i = 0; i < count; ++i) {
+            const pcc_adamw_tensor& s = h_tensors[i];
+            const size_t scales = state_bits == 8 ? (s.n + kStateBlock - 1) / kStateBlock * sizeof(float) : 0;
+            add(s.d_param, s.n * 4);
+            add(s.d_copy, s.n * 2);
+            add(s.d_m, s.n * state);
+            add(s.d_v, s.n * state);
+            add(s.d_m_scale, scales);
+            add(s.d_v_scale, scales);
+        }
+        std::sort(written.begin(), written.end());
+        for (size_t i = 1; i < written.size(); ++i)
+            if (written[i].first < written[i - 1].second) return PCC_E_ARG;
     } catch (const std::bad_alloc&) {
         return PCC_E_INTERNAL;
     }

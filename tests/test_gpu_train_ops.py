@@ -539,6 +539,22 @@ def test_two_streams_at_once_with_a_workspace_each():
         assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+@pytest.mark.parametrize("fan_in,fan_out", [(32, 16), (300, 7)])
+def test_without_any_rows(fan_in, fan_out):
+    x, w, bias, dz, off = _inputs(BF16, fan_in, fan_out, [0, 0], 0, ref.NONE, 1)
+    assert binding.pcc_grouped_linear(x, w, bias, off).shape == (0, fan_out)
+    dx, dw, db = binding.pcc_grouped_linear_grad(dz, x, w, off, dw=torch.ones_like(w, dtype=FP32), db=torch.ones_like(bias))
+    assert dx.shape == (0, fan_in) and (dw == 0).all() and (db == 0).all()
+    bits, grad = binding.pcc_mixture_loss(torch.zeros(0, 36, device="cuda"), torch.zeros(0, 3, dtype=torch.uint8, device="cuda"))
+    assert bits.numel() == 0 and grad.shape == (0, 36)
+
+
+def test_adamw_of_the_same_tensor_twice_is_refused():
+    p, g = torch.zeros(300, device="cuda"), torch.zeros(300, device="cuda")
+    with pytest.raises(binding.PccError):
+        binding.AdamW([p, p[100:]], [g, g[100:]])
+
+
 def test_gpu_tensors_that_do_not_fit_are_refused():
     x, w, bias, dz, off = _inputs(BF16, 32, 16, [4, 4], 0, ref.NONE, 1)
     for bad in (lambda: binding.pcc_grouped_linear(x, w.half(), bias, off), lambda: binding.pcc_grouped_linear(x, w, bias.half(), off),

@@ -40,6 +40,7 @@ def test_grouped_linear(changes):
 
 def test_grouped_linear_without_rows_does_nothing():
     assert call("pcc_grouped_linear", LINEAR, rows=0) == binding.PCC_OK
+    assert call("pcc_grouped_linear", LINEAR, rows=0, x=None, y=None) == binding.PCC_OK
 
 
 GRAD = dict(dz=P, lddz=16, x=P, ldx=32, w=P, off=P, groups=2, rows=8, fan_in=32, fan_out=16, type=0, x_act=0, dx=P, lddx=32, dw=P, db=P,
@@ -74,6 +75,7 @@ def test_mixture_loss(changes):
 
 def test_mixture_loss_of_nothing():
     assert call("pcc_mixture_loss", LOSS, count=0) == binding.PCC_OK
+    assert call("pcc_mixture_loss", LOSS, count=0, params=None, rgb=None, bits=None, grad=None) == binding.PCC_OK
 
 
 def _plan(count=1, grad_type=2, copy_type=0, bits=32, device=0, out=True, table=True, **tensor):
@@ -91,6 +93,12 @@ def _plan(count=1, grad_type=2, copy_type=0, bits=32, device=0, out=True, table=
                                      dict(d_copy=P + 1), dict(d_m=P + 2), dict(bits=8, d_m_scale=None), dict(bits=8, d_v_scale=P + 2), dict(n=1 << 41)])
 def test_adamw_create(changes):
     assert _plan(**changes) == ARG
+
+
+def test_adamw_refuses_tensors_that_share_bytes():
+    far = dict(d_grad=P, d_copy=None, d_m=2 * P, d_v=3 * P, d_m_scale=None, d_v_scale=None)
+    assert _plan(count=2, d_param=5 * P, **far) == ARG                       # one tensor twice
+    assert _plan(count=1, d_param=2 * P + 36, **far) == ARG                  # the last element of m is the parameter's first
 
 
 def test_adamw_step_without_a_plan():
