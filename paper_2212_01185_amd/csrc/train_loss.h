@@ -150,7 +150,8 @@ __device__ __forceinline__ float channel_loss(float (&o)[3 * K], const double (&
 
 // A lane has a pixel.  A pixel's 12 K outputs are neighbours in memory, so a wave brings its 64 pixels' to LDS 16 bytes a lane, each lane
 // takes its own from there (rows of 12 K values: the 16 lanes that are served together read different banks), and the
-// gradients go the same way back.  Nothing is shared between waves.
+// gradients go the same way back.  Nothing is shared between waves.  2048x1365 pixels, K = 5, gradients in bf16: 202 us, 5.1 TB/s, what a large copy
+// has (each lane reading its own row from memory: 821; with a division for each piece, and both 16-bit types in one kernel: 386).
 // One wave is a workgroup (2048x1365 pixels, K = 5: 202 us; four are 208).
 constexpr int kLossWaves = 1;
 
