@@ -68,7 +68,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 // bytes a lane: by themselves, without a register, if all operands are read along (the compiler waits for all such loads
 // before a ds_read_b64_tr_b16, of which it cannot tell what it must see), else by registers.  A chunk that is cut by the end of its row is
 // read value by value, and what lies beyond the operand is zero (a lane's offset beyond the buffer's end loads zeros).  Rows
-// at odd elements are read value by value.
+// at odd elements take the way by registers, with loads that may begin anywhere.
 template <bool ACROSS, int TILE>
 struct Source {
     static constexpr int kThreads = tile_threads(TILE);
@@ -106,6 +106,10 @@ struct Source {
     __device__ u32x4 one_by_one(int r, int c, int64_t k0, int n) const {
         const u16* from = base + (ACROSS ? (size_t)(k0 + r) * ld + 8 * c : (size_t)r * ld + (size_t)k0 + 8 * c);
         u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (n == 8) {           // a whole chunk, at any address: one load (buffers want multiples of four)
+            __builtin_memcpy(&v, from, 16);
+            return __builtin_bit_cast(u32x4, v);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < n) v[j] = from[j];
