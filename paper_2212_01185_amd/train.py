@@ -66,8 +66,18 @@ class Trainer:
             self.w16.append(self.w[-1].to(torch.bfloat16))
             self.dw.append(torch.zeros_like(self.w[-1]))
             self.db.append(torch.zeros_like(self.b[-1]))
-        self.optimizer = binding.AdamW(self.w + self.b, self.dw + self.db, copies=self.w16 + [None] * len(self.b), state_bits=state_bits, lr=lr,
-                                       betas=betas, eps=eps, weight_decay=weight_decay, lr_tensor=lr_tensor)
+        # 8-bit states have one scale for 256 elements of a tensor: where a network's share is not whole blocks it is a tensor of its
+        # own, so that no network's states hang on another's
+        def shares(t):
+            return list(t.unbind(0)) if state_bits == 8 and t[0].numel() % binding.STATE_BLOCK else [t]
+
+        lists = [[], [], []]
+        for row in list(zip(self.w, self.dw, self.w16)) + [(b, db, None) for b, db in zip(self.b, self.db)]:
+            parts = [shares(t) if t is not None else None for t in row]
+            for own, part in zip(lists, parts):
+                own.extend(part if part is not None else [None] * len(parts[0]))
+        self.optimizer = binding.AdamW(lists[0], lists[1], copies=lists[2], state_bits=state_bits, lr=lr, betas=betas, eps=eps,
+                                       weight_decay=weight_decay, lr_tensor=lr_tensor)
 
     def gradients(self, pictures) -> torch.Tensor:
         """Forward and backward pass; the gradients of each network's mean code length are left in ``dw`` and ``db``.

@@ -1,0 +1,64 @@
+"""Optimizer states of a training step where blocks, networks and numbers meet their limits.  Needs an MI355X."""
+import numpy as np
+import pytest
+import torch
+
+import train_reference as ref
+from paper_2212_01185_amd import synth, train
+
+pytestmark = pytest.mark.gpu
+
+
+def _bits(t):
+    return t.contiguous().view(torch.uint8)
+
+
+def _fill(trainer, step, dirty=None):
+    """Gradients of every network, of very different sizes; `dirty`: (network, value) of one element of each bias."""
+    gen = torch.Generator().manual_seed(step)
+    for t in trainer.dw + trainer.db:
+        for g in range(trainer.groups):
+            t[g] = (torch.randn(t[g].shape, generator=gen) * 10.0 ** (2 * g - 3)).to(t.device)
+    if dirty:
+        for t in trainer.db:
+            t[dirty[0], 5] = dirty[1]
+
+
+@pytest.mark.parametrize("state_bits", [32, 8])
+@pytest.mark.parametrize("make", [synth.make_blob, synth.make_paper_blob])
+def test_a_network_moves_as_it_would_alone(make, state_bits):
+    """From the same gradients, whatever the other networks' are: the same bits, also where one of the others' moments is not finite."""
+    blobs = [make(s) for s in (1, 2, 3)]
+    hyper = dict(lr=1e-3, weight_decay=0.01, state_bits=state_bits)
+    together, alone = train.Trainer(blobs, **hyper), [train.Trainer(b, **hyper) for b in blobs]
+    for step in range(4):
+        _fill(together, step, (1, float("inf")) if step == 2 else None)
+        for g, one in enumerate(alone):
+            for mine, all_of in zip(one.dw + one.db, together.dw + together.db):
+                mine.copy_(all_of[g:g + 1])
+            one.optimizer.pcc_adamw_step()
+        together.optimizer.pcc_adamw_step()
+        for g, one in enumerate(alone):
+            for name in ("w", "b", "w16"):
+                for i, (a, b) in enumerate(zip(getattr(one, name), getattr(together, name))):
+                    assert torch.equal(_bits(a), _bits(b[g:g + 1])), (step, g, name, i)
+    for g in (0, 2):
+        assert all(torch.isfinite(t[g]).all() for t in together.w + together.b)
+
+
+@pytest.mark.parametrize("state_bits", [32, 8])
+def test_a_step_goes_down_its_gradient(state_bits):
+    """Trainer.step moves weights by the AdamW step of the gradients that it leaves."""
+    hyper = dict(lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01)
+    trainer = train.Trainer([synth.make_blob(1), synth.make_blob(2)], state_bits=state_bits, **hyper)
+    before = [t.cpu().numpy() for t in trainer.w + trainer.b]
+    img = synth.make_image(3, synth.ImageSpec(33, 20, 5, 4.0, 20.0))
+    d = torch.from_numpy(np.stack([img])).cuda()
+    trainer.step([d, d])
+    for i, (p, now, g) in enumerate(zip(before, trainer.w + trainer.b, trainer.dw + trainer.db)):
+        one = ref.AdamW(p.reshape(-1), 32, **hyper)         # the update uses the moments before they are rounded
+        one.step(g.cpu().numpy().reshape(-1))
+        # a quotient of at most 1 from some ten roundings on each side, times the rate; the parameter's product and difference on each side
+        tol = 2.0 ** -24 * (24 * hyper["lr"] + 4 * np.abs(one.p))
+        assert np.all(np.abs(now.cpu().numpy().reshape(-1) - one.p) <= tol), i
+        assert np.any(now.cpu().numpy() != p)
