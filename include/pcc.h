@@ -288,8 +288,9 @@ int pcc_mixture_loss(const float *d_params, size_t ldp, const uint8_t *d_rgb, co
  * scale is the block's largest magnitude / 448, codes are rounded up or down by
  * a fixed sequence of place in the block and t, in proportion to what is
  * cut off (to the nearest, a v that changes by 0.1 % a step would never
- * move); a v above 0 never gets the code of 0.  The update itself uses the
- * moments before they are rounded. */
+ * move); a v above 0 never gets the code of 0.  A moment that is not finite has
+ * the code of NaN, and the scale is that of the others.  The update itself uses
+ * the moments before they are rounded. */
 typedef struct {
     float *d_param;
     const void *d_grad;

@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t dither_bits(uint32_t i, uint32_t t) {
 
 // e4m3 code of y, 0 <= y <= 448, after `part` / 2^20 of a step: bits from the exponent on, or eighths of 2^-6 below it.
 __device__ __forceinline__ uint32_t code_of(float y, uint32_t part) {
-    if (!(y <= 1e30f)) return 0x7Fu;      // not a number: its own code
+    if (!(y <= 1e30f)) return 0x7Fu;      // not a number, or infinite: the code of NaN
     const uint32_t normal = ((__builtin_bit_cast(uint32_t, y) + part) >> 20) - (120u << 3);
     const uint32_t small = (uint32_t)(y * 512.0f + (float)part * 0x1p-20f);
     const uint32_t code = y >= 0x1p-6f ? normal : small;
@@ -197,7 +197,19 @@ struct AdamwBlock {
                 mmax = fmaxf(mmax, j < n ? fabsf(m[j]) : 0.0f);
                 rmax = fmaxf(rmax, j < n ? r[j] : 0.0f);
             }
-            const float msc = wave_max(mmax) * (1.0f / 448.0f), rsc = wave_max(rmax) * (1.0f / 448.0f);
+            mmax = wave_max(mmax);
+            rmax = wave_max(rmax);
+            if (mmax == INFINITY || rmax == INFINITY) {     // an infinite scale would make every other code of the block 0 * inf
+                mmax = rmax = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mmax = fmaxf(mmax, j < n && fabsf(m[j]) < INFINITY ? fabsf(m[j]) : 0.0f);
+                    rmax = fmaxf(rmax, j < n && r[j] < INFINITY ? r[j] : 0.0f);
+                }
+                mmax = wave_max(mmax);
+                rmax = wave_max(rmax);
+            }
+            const float msc = mmax * (1.0f / 448.0f), rsc = rmax * (1.0f / 448.0f);
             const float minv = msc >= 0x1p-100f ? 1.0f / msc : 0.0f, rinv = rsc >= 0x1p-100f ? 1.0f / rsc : 0.0f;
             uint32_t new_m = 0, new_v = 0;
 #pragma unroll

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import train_reference as ref
-from paper_2212_01185_amd import synth, train
+from paper_2212_01185_amd import binding, synth, train
 
 pytestmark = pytest.mark.gpu
 
@@ -62,3 +62,45 @@ def test_a_step_goes_down_its_gradient(state_bits):
         tol = 2.0 ** -24 * (24 * hyper["lr"] + 4 * np.abs(one.p))
         assert np.all(np.abs(now.cpu().numpy().reshape(-1) - one.p) <= tol), i
         assert np.any(now.cpu().numpy() != p)
+
+
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 3e30])
+def test_a_moment_that_is_not_finite_stays_in_its_element(grad_dtype, value):
+    """In 8 bits as in 32: the others of its block have the states and parameters that they have where its gradient is 0."""
+    if grad_dtype == torch.float16 and value == 3e30:
+        pytest.skip("no such number")
+    n, at = 1024, 300
+    gen = torch.Generator().manual_seed(7)
+    start = torch.randn(n, generator=gen).cuda()
+    values = [torch.randn(n, generator=gen).to(grad_dtype) for _ in range(4)]
+
+    def run(dirty, bits):
+        p, g = [start.clone()], [torch.zeros(n, dtype=grad_dtype, device="cuda")]
+        opt = binding.AdamW(p, g, state_bits=bits)
+        out = []
+        for k, v in enumerate(values):
+            g[0].copy_(v)
+            g[0][at] = dirty if k == 1 else 0.0
+            opt.pcc_adamw_step()
+            scales = [opt.m_scale[0].clone(), opt.v_scale[0].clone()] if bits == 8 else []
+            out.append([p[0].clone(), _bits(opt.m[0]).clone().view(n, -1), _bits(opt.v[0]).clone().view(n, -1)] + scales)
+        return out
+
+    others = torch.arange(n, device="cuda") != at
+    for bits in (32, 8):
+        clean, dirty = run(0.0, bits), run(value, bits)
+        for k, (a, b) in enumerate(zip(clean, dirty)):
+            if value == 3e30 and bits == 8:                 # the first moment is finite, and its block's scale is its own
+                a, b = [a[0][~block(at, n)], a[2], a[4]], [b[0][~block(at, n)], b[2], b[4]]
+                assert torch.equal(a[0], b[0]) and torch.equal(a[1][others], b[1][others]) and torch.equal(a[2], b[2]), (bits, k)
+                continue
+            for x, y in zip(a[:3], b[:3]):
+                assert torch.equal(x[others], y[others]), (bits, k)
+            assert all(torch.equal(x, y) for x, y in zip(a[3:], b[3:])), (bits, k)
+        assert value == 3e30 or torch.isnan(dirty[-1][0][at])
+
+
+def block(at, n):
+    i = torch.arange(n, device="cuda")
+    return i // binding.STATE_BLOCK == at // binding.STATE_BLOCK
