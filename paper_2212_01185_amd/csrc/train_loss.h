@@ -50,6 +50,8 @@ __device__ __forceinline__ float mills(float z) {
     return p * t;
 }
 
+constexpr float kFar = 0x1p40f;
+
 struct Bin {
     float q;        // probability of the level
     float d_mu;     // f(a) - f(b)
@@ -65,7 +67,8 @@ __device__ __forceinline__ float with_sign(float v, float sign) {
 template <int DIST>
 __device__ __forceinline__ Bin bin_of(float mid, float h, bool first, bool last) {
     const bool mirrored = __builtin_signbit(mid);
-    const float m = fabsf(mid), near = m - h, far = m + h;
+    // further than kFar nothing is left of the component; an infinite distance would make m (f(near) - f(far)) inf * 0 (a NaN stays one)
+    const float m = fabsf(mid) > kFar ? kFar : fabsf(mid), near = m - h, far = m + h;
     const bool open_near = mirrored ? last : first, open_far = mirrored ? first : last;
     float q, diff, sum;     // diff, sum: f(near) -+ f(far)
     if (DIST == 1) {
