@@ -301,7 +301,8 @@ typedef struct {
 } pcc_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2, eps, weight_decay;
+    double lr, beta1, beta2, eps, weight_decay; /* betas in [0, 1); eps 0 or at least 2^-126.  With 0 an element whose
+                                                   gradients were all 0 becomes 0 / 0 */
     const float *d_lr; /* device; used in place of lr if not NULL: a captured step then follows a schedule */
 } pcc_adamw_hyper;
 

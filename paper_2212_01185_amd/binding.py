@@ -383,8 +383,8 @@ class AdamW:
             raise ValueError("params, grads and copies must be lists of one length, not empty")
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
-        if not (betas[0] >= 0 and betas[0] < 1 and betas[1] >= 0 and betas[1] < 1 and eps >= 0):
-            raise ValueError("betas must be in [0, 1), eps at least 0")
+        if not (betas[0] >= 0 and betas[0] < 1 and betas[1] >= 0 and betas[1] < 1 and (eps == 0 or eps >= 2.0 ** -126)):
+            raise ValueError("betas must be in [0, 1), eps 0 or at least 2^-126")
         copies = [None] * len(params) if copies is None else list(copies)
         device = params[0].device
         state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn

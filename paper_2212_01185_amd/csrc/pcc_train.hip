@@ -393,7 +393,8 @@ void pcc_adamw_destroy(pcc_adamw* plan) {
 
 int pcc_adamw_step(pcc_adamw* plan, const pcc_adamw_hyper* h, int64_t* d_step, void* hip_stream) {
     if (!plan || !h || !d_step || !aligned(d_step, 8) || !aligned(h->d_lr, 4)) return PCC_E_ARG;
-    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0 && h->eps >= 0.0)) return PCC_E_ARG;
+    // (an eps below fp32's normal numbers has an infinite reciprocal, and a moment of 0 would make it NaN)
+    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0 && h->beta2 >= 0.0 && h->beta2 < 1.0 && (h->eps == 0.0 || h->eps >= 0x1p-126))) return PCC_E_ARG;
     DeviceGuard guard(plan->device);
     if (!guard.ok) return PCC_E_HIP;
     AdamwArgs a = {};

@@ -104,3 +104,17 @@ def test_a_moment_that_is_not_finite_stays_in_its_element(grad_dtype, value):
 def block(at, n):
     i = torch.arange(n, device="cuda")
     return i // binding.STATE_BLOCK == at // binding.STATE_BLOCK
+
+
+def test_an_eps_below_the_normal_numbers_is_refused():
+    """Its reciprocal would be infinite: an element without any gradient became NaN."""
+    p, g = [torch.ones(64, device="cuda")], [torch.zeros(64, device="cuda")]
+    opt = binding.AdamW(p, g, lr=0.5, weight_decay=0.0)
+    for eps in (1e-40, -1e-8, float("nan")):
+        opt.eps = eps
+        with pytest.raises(binding.PccError) as e:
+            opt.pcc_adamw_step()
+        assert e.value.code == binding.PCC_E_ARG
+    opt.eps = 2.0 ** -126
+    opt.pcc_adamw_step()
+    assert (p[0] == 1).all() and opt.step.item() == 1
