@@ -49,6 +49,8 @@ class Trainer:
         parsed = [parse_blob(bytes(b)) for b in blobs]
         if not parsed or any(p[1:] != parsed[0][1:] or [w.shape for w, _ in p[0]] != [w.shape for w, _ in parsed[0][0]] for p in parsed):
             raise ValueError("blobs must be one or more networks of one shape")
+        if not eps > 0:
+            raise ValueError("eps must be above 0: padded inputs and networks without pictures have moments of 0")
         self.k, self.nbhd, self.delay, self.act, self.dist = parsed[0][1:]
         self.groups, self.device = len(parsed), torch.device("cuda", device)
         self.dims = [parsed[0][0][0][0].shape[1]] + [w.shape[0] for w, _ in parsed[0][0]]
