@@ -84,11 +84,11 @@ class Trainer:
     def gradients(self, pictures) -> torch.Tensor:
         """Forward and backward pass; the gradients of each network's mean code length are left in ``dw`` and ``db``.
 
-        pictures: for every network a uint8 tensor [n, H, W, 3] or a list of them (which may be empty).  Returns the mean
+        pictures: for every network a uint8 tensor [n, H, W, 3] or a list of them (either may be empty).  Returns the mean
         bits per sub-pixel of each network's pictures, fp64 [networks] (0 for a network without any)."""
         if self.groups == 1 and isinstance(pictures, torch.Tensor):
             pictures = [pictures]
-        pictures = [[p] if isinstance(p, torch.Tensor) else list(p) for p in pictures]
+        pictures = [[p for p in ([own] if isinstance(own, torch.Tensor) else own) if p.numel()] for own in pictures]
         if len(pictures) != self.groups or not any(pictures):
             raise ValueError("pictures must be given for each network, and some for one of them")
         lengths = [sum(int(p.shape[0] * p.shape[1] * p.shape[2]) for p in own) for own in pictures]

@@ -118,3 +118,15 @@ def test_an_eps_below_the_normal_numbers_is_refused():
     opt.eps = 2.0 ** -126
     opt.pcc_adamw_step()
     assert (p[0] == 1).all() and opt.step.item() == 1
+
+
+def test_pictures_without_pixels():
+    """Tensors of no pictures count as none, and every network's being one is refused as no pictures are."""
+    trainer = train.Trainer([synth.make_blob(1), synth.make_blob(2)])
+    d = torch.randint(0, 256, (2, 9, 7, 3), dtype=torch.uint8, device="cuda")
+    want = trainer.gradients([d, []]).clone()
+    dw = [t.clone() for t in trainer.dw]
+    got = trainer.gradients([[d[:0], d], d[:0]])
+    assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(dw, trainer.dw))
+    with pytest.raises(ValueError, match="pictures"):
+        trainer.gradients([d[:0], [d[:, :0]]])
