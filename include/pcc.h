@@ -309,9 +309,9 @@ typedef struct {
 typedef struct pcc_adamw pcc_adamw;
 
 /* Lay out the list of tensors (host array, copied) on device `hip_device`.  The
- * tensors stay the caller's and must outlive the plan; what a step writes must not
- * overlap (PCC_E_ARG).  Allocates device memory
- * and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
+ * tensors stay the caller's, where they are, and must outlive the plan; what a step
+ * writes must not overlap, nor a gradient with it (PCC_E_ARG; an fp32 gradient may be
+ * its own parameter).  Allocates device memory and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
  * PCC_BF16 or PCC_FP16; state_bits 32 or 8. */
 int pcc_adamw_create(pcc_adamw **out, const pcc_adamw_tensor *h_tensors, int count, int grad_type, int copy_type,
                      int state_bits, int hip_device);

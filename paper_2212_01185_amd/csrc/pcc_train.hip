@@ -1,5 +1,6 @@
 // Host side of the training operators of include/pcc.h.
 #include <algorithm>
+#include <iterator>
 #include <new>
 #include <utility>
 #include <vector>
@@ -351,6 +352,14 @@ int pcc_adamw_create(pcc_adamw** out, const pcc_adamw_tensor* h_tensors, int cou
         std::sort(written.begin(), written.end());
         for (size_t i = 1; i < written.size(); ++i)
             if (written[i].first < written[i - 1].second) return PCC_E_ARG;
+        // nor may a gradient lie where a step writes, but for its own parameter's place, element by element
+        for (int i = 0; i < count; ++i) {
+            const pcc_adamw_tensor& s = h_tensors[i];
+            if (s.n == 0 || (grad_type == PCC_FP32 && s.d_grad == s.d_param)) continue;
+            const uintptr_t lo = (uintptr_t)s.d_grad, hi = lo + s.n * size_of(grad_type);
+            const auto next = std::lower_bound(written.begin(), written.end(), std::make_pair(hi, (uintptr_t)0));  // the first that begins behind it
+            if (next != written.begin() && std::prev(next)->second > lo) return PCC_E_ARG;
+        }
     } catch (const std::bad_alloc&) {
         return PCC_E_INTERNAL;
     }

@@ -130,3 +130,22 @@ def test_pictures_without_pixels():
     assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(dw, trainer.dw))
     with pytest.raises(ValueError, match="pictures"):
         trainer.gradients([d[:0], [d[:, :0]]])
+
+
+def test_gradients_that_touch_or_share_memory():
+    """Gradients right beside what is written, one gradient of two parameters, and a gradient that is its parameter."""
+    space = torch.randn(600, device="cuda")
+    p, q, g = space[:200], space[400:], space[200:400]
+    start = [t.clone() for t in (p, q, g)]
+    binding.AdamW([p, q], [g, g]).pcc_adamw_step()
+    for t, before in ((p, start[0]), (q, start[1])):
+        alone = before.clone()
+        binding.AdamW([alone], [start[2].clone()]).pcc_adamw_step()
+        assert torch.equal(t, alone)
+    assert torch.equal(g, start[2])
+    own, apart = start[0].clone(), start[0].clone()
+    binding.AdamW([own], [own]).pcc_adamw_step()
+    binding.AdamW([apart], [start[0].clone()]).pcc_adamw_step()
+    assert torch.equal(own, apart)
+    with pytest.raises(binding.PccError):
+        binding.AdamW([p, q], [g, p])
