@@ -135,7 +135,7 @@ int launch_narrow_forward(Grouped& a, hipStream_t st) {
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
     const size_t weights = narrow_forward_lds(a.in, a.out), rows = narrow_rows_lds(a.out, a.y32);
     const int threads = kNarrowThreads;
-    a.staged = even_rows(a.y, a.ldy * (a.y32 ? 2 : 1)) && weights + threads / 64 * rows <= kMaxLds && narrow_row_pieces(a.out, a.y32) <= 64;
+    a.staged = even_rows(a.y, a.ldy * (a.y32 ? 2 : 1)) && weights + threads / 64 * rows <= kMaxLds && narrow_row_pieces(a.out, a.y32) <= kMaxRowPieces;
     const size_t lds = weights + (a.staged ? threads / 64 * rows : 0);
     auto go = [&](auto kernel) {
         if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }

@@ -26,12 +26,24 @@ __host__ __device__ constexpr size_t narrow_forward_lds(int in, int out) {
 __host__ __device__ constexpr int narrow_row_pieces(int features, int y32) { return (features * (y32 ? 4 : 2) + 15) / 16; }
 __host__ __device__ constexpr size_t narrow_rows_lds(int features, int y32) { return (size_t)kNarrowRowsWave * (narrow_row_pieces(features, y32) + 1) * 16; }
 
+// The row of a wave's piece, id / pieces, by a product: exact for all rows of up to 50 pieces (with 51, piece 1,325 would be the one before
+// row 26's first).
+constexpr int kMaxRowPieces = 50;
+__host__ __device__ constexpr uint32_t pieces_inverse(int pieces) { return (65536 + pieces - 1) / pieces; }
+__host__ __device__ constexpr int row_of_piece(int id, uint32_t inverse) { return (int)((uint32_t)id * inverse >> 16); }
+constexpr bool rows_of_pieces_are_exact(int pieces) {
+    for (int id = 0; id < kNarrowRowsWave * pieces; ++id)
+        if (row_of_piece(id, pieces_inverse(pieces)) != id / pieces) return false;
+    return pieces == 1 || rows_of_pieces_are_exact(pieces - 1);
+}
+static_assert(rows_of_pieces_are_exact(kMaxRowPieces), "rows of pieces");
+
 // Rows in LDS (of one wave) to memory, 16 bytes a lane, neighbours next to each other.
 __device__ __forceinline__ void store_rows(const uint8_t* lds, uint8_t* to, size_t ld_bytes, int rows, int row_bytes) {
     const int pieces = (row_bytes + 15) / 16, lane = threadIdx.x & 63;
-    const uint32_t inverse = (65536 + pieces - 1) / pieces;         // exact for pieces of up to 2,048 numbers
+    const uint32_t inverse = pieces_inverse(pieces);
     for (int id = lane; id < rows * pieces; id += 64) {
-        const int r = (int)((uint32_t)id * inverse >> 16), c = id - r * pieces, left = row_bytes - 16 * c;
+        const int r = row_of_piece(id, inverse), c = id - r * pieces, left = row_bytes - 16 * c;
         const uint8_t* from = lds + (r * (pieces + 1) + c) * 16;
         uint8_t* at = to + (size_t)r * ld_bytes + 16 * c;
         if (left >= 16) { u32x4 v = *reinterpret_cast<const u32x4*>(from);
