@@ -166,7 +166,6 @@ uint64_t backward_chunks(Grouped& a) {
 template <class T>
 int launch_narrow_backward(Grouped& a, hipStream_t st) {
     const uint64_t blocks = backward_chunks(a);
-    a.wide_out = 1;
     a.wide_dw = aligned(a.dw, 16) && (size_t)a.in * a.out % 4 == 0;
     if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);

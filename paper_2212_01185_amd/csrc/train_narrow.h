@@ -322,8 +322,7 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_backward_kernel
 #pragma unroll
                     for (int e = 0; e < 4; ++e) { o[e] = to16<T>(d0[e]); o[4 + e] = to16<T>(d1[e]); }
                     u16* to = static_cast<u16*>(a.y) + (size_t)(ch.lo + r0 + my_row) * a.ldy + f;
-                    if (a.wide_out) __builtin_memcpy(to, &o, 16);
-                    else for (int e = 0; e < 8; ++e) to[e] = o[e];
+                    __builtin_memcpy(to, &o, 16);       // inputs are a multiple of eight, in rows that begin at even elements
                 }
             }
         }
