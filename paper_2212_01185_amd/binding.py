@@ -241,6 +241,7 @@ class Codec:
 
 # ---- The operators of a training step ----
 # Free functions: they launch on the current stream of their tensors' device.  Rows of tensors may be views with a longer stride.
+# Autograd does not record them: tensors that require gradients are refused unless it is off.
 
 _TYPES = {torch.bfloat16: PCC_BF16, torch.float16: PCC_FP16, torch.float32: PCC_FP32}
 
@@ -275,6 +276,12 @@ def _call(what: str, device, *args) -> None:
         raise PccError(rc, what)
 
 
+def _unrecorded(*tensors) -> None:
+    """Refuses tensors whose gradients autograd is asked for: the operators' backward passes are calls of their own."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
+        raise ValueError("autograd does not record these operators: call them under torch.no_grad() or on detached tensors")
+
+
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
@@ -307,6 +314,7 @@ def pcc_grouped_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | No
     """act(x_i w_g^T + bias_g) for rows offsets[g] <= i < offsets[g + 1] of each group g.  x [rows, in] and w [groups, out, in]
     bf16 or fp16, bias [groups, out] fp32, offsets [groups + 1] int64; the result has x's type or fp32.  Rows of no group are left
     as they are in `out`, and undefined in a new tensor."""
+    _unrecorded(x, w, bias, out)
     ldx, groups, n_out = _check_groups(x, w, offsets)
     if bias is not None:
         _check("bias", bias, (torch.float32,), (groups, n_out), x.device)
@@ -324,6 +332,7 @@ def pcc_grouped_linear_grad(dz: torch.Tensor, x: torch.Tensor, w: torch.Tensor, 
     """(dx, dw, db) of pcc_grouped_linear.  dz [rows, out] is the gradient before the layer's activation; x_act the activation that
     made x: dx is the gradient before that one, the dz of the layer in front (None without want_dx).  dw [groups, out, in] and
     db [groups, out] are fp32.  Rows of no group are left as they are in `dx`, and undefined in a new tensor."""
+    _unrecorded(dz, x, w, dx, dw, db)
     ldx, groups, n_out = _check_groups(x, w, offsets)
     rows, n_in = int(x.shape[0]), int(x.shape[1])
     lddz = _check("dz", dz, (x.dtype,), (rows, n_out), x.device, rows=True)
@@ -349,6 +358,7 @@ def pcc_mixture_loss(params: torch.Tensor, rgb: torch.Tensor, dist: int = 0, sca
                      want_grad: bool = True, grad_dtype: torch.dtype = torch.float32, grad: torch.Tensor | None = None):
     """(bits [count], gradient [count, 12 K]) of pixels rgb uint8 [count, 3] under head outputs params fp32 [count, 12 K]: the code
     length of Eq. (5) with the coder's one count for every level, and scale * weight times its gradient.  Pixels of weight 0 have 0."""
+    _unrecorded(params, weight, grad)
     ldp = _check("params", params, (torch.float32,), (None, None), rows=True)
     count, outputs = int(params.shape[0]), int(params.shape[1])
     _check("rgb", rgb, (torch.uint8,), (count, 3), params.device)

@@ -149,3 +149,17 @@ def test_gradients_that_touch_or_share_memory():
     assert torch.equal(own, apart)
     with pytest.raises(binding.PccError):
         binding.AdamW([p, q], [g, p])
+
+
+def test_parameters_of_a_module_without_autograd():
+    """What requires gradients is taken where autograd is off, and always by the optimizer, which writes in place."""
+    x, off = torch.randn(5, 8, device="cuda").bfloat16(), torch.tensor([0, 5], device="cuda")
+    w = torch.nn.Parameter(torch.randn(1, 3, 8, device="cuda"))
+    w16 = torch.nn.Parameter(w.detach().bfloat16())
+    with torch.no_grad():
+        y = binding.pcc_grouped_linear(x, w16, None, off)
+        _, dw, _ = binding.pcc_grouped_linear_grad(y, x, w16, off, want_dx=False)
+    assert torch.equal(y, binding.pcc_grouped_linear(x, w16.detach(), None, off))
+    before = w.detach().clone()
+    binding.AdamW([w], [dw]).pcc_adamw_step()
+    assert not torch.equal(before, w.detach())

@@ -31,3 +31,25 @@ def test_adamw_refuses_a_gradient_where_it_writes(grad_type, grad):
     t[1] = binding._AdamwTensor(PARAM + 0x1000, GRAD, None, M + 0x1000, V + 0x1000, None, None, 100)
     h = C.c_void_p()
     assert binding.load().pcc_adamw_create(C.byref(h), t, 2, grad_type, 0, 32, 0) == binding.PCC_E_ARG
+
+
+def test_operators_that_autograd_does_not_record_refuse_its_tensors():
+    """A result without a graph would drop the gradients of everything before it, and say nothing."""
+    t = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    asks = lambda x: x.requires_grad_(True)  # noqa: E731
+    off, f = torch.tensor([0, 4]), torch.zeros(4, 60)
+    rgb = torch.zeros(4, 3, dtype=torch.uint8)
+    calls = (lambda: binding.pcc_grouped_linear(asks(t(4, 8)), t(1, 3, 8), None, off),
+             lambda: binding.pcc_grouped_linear(t(4, 8), asks(t(1, 3, 8)), None, off),
+             lambda: binding.pcc_grouped_linear(t(4, 8), t(1, 3, 8), asks(torch.zeros(1, 3)), off),
+             lambda: binding.pcc_grouped_linear(t(4, 8), t(1, 3, 8), None, off, out=asks(t(4, 3))),
+             lambda: binding.pcc_grouped_linear_grad(asks(t(4, 3)), t(4, 8), t(1, 3, 8), off),
+             lambda: binding.pcc_grouped_linear_grad(t(4, 3), asks(t(4, 8)), t(1, 3, 8), off),
+             lambda: binding.pcc_grouped_linear_grad(t(4, 3), t(4, 8), asks(t(1, 3, 8)), off),
+             lambda: binding.pcc_mixture_loss(asks(f.clone()), rgb),
+             lambda: binding.pcc_mixture_loss(f, rgb, weight=asks(torch.ones(4))))
+    for call in calls:
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):        # off: the next check, that tensors are on a GPU
+            call()
