@@ -213,8 +213,9 @@ int pcc_last_timings(pcc_ctx *ctx, float *h_ms);
  * asynchronous, allocate nothing, keep nothing, use no memory but their
  * arguments and may be captured into a HIP graph.  Types are PCC_BF16,
  * PCC_FP16 and PCC_FP32.  ld... is the distance between rows in elements, at
- * least the row's length and at most 2^22.  Outputs must not overlap inputs.
- * Without any rows the pointers to rows may be NULL. */
+ * least the row's length and at most 2^22.  Outputs must not overlap inputs or
+ * each other (PCC_E_ARG; rows at one distance may lie beside each other, as columns
+ * of one buffer).  Without any rows the pointers to rows may be NULL. */
 
 #define PCC_BF16 0
 #define PCC_FP16 1

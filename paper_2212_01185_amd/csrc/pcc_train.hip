@@ -1,5 +1,6 @@
 // Host side of the training operators of include/pcc.h.
 #include <algorithm>
+#include <initializer_list>
 #include <iterator>
 #include <new>
 #include <utility>
@@ -39,6 +40,25 @@ constexpr size_t kMaxRows = (size_t)1 << 40;
 
 bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 size_t size_of(int type) { return type == PCC_FP32 ? 4 : 2; }
+
+// `count` rows of `length` bytes, `pitch` apart; what is one piece is one row.
+struct Span {
+    const void* p;
+    size_t count, pitch, length;
+};
+Span piece(const void* p, size_t bytes) { return {p, 1, bytes, bytes}; }
+// Whether they share bytes.  Rows at one distance may lie beside each other (columns of one buffer).
+bool overlap(const Span& a, const Span& b) {
+    if (!a.p || !b.p || !a.count || !b.count || !a.length || !b.length) return false;
+    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+    if (a0 + (a.count - 1) * a.pitch + a.length <= b0 || b0 + (b.count - 1) * b.pitch + b.length <= a0) return false;
+    if (a.pitch != b.pitch || a.count == 1 || b.count == 1) return true;
+    const size_t apart = a0 <= b0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;    // of b's row from a's in front of it
+    return apart < a.length || a.pitch - apart < b.length;
+}
+bool overlap(const Span& a, std::initializer_list<Span> others) {
+    return std::any_of(others.begin(), others.end(), [&](const Span& b) { return overlap(a, b); });
+}
 
 // ---------------------------------------------------------------------------
 // Grouped products.
@@ -213,6 +233,7 @@ int pcc_contexts(const uint8_t* d_img, int n, int H, int W, int nbhd, int delay,
     if (width < 3 * nbhd || width > PCC_MAX_FEATURES || !ld_ok(ldx, width) || !aligned(d_x, 2)) return PCC_E_ARG;
     const uint64_t blocks = (pixels + kContextThreads - 1) / kContextThreads;
     if (pixels > kMaxRows || blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (overlap({d_x, pixels, ldx * 2, (size_t)width * 2}, piece(d_img, pixels * 3))) return PCC_E_ARG;
     const int wide = aligned(d_x, 4) && ldx % 2 == 0 && width % 8 == 0 && width <= kContextWidth;
     auto go = [&](auto kernel) {
         return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(kContextThreads), 0, (hipStream_t)hip_stream, d_img, pixels, H, W, (u16*)d_x, width, ldx, wide); });
@@ -226,6 +247,9 @@ int pcc_grouped_linear(const void* d_x, size_t ldx, const void* d_w, const float
     if ((type != PCC_BF16 && type != PCC_FP16) || (y_type != type && y_type != PCC_FP32) || act < PCC_ACT_RELU || act > PCC_ACT_NONE) return PCC_E_ARG;
     if (!aligned(d_x, 2) || !aligned(d_w, 2) || !aligned(d_bias, 4) || !aligned(d_offsets, 8) || !aligned(d_y, size_of(y_type))) return PCC_E_ARG;
     if (rows == 0) return PCC_OK;
+    const size_t weights = (size_t)groups * in * out, outputs = (size_t)groups * out;
+    if (overlap({d_y, rows, ldy * size_of(y_type), out * size_of(y_type)},
+                {{d_x, rows, ldx * 2, (size_t)in * 2}, piece(d_w, weights * 2), piece(d_bias, outputs * 4), piece(d_offsets, (size_t)(groups + 1) * 8)})) return PCC_E_ARG;
     Grouped a = {};
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.bias = d_bias; a.off = d_offsets; a.y = d_y;
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.in = in; a.out = out; a.act = act;
@@ -260,6 +284,12 @@ int pcc_grouped_linear_grad(const void* d_dz, size_t lddz, const void* d_x, size
     const size_t need = d_dw ? pcc_grouped_linear_grad_workspace_bytes(rows, groups, in, out) : 0;
     if (need && (!d_workspace || workspace_bytes < need)) return PCC_E_SCRATCH;
     if (need && !aligned(d_workspace, 16)) return PCC_E_ARG;
+    const size_t weights = (size_t)groups * in * out, outputs = (size_t)groups * out;
+    const Span dz = {d_dz, rows, lddz * 2, (size_t)out * 2}, x = {d_x, rows, ldx * 2, (size_t)in * 2}, w = piece(d_w, weights * 2),
+               offsets = piece(d_offsets, (size_t)(groups + 1) * 8), dx = {d_dx, rows, lddx * 2, (size_t)in * 2}, dw = piece(d_dw, weights * 4),
+               db = piece(d_db, outputs * 4), space = piece(d_workspace, need);
+    if (overlap(dx, {dz, x, w, offsets, dw, db, space}) || overlap(dw, {dz, x, w, offsets, db, space}) || overlap(db, {dz, x, w, offsets, space}) ||
+        overlap(space, {dz, x, w, offsets})) return PCC_E_ARG;
     hipStream_t st = (hipStream_t)hip_stream;
     Grouped a = {};
     a.x = (const u16*)d_x; a.w = (const u16*)d_w; a.dz = (const u16*)d_dz; a.off = d_offsets; a.y = d_dx; a.dw = d_dw; a.db = d_db;
@@ -292,6 +322,11 @@ int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, co
     if (!ld_ok(ldp, 12 * K) || (d_grad && (!ld_ok(ldg, 12 * K) || grad_type < PCC_BF16 || grad_type > PCC_FP32))) return PCC_E_ARG;
     if (!aligned(d_params, 4) || !aligned(d_weight, 4) || !aligned(d_bits, 4) || (d_grad && !aligned(d_grad, size_of(grad_type)))) return PCC_E_ARG;
     if (count == 0) return PCC_OK;
+    const size_t length = (size_t)12 * K;
+    const Span params = {d_params, count, ldp * 4, length * 4}, rgb = piece(d_rgb, count * 3), weight = piece(d_weight, count * 4), bits = piece(d_bits, count * 4),
+               grad = {d_grad, count, ldg * size_of(grad_type), length * size_of(grad_type)};
+    const bool in_place = d_grad == d_params && grad_type == PCC_FP32 && ldg == ldp;
+    if (overlap(bits, {params, rgb, weight, grad}) || overlap(grad, {rgb, weight}) || (!in_place && overlap(grad, params))) return PCC_E_ARG;
     const size_t blocks = (count + 64 * kLossWaves - 1) / (64 * kLossWaves), lds = (size_t)kLossWaves * 64 * 12 * K * sizeof(float);
     if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
     auto go = [&](auto kernel) {

@@ -163,3 +163,35 @@ def test_parameters_of_a_module_without_autograd():
     before = w.detach().clone()
     binding.AdamW([w], [dw]).pcc_adamw_step()
     assert not torch.equal(before, w.detach())
+
+
+def test_outputs_beside_their_inputs_in_one_buffer():
+    """Columns of one buffer, and rows that end where others begin, are no overlap."""
+    rows, off = 70, torch.tensor([0, 70], device="cuda")
+    gen = torch.Generator().manual_seed(4)
+    x0, w = torch.randn(rows, 32, generator=gen).bfloat16().cuda(), torch.randn(1, 16, 32, generator=gen).bfloat16().cuda()
+    dz0, bias = torch.randn(rows, 16, generator=gen).bfloat16().cuda(), torch.zeros(1, 16, device="cuda")
+    want = binding.pcc_grouped_linear(x0, w, bias, off)
+    dx0, dw0, db0 = binding.pcc_grouped_linear_grad(dz0, x0, w, off)
+    for first in (0, 16):                            # y in front of x, and behind it
+        buffer = torch.zeros(rows, 48, device="cuda", dtype=torch.bfloat16)
+        x, y = buffer[:, 16 - first:48 - first], buffer[:, 32:] if first else buffer[:, :16]
+        x.copy_(x0)
+        binding.pcc_grouped_linear(x, w, bias, off, out=y)
+        assert torch.equal(y, want) and torch.equal(x, x0)
+    buffer = torch.zeros(rows, 80, device="cuda", dtype=torch.bfloat16)
+    dz, x, dx = buffer[:, :16], buffer[:, 16:48], buffer[:, 48:]
+    dz.copy_(dz0)
+    x.copy_(x0)
+    _, dw, db = binding.pcc_grouped_linear_grad(dz, x, w, off, dx=dx)
+    assert torch.equal(dx, dx0) and torch.equal(dw, dw0) and torch.equal(db, db0) and torch.equal(x, x0) and torch.equal(dz, dz0)
+    line = torch.zeros(rows * 48, device="cuda", dtype=torch.bfloat16)
+    x, y = line[:rows * 32].view(rows, 32), line[rows * 32:].view(rows, 16)
+    x.copy_(x0)
+    binding.pcc_grouped_linear(x, w, bias, off, out=y)
+    assert torch.equal(y, want)
+    params = torch.randn(rows, 120, generator=gen).cuda()
+    rgb = torch.randint(0, 256, (rows, 3), generator=gen).to(torch.uint8).cuda()
+    apart = binding.pcc_mixture_loss(params[:, :60].contiguous(), rgb)
+    bits, grad = binding.pcc_mixture_loss(params[:, :60], rgb, grad=params[:, 60:])
+    assert torch.equal(bits, apart[0]) and torch.equal(grad, apart[1])

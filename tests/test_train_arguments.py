@@ -53,3 +53,49 @@ def test_operators_that_autograd_does_not_record_refuse_its_tensors():
             call()
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):        # off: the next check, that tensors are on a GPU
             call()
+
+
+def _refused(name, defaults, **changes):
+    args = dict(defaults)
+    assert set(changes) <= set(args)
+    args.update(changes)
+    return getattr(binding.load(), name)(*args.values()) == binding.PCC_E_ARG
+
+
+A, B, D, E, F, G, H = (0x100000 * i for i in range(1, 8))
+CONTEXTS = dict(img=A, n=2, H=16, W=8, nbhd=10, delay=2, x=B, width=32, ldx=32, stream=None)
+LINEAR = dict(x=A, ldx=32, w=B, bias=D, off=E, groups=2, rows=100, fan_in=32, fan_out=16, type=0, act=0, y=F, y_type=0, ldy=16, stream=None)
+BACKWARD = dict(dz=A, lddz=16, x=B, ldx=32, w=D, off=E, groups=2, rows=100, fan_in=32, fan_out=16, type=0, x_act=0, dx=F, lddx=32, dw=G, db=H,
+                workspace=0x900000, workspace_bytes=1 << 20, stream=None)
+LOSS = dict(params=A, ldp=60, rgb=B, weight=D, count=100, K=5, dist=0, scale=1.0, bits=E, grad=F, grad_type=2, ldg=60, stream=None)
+
+
+@pytest.mark.parametrize("name,defaults,changes", [
+    ("pcc_contexts", CONTEXTS, dict(x=A)), ("pcc_contexts", CONTEXTS, dict(x=A + 3 * 256 - 2)), ("pcc_contexts", CONTEXTS, dict(x=A - 2 * 32 * 256 + 2)),
+    ("pcc_grouped_linear", LINEAR, dict(y=A)), ("pcc_grouped_linear", LINEAR, dict(y=A + 2 * 3199)), ("pcc_grouped_linear", LINEAR, dict(y=B + 2046)),
+    ("pcc_grouped_linear", LINEAR, dict(y=D + 126)), ("pcc_grouped_linear", LINEAR, dict(y=E + 22)), ("pcc_grouped_linear", LINEAR, dict(y=A - 3198)),
+    ("pcc_grouped_linear", LINEAR, dict(y=A - 6396, y_type=2)),
+    # columns of one buffer that run into each other: to the right, and into the next row
+    ("pcc_grouped_linear", LINEAR, dict(ldx=48, ldy=48, y=A + 62)), ("pcc_grouped_linear", LINEAR, dict(ldx=47, ldy=47, y=A + 64)),
+    ("pcc_grouped_linear", LINEAR, dict(ldx=47, ldy=47, y=A - 30)), ("pcc_grouped_linear", LINEAR, dict(ldx=48, ldy=49, y=A + 64)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(dx=A)), ("pcc_grouped_linear_grad", BACKWARD, dict(dx=B)), ("pcc_grouped_linear_grad", BACKWARD, dict(dx=D)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(dx=E)), ("pcc_grouped_linear_grad", BACKWARD, dict(dx=G)), ("pcc_grouped_linear_grad", BACKWARD, dict(dx=H)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(dw=A)), ("pcc_grouped_linear_grad", BACKWARD, dict(dw=B)), ("pcc_grouped_linear_grad", BACKWARD, dict(dw=D)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(dw=E)), ("pcc_grouped_linear_grad", BACKWARD, dict(db=A)), ("pcc_grouped_linear_grad", BACKWARD, dict(db=B)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(db=D)), ("pcc_grouped_linear_grad", BACKWARD, dict(db=E)), ("pcc_grouped_linear_grad", BACKWARD, dict(db=G + 4092)),
+    ("pcc_mixture_loss", LOSS, dict(grad=A + 4)), ("pcc_mixture_loss", LOSS, dict(grad=A, ldg=61)), ("pcc_mixture_loss", LOSS, dict(grad=A, grad_type=0)),
+    ("pcc_mixture_loss", LOSS, dict(grad=B)), ("pcc_mixture_loss", LOSS, dict(grad=D)), ("pcc_mixture_loss", LOSS, dict(bits=A)),
+    ("pcc_mixture_loss", LOSS, dict(bits=B)), ("pcc_mixture_loss", LOSS, dict(bits=D)), ("pcc_mixture_loss", LOSS, dict(bits=F)),
+    ("pcc_mixture_loss", LOSS, dict(ldp=120, ldg=120, grad=A + 236))])
+def test_outputs_that_overlap_are_refused(name, defaults, changes):
+    """What is written first would be read, or written over."""
+    assert _refused(name, defaults, **changes)
+
+
+@pytest.mark.parametrize("space", [A, B, D, E, F, G, H])
+def test_a_workspace_that_overlaps_is_refused(space):
+    rows, far = 40000, 0x10000000
+    need = binding.load().pcc_grouped_linear_grad_workspace_bytes(rows, 2, 32, 16)
+    assert 0 < need < far
+    args = {k: v * 0x100 if v in (A, B, D, E, F, G, H) else v for k, v in BACKWARD.items()}
+    assert _refused("pcc_grouped_linear_grad", args, rows=rows, workspace=space * 0x100 - need + 16, workspace_bytes=need)
