@@ -215,7 +215,8 @@ int pcc_last_timings(pcc_ctx *ctx, float *h_ms);
  * PCC_FP16 and PCC_FP32.  ld... is the distance between rows in elements, at
  * least the row's length and at most 2^22.  Outputs must not overlap inputs or
  * each other (PCC_E_ARG; rows at one distance may lie beside each other, as columns
- * of one buffer).  Without any rows the pointers to rows may be NULL. */
+ * of one buffer).  Without any rows the pointers to rows may be NULL.  A call that
+ * would take 2^32 threads or more (products of some 2^31 rows) is PCC_E_ARG. */
 
 #define PCC_BF16 0
 #define PCC_FP16 1

@@ -38,6 +38,9 @@ struct DeviceGuard {
 constexpr size_t kMaxLd = (size_t)1 << 22;
 constexpr size_t kMaxRows = (size_t)1 << 40;
 
+// A launch has fewer than 2^32 threads (some grids are rounded up to a multiple of eight workgroups).
+bool launchable(uint64_t blocks, int threads) { return blocks < ((uint64_t)1 << 32) / threads - 8; }
+
 bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 size_t size_of(int type) { return type == PCC_FP32 ? 4 : 2; }
 
@@ -98,7 +101,7 @@ int launch_tiles_of(Grouped& a, hipStream_t st) {
     a.tiles_n = (uint32_t)((a.out + TILE - 1) / TILE);
     a.mult = 1;
     const uint64_t chunks = ((uint64_t)a.rows >> a.log2) + a.groups, blocks = chunks * a.tiles_m * (MODE == kWeights ? a.tiles_n : 1);
-    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (!launchable(blocks, tile_threads(TILE))) return PCC_E_ARG;
     const bool wide = (MODE == kBackward || even_rows(a.x, a.ldx)) && (MODE == kForward || even_rows(a.dz, a.lddz)) &&
                       (MODE == kWeights || even_rows(a.w, (size_t)a.in));
     a.wide_x = aligned(a.x, 8) && a.ldx % 4 == 0;
@@ -151,7 +154,7 @@ int launch_narrow_forward(Grouped& a, hipStream_t st) {
     chunk_rows(a, 256, 5);
     a.wide_out = aligned(a.y, 16) && a.ldy % (a.y32 ? 4 : 8) == 0;
     const uint64_t blocks = chunk_count(a);
-    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (!launchable(blocks, kNarrowThreads)) return PCC_E_ARG;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
     const size_t weights = narrow_forward_lds(a.in, a.out), rows = narrow_rows_lds(a.out, a.y32);
     const int threads = kNarrowThreads;
@@ -187,7 +190,7 @@ template <class T>
 int launch_narrow_backward(Grouped& a, hipStream_t st) {
     const uint64_t blocks = backward_chunks(a);
     a.wide_dw = aligned(a.dw, 16) && (size_t)a.in * a.out % 4 == 0;
-    if (blocks + 8 > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (!launchable(blocks, kNarrowThreads)) return PCC_E_ARG;
     const uint32_t grid = (uint32_t)((blocks + 7) / 8 * 8);
     auto go = [&](auto kernel, size_t lds) {
         if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
@@ -232,7 +235,7 @@ int pcc_contexts(const uint8_t* d_img, int n, int H, int W, int nbhd, int delay,
     if (!((nbhd == 10 && delay == 2) || (nbhd == 12 && (delay == 3 || delay == 1)))) return PCC_E_ARG;
     if (width < 3 * nbhd || width > PCC_MAX_FEATURES || !ld_ok(ldx, width) || !aligned(d_x, 2)) return PCC_E_ARG;
     const uint64_t blocks = (pixels + kContextThreads - 1) / kContextThreads;
-    if (pixels > kMaxRows || blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (pixels > kMaxRows || !launchable(blocks, kContextThreads)) return PCC_E_ARG;
     if (overlap({d_x, pixels, ldx * 2, (size_t)width * 2}, piece(d_img, pixels * 3))) return PCC_E_ARG;
     const int wide = aligned(d_x, 4) && ldx % 2 == 0 && width % 8 == 0 && width <= kContextWidth;
     auto go = [&](auto kernel) {
@@ -328,7 +331,7 @@ int pcc_mixture_loss(const float* d_params, size_t ldp, const uint8_t* d_rgb, co
     const bool in_place = d_grad == d_params && grad_type == PCC_FP32 && ldg == ldp;
     if (overlap(bits, {params, rgb, weight, grad}) || overlap(grad, {rgb, weight}) || (!in_place && overlap(grad, params))) return PCC_E_ARG;
     const size_t blocks = (count + 64 * kLossWaves - 1) / (64 * kLossWaves), lds = (size_t)kLossWaves * 64 * 12 * K * sizeof(float);
-    if (blocks > 0x7FFFFFFFull) return PCC_E_ARG;
+    if (!launchable(blocks, 64 * kLossWaves)) return PCC_E_ARG;
     auto go = [&](auto kernel) {
         if (!allow_lds(kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
         return launch([&] {

@@ -99,3 +99,11 @@ def test_a_workspace_that_overlaps_is_refused(space):
     assert 0 < need < far
     args = {k: v * 0x100 if v in (A, B, D, E, F, G, H) else v for k, v in BACKWARD.items()}
     assert _refused("pcc_grouped_linear_grad", args, rows=rows, workspace=space * 0x100 - need + 16, workspace_bytes=need)
+
+
+@pytest.mark.parametrize("name,defaults,changes", [
+    ("pcc_contexts", CONTEXTS, dict(n=3, H=1 << 15, W=1 << 16, x=1 << 40)), ("pcc_grouped_linear", LINEAR, dict(rows=1 << 32, fan_in=7, fan_out=5, y=1 << 60)),
+    ("pcc_grouped_linear_grad", BACKWARD, dict(rows=1 << 32, fan_in=7, fan_out=5, dz=1 << 50, x=1 << 52, dx=1 << 54, workspace=1 << 56, workspace_bytes=1 << 40)),
+    ("pcc_mixture_loss", LOSS, dict(count=1 << 33, params=1 << 50, rgb=1 << 52, weight=1 << 53, bits=1 << 54, grad=1 << 56))])
+def test_more_threads_than_a_launch_has_are_refused(name, defaults, changes):
+    assert _refused(name, defaults, **changes)
