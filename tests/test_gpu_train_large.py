@@ -1,0 +1,118 @@
+"""Paths of the training operators that only large calls take.  Needs an MI355X."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import train_reference as ref
+from paper_2212_01185_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+# ---------------------------------------------------------------------------------------------------- products in tiles of 256
+
+def _view(t, before, behind):
+    """t on the GPU as columns of a wider buffer of NaN."""
+    full = torch.full((t.shape[0], before + t.shape[1] + behind), float("nan"), dtype=t.dtype)
+    full[:, before:before + t.shape[1]] = t
+    return full.cuda()[:, before:before + t.shape[1]]
+
+
+# Rows of x begin at even elements (with whole chunks of eight, and with one cut by the row's end) or at odd ones; those of the result in
+# whole pieces or not.  Groups of 9,000 and 8,000 rows with an empty one between, and rows of no group behind: 512 rows a group and
+# 256 tiles at least are what the launch wants.
+@pytest.mark.parametrize("fan_in,fan_out,dtype,out_dtype,x_pad,y_pad,act,with_bias", [
+    (256, 1030, BF16, BF16, (0, 0), (0, 2), ref.RELU, True), (250, 1030, FP16, FP32, (0, 0), (0, 0), ref.LEAKY, True),
+    (250, 1030, BF16, BF16, (2, 4), (4, 2), ref.NONE, False), (250, 1032, FP16, FP16, (0, 0), (1, 2), ref.RELU, True),
+    (263, 1030, FP16, FP32, (0, 0), (0, 2), ref.NONE, True), (264, 1030, BF16, FP32, (1, 0), (0, 0), ref.LEAKY, True),
+    (63, 1031, BF16, BF16, (0, 1), (0, 0), ref.RELU, False), (1000, 900, FP16, FP16, (0, 8), (0, 0), ref.RELU, True)])
+def test_forward_in_large_tiles(fan_in, fan_out, dtype, out_dtype, x_pad, y_pad, act, with_bias):
+    lengths, tail = [9000, 0, 8000], 3
+    rows, groups = sum(lengths) + tail, len(lengths)
+    assert rows // groups >= 512 and (rows // 256 + groups) * (-(-fan_out // 256)) >= 256
+    gen = torch.Generator().manual_seed(fan_in + fan_out)
+    x = torch.randn(rows, fan_in, generator=gen).to(dtype)
+    x[-tail:] = float("nan")
+    w = (torch.randn(groups, fan_out, fan_in, generator=gen) / math.sqrt(fan_in)).to(dtype)
+    bias = torch.randn(groups, fan_out, generator=gen) if with_bias else None
+    offsets = [0] + np.cumsum(lengths).tolist()
+    full = torch.full((rows, y_pad[0] + fan_out + y_pad[1]), 5.0, dtype=out_dtype, device="cuda")
+    out = full[:, y_pad[0]:y_pad[0] + fan_out]
+    got = binding.pcc_grouped_linear(_view(x, *x_pad), w.cuda(), bias.cuda() if with_bias else None, torch.tensor(offsets).cuda(), act, out=out)
+    want, bound = ref.linear(x, w, bias, offsets, act)
+    ref.assert_near(got, want, bound, (fan_in, fan_out))
+    assert (got[-tail:] == 5).all() and (full[:, :y_pad[0]] == 5).all() and (full[:, y_pad[0] + fan_out:] == 5).all()
+
+
+# ---------------------------------------------------------------------------------------------------- sums of many groups
+
+@pytest.mark.parametrize("fan_in,fan_out", [(48, 24), (200, 264)])
+def test_sums_of_cut_groups_behind_many_others(fan_in, fan_out):
+    """Groups of several chunks before and behind the 64th and 128th: their sums are numbered over all groups in front."""
+    lengths = [7 * (g % 5) for g in range(150)]
+    for g in (0, 3, 63, 64, 70, 127, 128, 149):
+        lengths[g] = 4000 + 100 * (g % 7)
+    gen = torch.Generator().manual_seed(9)
+    rows = sum(lengths)
+    x, dz = torch.randn(rows, fan_in, generator=gen).to(BF16), torch.randn(rows, fan_out, generator=gen).to(BF16)
+    w = (torch.randn(150, fan_out, fan_in, generator=gen) / math.sqrt(fan_in)).to(BF16)
+    offsets = [0] + np.cumsum(lengths).tolist()
+    first = binding.pcc_grouped_linear_grad(dz.cuda(), x.cuda(), w.cuda(), torch.tensor(offsets).cuda(), ref.RELU)
+    for name, got, (value, bound) in zip(("dx", "dw", "db"), first, ref.linear_grad(dz, x, w, offsets, ref.RELU)):
+        ref.assert_near(got, value, bound, name)
+    again = binding.pcc_grouped_linear_grad(dz.cuda(), x.cuda(), w.cuda(), torch.tensor(offsets).cuda(), ref.RELU)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+# ---------------------------------------------------------------------------------------------------- AdamW
+
+SIZES = [9_000_001, 4097, 8_000_003, 255, 300_000]     # 17.3 million: pieces of four blocks a wave, and more of them than workgroups
+APART = 1 << 21                                         # elements of a plan that has pieces of one block a wave
+
+
+@pytest.mark.parametrize("grad_dtype", [FP32, BF16])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_of_many_elements(bits, shift, grad_dtype):
+    """Every element has the bits that it has in a plan of few elements; some stretches are compared with the reference as well."""
+    gen = torch.Generator(device="cuda").manual_seed(bits + shift)
+    hyper = dict(lr=1e-3, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.1)
+    make = lambda n, dtype: torch.randn(n + 8, generator=gen, device="cuda").to(dtype)[shift:shift + n]  # noqa: E731
+    params, grads = [make(n, FP32) for n in SIZES], [make(n, grad_dtype) for n in SIZES]
+    copies = [torch.zeros(n + 8, dtype=BF16, device="cuda")[shift:shift + n] for n in SIZES]
+    start = [p.clone() for p in params]
+    opt = binding.AdamW(params, grads, copies=copies, state_bits=bits, **hyper)
+    spans = [(i, a, min(a + APART, n)) for i, n in enumerate(SIZES) for a in range(0, n, APART)]
+    few_grads = [torch.empty(b - a, dtype=grad_dtype, device="cuda") for _, a, b in spans]
+    few = [binding.AdamW([start[i][a:b].clone()], [g], copies=[torch.zeros(b - a, dtype=BF16, device="cuda")], state_bits=bits, **hyper)
+           for (i, a, b), g in zip(spans, few_grads)]
+    # stretches of two blocks: at the ends of tensors, at a piece's end, where a workgroup takes its second piece
+    looked_at = [(i, a) for i, n in enumerate(SIZES) for a in (0, 4096 - 256, 1024 * 4096 - 256, 4096 * 1024 + 4096 - 256, n // 256 * 256 - 256) if 0 <= a < n]
+    want = [ref.AdamW(start[i][a:a + 512].cpu().numpy(), bits, **hyper) for i, a in looked_at]
+    for _ in range(3):
+        for g in grads:
+            g.copy_(torch.randn(g.shape, generator=gen, device="cuda"))
+        for (i, a, b), g, one in zip(spans, few_grads, few):
+            g.copy_(grads[i][a:b])
+            one.pcc_adamw_step()
+        opt.pcc_adamw_step()
+        for (i, a), r in zip(looked_at, want):
+            r.step(grads[i][a:a + 512].float().cpu().numpy())
+    for (i, a, b), one in zip(spans, few):
+        pairs = [(params[i], one.params[0]), (copies[i], one.copies[0]), (opt.m[i], one.m[0]), (opt.v[i], one.v[0])]
+        assert all(torch.equal(x[a:b].view(torch.uint8) if x.element_size() == 1 else x[a:b], y.view(torch.uint8) if y.element_size() == 1 else y)
+                   for x, y in pairs), (i, a)
+        if bits == 8:
+            blocks = slice(a // 256, -(-b // 256))
+            assert torch.equal(opt.m_scale[i][blocks], one.m_scale[0]) and torch.equal(opt.v_scale[i][blocks], one.v_scale[0]), (i, a)
+    for (i, a), r in zip(looked_at, want):
+        m, v = (t[i][a:a + 512] for t in (opt.m, opt.v))
+        assert np.array_equal((m.view(torch.uint8) if bits == 8 else m).cpu().numpy(), r.m), (i, a)
+        assert np.array_equal((v.view(torch.uint8) if bits == 8 else v).cpu().numpy(), r.v), (i, a)
+        # in each of three steps the quotient and the product, each off by a step of fp32 at most on an update of ten rates at most, and the
+        # parameter's own three roundings
+        assert np.all(np.abs(params[i][a:a + 512].cpu().numpy() - r.p) <= 3 * 2.0 ** -24 * (3 * np.abs(r.p) + 12 * hyper["lr"] * 10)), (i, a)
