@@ -116,3 +116,96 @@ def test_adamw_of_many_elements(bits, shift, grad_dtype):
         # in each of three steps the quotient and the product, each off by a step of fp32 at most on an update of ten rates at most, and the
         # parameter's own three roundings
         assert np.all(np.abs(params[i][a:a + 512].cpu().numpy() - r.p) <= 3 * 2.0 ** -24 * (3 * np.abs(r.p) + 12 * hyper["lr"] * 10)), (i, a)
+
+
+def test_adamw_behind_the_four_billionth_element():
+    n, tail = (1 << 32) + 70000, 70000 + 4096
+    p = torch.zeros(n, device="cuda")
+    g = torch.zeros(n, dtype=BF16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    p[-tail:] = torch.randn(tail, generator=gen, device="cuda")
+    g[-tail:] = torch.randn(tail, generator=gen, device="cuda").to(BF16)
+    few = [p[-tail:].clone()]
+    opt, one = binding.AdamW([p], [g], state_bits=8), binding.AdamW(few, [g[-tail:].clone()], state_bits=8)
+    for _ in range(2):
+        opt.pcc_adamw_step()
+        one.pcc_adamw_step()
+    assert torch.equal(p[-tail:], few[0]) and not p[:1 << 20].any()
+    for a, b in ((opt.m[0], one.m[0]), (opt.v[0], one.v[0])):
+        assert torch.equal(a[-tail:].view(torch.uint8), b.view(torch.uint8))
+
+
+# ---------------------------------------------------------------------------------------------------- rows far apart
+
+def _apart(t, ld=1 << 15):
+    """t's values in rows `ld` elements apart: the last ones lie behind the 2^32nd element."""
+    full = torch.empty((t.shape[0], ld), dtype=t.dtype, device="cuda")
+    assert t.shape[0] * ld > 1 << 32
+    full[:, :t.shape[1]] = t
+    return full[:, :t.shape[1]]
+
+
+@pytest.mark.parametrize("fan_in,fan_out", [(32, 48), (200, 264), (201, 264)])
+def test_products_of_rows_far_apart(fan_in, fan_out):
+    rows = (1 << 17) + 600
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, dz = (torch.randn(rows, n, generator=gen, device="cuda").to(BF16) for n in (fan_in, fan_out))
+    w, off = torch.randn(2, fan_out, fan_in, generator=gen, device="cuda").to(BF16), torch.tensor([0, 100, rows], device="cuda")
+    ld = 1 << 15
+    y = torch.empty((rows, ld), dtype=FP32, device="cuda")[:, :fan_out]
+    got = binding.pcc_grouped_linear(_apart(x), w, None, off, ref.RELU, out=y)
+    assert torch.equal(got, binding.pcc_grouped_linear(x.contiguous(), w, None, off, ref.RELU, out_dtype=FP32))
+    del y, got
+    dx = torch.empty((rows, ld), dtype=BF16, device="cuda")[:, :fan_in]
+    far, near = binding.pcc_grouped_linear_grad(_apart(dz), _apart(x), w, off, ref.RELU, dx=dx), binding.pcc_grouped_linear_grad(dz, x, w, off, ref.RELU)
+    if fan_in % 2 == 0:                 # odd rows one behind the other take other loads, and the same order of sums
+        assert all(torch.equal(a, b) for a, b in zip(far, near))
+    want = ref.linear_grad(dz[-500:], x[-500:], w[1:], [0, 500], ref.RELU)[0]
+    ref.assert_near(far[0][-500:], *want, "dx")
+
+
+def test_contexts_and_loss_of_rows_far_apart():
+    img = torch.randint(0, 256, (1, 260, 600, 3), dtype=torch.uint8, device="cuda")
+    rows = 260 * 600
+    far = torch.empty((rows, 1 << 15), dtype=BF16, device="cuda")[:, :40]
+    assert torch.equal(binding.pcc_contexts(img, 12, 3, 40, out=far), binding.pcc_contexts(img, 12, 3, 40))
+    del far
+    params = torch.randn(rows, 60, device="cuda")
+    near = binding.pcc_mixture_loss(params, img.view(-1, 3), grad_dtype=FP16)
+    grad = torch.empty((rows, 1 << 15), dtype=FP16, device="cuda")[:, :60]
+    far = binding.pcc_mixture_loss(_apart(params), img.view(-1, 3), grad=grad)
+    assert torch.equal(near[0], far[0]) and torch.equal(near[1], far[1])
+
+
+# ---------------------------------------------------------------------------------------------------- all the groups there may be
+
+def test_as_many_groups_as_there_may_be():
+    groups, fan_in, fan_out = 65535, 8, 6
+    gen = torch.Generator().manual_seed(5)
+    lengths = torch.randint(0, 3, (groups,), generator=gen)
+    lengths[40000] = 3000
+    lengths[-1] = 1
+    offsets = torch.nn.functional.pad(lengths.cumsum(0), (1, 0))
+    rows = int(offsets[-1])
+    x, dz = torch.randn(rows, fan_in, generator=gen).to(BF16), torch.randn(rows, fan_out, generator=gen).to(BF16)
+    w = torch.randn(groups, fan_out, fan_in, generator=gen).to(BF16)
+    bias = torch.randn(groups, fan_out, generator=gen)
+    of = torch.repeat_interleave(torch.arange(groups), lengths)
+    y = binding.pcc_grouped_linear(x.cuda(), w.cuda(), bias.cuda(), offsets.cuda(), out_dtype=FP32)
+    want, size = torch.zeros(rows, fan_out, dtype=torch.float64), torch.zeros(rows, fan_out, dtype=torch.float64)
+    for k in range(fan_in):
+        want += x[:, k:k + 1].double() * w[of, :, k].double()
+        size += (x[:, k:k + 1].double() * w[of, :, k].double()).abs()
+    ref.assert_near(y, want + bias[of].double(), (fan_in + 3) * ref.EPS32 * (size + bias[of].abs().double()), "y")
+    dx, dw, db = binding.pcc_grouped_linear_grad(dz.cuda(), x.cuda(), w.cuda(), offsets.cuda())
+    want, size = torch.zeros(rows, fan_in, dtype=torch.float64), torch.zeros(rows, fan_in, dtype=torch.float64)
+    for k in range(fan_out):
+        want += dz[:, k:k + 1].double() * w[of, k].double()
+        size += (dz[:, k:k + 1].double() * w[of, k].double()).abs()
+    ref.assert_near(dx, want, (fan_out + 2) * ref.EPS32 * size, "dx")
+    terms = dz[:, :, None].double() * x[:, None].double()
+    sums, sizes = torch.zeros(w.shape, dtype=torch.float64).index_add_(0, of, terms), torch.zeros(w.shape, dtype=torch.float64).index_add_(0, of, terms.abs())
+    ref.assert_near(dw, sums, (lengths + 2).double()[:, None, None] * ref.EPS32 * sizes, "dw")
+    sums = torch.zeros(groups, fan_out, dtype=torch.float64).index_add_(0, of, dz.double())
+    sizes = torch.zeros(groups, fan_out, dtype=torch.float64).index_add_(0, of, dz.double().abs())
+    ref.assert_near(db, sums, (lengths + 2).double()[:, None] * ref.EPS32 * sizes, "db")
