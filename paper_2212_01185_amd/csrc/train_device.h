@@ -101,41 +101,67 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
     return v;
 }
 
+// Where a group's chunks begin in an order that its offset alone tells: group g has the places from `place`(g) to `place`(g + 1), one more than it
+// needs at most, since a row at the offset a of chunks of c rows has a / c chunks in front of it and each group adds one for its part.
+__device__ __forceinline__ uint32_t whole_chunks(int64_t rows, int log2, uint32_t mult) { return (uint32_t)(rows >> log2) / mult; }
+__device__ __forceinline__ uint32_t place(const int64_t* __restrict__ off, int g, int64_t rows, int log2, uint32_t mult) {
+    return whole_chunks(clamp64(off[g], 0, rows), log2, mult) + (uint32_t)g;
+}
+// The same for the sums of groups of more than one chunk, where there are more than 64 groups: within the workspace's rows / c + groups, or 2 rows / c
+// (such a group of n chunks has an offset c behind its own at least, and n <= 2 (b / c - a / c)).
+__device__ __forceinline__ uint32_t shared_place(int64_t lo, int g, int groups, int64_t rows, int log2, uint32_t mult) {
+    const uint32_t before = whole_chunks(lo, log2, mult);
+    return (uint32_t)groups <= whole_chunks(rows, log2, mult) ? before + (uint32_t)g : 2 * before;
+}
+
+// find_chunk for more than 64 groups: searched 64 at a time by their places (65,535 in three steps), some of which hold no chunk.  Numbering the
+// chunks as they are would take every workgroup through all offsets (65,535 rows of 32 to 32, us, numbered and so: 4,096 groups 540 and 32, 65,535
+// groups 131,000 and 445).
+__device__ __forceinline__ Chunk search_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t mult, uint32_t tiles, uint32_t b, bool empty) {
+    const Chunk none = {-1, 0, 0, 0, 0, 0};
+    const int lane = threadIdx.x & 63;
+    const uint32_t all = uniform(place(off, groups, rows, log2, mult)) * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
+    if (at >= each || t >= all) return none;
+    const uint32_t wanted = t / tiles;
+    int from = 0, to = groups;
+    while (to - from > 1) {
+        const int apart = (to - from + 63) / 64, g = from + lane * apart;
+        const uint64_t before = __ballot(g < to && place(off, g, rows, log2, mult) <= wanted);
+        from += before ? (63 - __clzll((long long)before)) * apart : 0;
+        to = to - from > apart ? from + apart : to;
+    }
+    int64_t lo, hi;
+    const uint32_t count = uniform(group_chunks(off, from, groups, rows, log2, mult, empty, lo, hi)), first = uniform(place(off, from, rows, log2, mult));
+    const uint32_t places = uniform(place(off, from + 1, rows, log2, mult)) - first;
+    if (wanted < first || wanted - first >= places) return none;        // (in front of the first group, or offsets that fall)
+    const uint32_t in_group = t - first * tiles, chunk = in_group % places;
+    if (chunk >= count) return none;        // a place without a chunk
+    lo = uniform64(lo);
+    hi = uniform64(hi);
+    const int64_t size = (int64_t)mult << log2, clo = lo + (int64_t)chunk * size, chi = clo + size;
+    return {from, clo, chi < hi ? chi : hi, shared_place(lo, from, groups, rows, log2, mult) + chunk, count, in_group / places};
+}
+
 // Workgroup b's chunk and tile (of `tiles` that each chunk has).  All lanes of a wave together; the result is the same in every lane.
 // `shared` is only found with `empty`, for sums.
 // The chip's eight dies take workgroups in turn and have an L2 each, so die d gets the d-th eighth of the work, and within a group
-// the chunks of one tile come one after the other: they read the same weights at about the same time.
+// the chunks of one tile come one after the other: they read the same weights at about the same time.  A lane has a group.
 __device__ __forceinline__ Chunk find_chunk(const int64_t* __restrict__ off, int groups, int64_t rows, int log2, uint32_t mult, uint32_t tiles, uint32_t b, bool empty) {
+    if (groups > 64) return search_chunk(off, groups, rows, log2, mult, tiles, b, empty);
     const int lane = threadIdx.x & 63;
-    uint32_t total = 0;
-    if (groups > 64) {                  // else the search itself says it
-        for (int g0 = 0; g0 < groups; g0 += 64) {
-            int64_t lo, hi;
-            total += wave_sum(group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi));
-        }
-    }
-    uint32_t before = 0, shared = 0;
-    for (int g0 = 0; g0 < groups; g0 += 64) {
-        int64_t lo, hi;
-        const uint32_t n = group_chunks(off, g0 + lane, groups, rows, log2, mult, empty, lo, hi);
-        const uint32_t sum = groups == 1 ? uniform(n) : wave_prefix(n);
-        if (groups <= 64) total = groups == 1 ? sum : (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
-        const uint32_t all = total * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
-        if (at >= each || t >= all) break;
-        const uint64_t beyond = __ballot((before + sum) * tiles > t);
-        if (beyond) {
-            const int found = __ffsll((unsigned long long)beyond) - 1;
-            const int64_t glo = uniform64(__shfl(lo, found)), ghi = uniform64(__shfl(hi, found));
-            const uint32_t count = uniform((uint32_t)__shfl((int)n, found)), first = before + uniform((uint32_t)__shfl((int)sum, found)) - count;
-            const uint32_t in_group = t - first * tiles, chunk = tiles == 1 ? in_group : in_group % count;
-            const int64_t size = (int64_t)mult << log2, clo = glo + (int64_t)chunk * size, chi = clo + size;
-            if (empty && groups > 1) shared += wave_sum(n > 1 && lane < found ? n : 0);
-            return {g0 + found, clo, chi < ghi ? chi : ghi, shared + chunk, count, tiles == 1 ? 0 : in_group / count};
-        }
-        before += uniform((uint32_t)__shfl((int)sum, 63));
-        if (empty) shared += wave_sum(n > 1 ? n : 0);
-    }
-    return {-1, 0, 0, 0, 0, 0};
+    int64_t lo, hi;
+    const uint32_t n = group_chunks(off, lane, groups, rows, log2, mult, empty, lo, hi);
+    const uint32_t sum = groups == 1 ? uniform(n) : wave_prefix(n);
+    const uint32_t total = groups == 1 ? sum : (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
+    const uint32_t all = total * tiles, each = (all + 7) / 8, at = b / 8, t = (b % 8) * each + at;
+    if (at >= each || t >= all) return {-1, 0, 0, 0, 0, 0};
+    const int found = __ffsll((unsigned long long)__ballot(sum * tiles > t)) - 1;
+    const int64_t glo = uniform64(__shfl(lo, found)), ghi = uniform64(__shfl(hi, found));
+    const uint32_t count = uniform((uint32_t)__shfl((int)n, found)), first = uniform((uint32_t)__shfl((int)sum, found)) - count;
+    const uint32_t in_group = t - first * tiles, chunk = tiles == 1 ? in_group : in_group % count;
+    const int64_t size = (int64_t)mult << log2, clo = glo + (int64_t)chunk * size, chi = clo + size;
+    const uint32_t shared = empty && groups > 1 ? wave_sum(n > 1 && lane < found ? n : 0) : 0;
+    return {found, clo, chi < ghi ? chi : ghi, shared + chunk, count, tiles == 1 ? 0 : in_group / count};
 }
 
 }  // namespace pcc_train

@@ -359,10 +359,12 @@ __global__ __launch_bounds__(256) void grouped_reduce_kernel(Grouped a) {
     int64_t lo, hi;
     const uint32_t count = uniform(group_chunks(a.off, g, a.groups, a.rows, a.log2, a.mult, true, lo, hi));
     if (count <= 1) return;
-    uint32_t first = 0;
-    for (int g0 = 0; g0 < g; g0 += 64) {
-        const uint32_t n = group_chunks(a.off, g0 + lane, g, a.rows, a.log2, a.mult, true, lo, hi);
-        first += wave_sum(n > 1 ? n : 0);
+    uint32_t first;
+    if (a.groups > 64) {
+        first = uniform(shared_place(lo, g, a.groups, a.rows, a.log2, a.mult));
+    } else {
+        const uint32_t n = group_chunks(a.off, lane, g, a.rows, a.log2, a.mult, true, lo, hi);
+        first = wave_sum(n > 1 ? n : 0);
     }
     if (first + count > a.shared_max) return;
     const size_t size = (size_t)a.in * a.out, all = size + a.out, stride = partial_values(a.in, a.out);

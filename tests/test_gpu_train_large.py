@@ -209,3 +209,63 @@ def test_as_many_groups_as_there_may_be():
     sums = torch.zeros(groups, fan_out, dtype=torch.float64).index_add_(0, of, dz.double())
     sizes = torch.zeros(groups, fan_out, dtype=torch.float64).index_add_(0, of, dz.double().abs())
     ref.assert_near(db, sums, (lengths + 2).double()[:, None] * ref.EPS32 * sizes, "db")
+
+
+@pytest.mark.parametrize("fan_in,fan_out", [(32, 32), (200, 8)])
+def test_time_does_not_grow_with_the_square_of_groups(fan_in, fan_out):
+    """As many groups as there may be, of a row each: 130 ms when every workgroup read all offsets, under 1 ms since."""
+    groups = 65535
+    x, w = torch.ones(groups, fan_in, dtype=BF16, device="cuda"), torch.ones(groups, fan_out, fan_in, dtype=BF16, device="cuda")
+    off = torch.arange(groups + 1, device="cuda")
+    dz = torch.ones(groups, fan_out, dtype=BF16, device="cuda")
+    for call in (lambda: binding.pcc_grouped_linear(x, w, None, off), lambda: binding.pcc_grouped_linear_grad(dz, x, w, off)):
+        times = []
+        for _ in range(4):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            call()
+            end.record()
+            torch.cuda.synchronize()
+            times.append(start.elapsed_time(end))
+        assert min(times) < 20
+
+
+@pytest.mark.parametrize("fan_in,fan_out", [(48, 24), (200, 264)])
+@pytest.mark.parametrize("kind", ["overlap", "fall", "beyond"])
+def test_offsets_of_many_groups_that_make_no_sense_stay_inside(fan_in, fan_out, kind):
+    rows, groups = 30000, 130
+    off = {"overlap": torch.tensor([0, rows] * 65 + [0]), "fall": torch.linspace(rows, 0, groups + 1).long(),
+           "beyond": torch.tensor([-5, 1 << 60, 7, -(1 << 60), 40] * 26 + [1 << 40])}[kind].cuda()
+    x, dz = torch.ones(rows, fan_in, dtype=BF16, device="cuda"), torch.ones(rows, fan_out, dtype=BF16, device="cuda")
+    w = torch.ones(groups, fan_out, fan_in, dtype=BF16, device="cuda")
+    y, dx = (torch.full((rows + 20, n), 5.0, dtype=BF16, device="cuda") for n in (fan_out, fan_in))
+    need = binding.load().pcc_grouped_linear_grad_workspace_bytes(rows, groups, fan_in, fan_out)
+    space = torch.full((need + (1 << 20),), 77, dtype=torch.uint8, device="cuda")
+    binding.pcc_grouped_linear(x, w, None, off, out=y[10:-10])
+    binding.pcc_grouped_linear_grad(dz, x, w, off, dx=dx[10:-10], workspace=space[:need])
+    torch.cuda.synchronize()
+    assert need > 0 and (space[need:] == 77).all() and all((t[:10] == 5).all() and (t[-10:] == 5).all() for t in (y, dx))
+
+
+@pytest.mark.parametrize("fan_in,fan_out", [(48, 24), (200, 264)])
+@pytest.mark.parametrize("first", [0, 1, 5000])
+def test_more_than_64_groups_behind_rows_of_none(fan_in, fan_out, first):
+    """The first group need not begin at the first row; more than 64 groups are found by their offsets."""
+    lengths = [(37 * g) % 90 for g in range(200)]
+    lengths[11], lengths[120] = 1500, 2300
+    offsets = (first + np.concatenate([[0], np.cumsum(lengths)])).tolist()
+    rows = offsets[-1] + 700
+    gen = torch.Generator().manual_seed(first)
+    x, dz = torch.randn(rows, fan_in, generator=gen).to(BF16), torch.randn(rows, fan_out, generator=gen).to(BF16)
+    w = (torch.randn(200, fan_out, fan_in, generator=gen) / math.sqrt(fan_in)).to(BF16)
+    nobody = torch.ones(rows, dtype=torch.bool)
+    nobody[offsets[0]:offsets[-1]] = False
+    x[nobody], dz[nobody] = float("nan"), float("inf")
+    y, dx = (torch.full((rows, n), 5.0, dtype=BF16, device="cuda") for n in (fan_out, fan_in))
+    off = torch.tensor(offsets).cuda()
+    binding.pcc_grouped_linear(x.cuda(), w.cuda(), None, off, ref.RELU, out=y)
+    _, dw, db = binding.pcc_grouped_linear_grad(dz.cuda(), x.cuda(), w.cuda(), off, ref.LEAKY, dx=dx)
+    ref.assert_near(y, *ref.linear(x, w, None, offsets, ref.RELU), "y")
+    for name, got, (value, bound) in zip(("dx", "dw", "db"), (dx, dw, db), ref.linear_grad(dz, x, w, offsets, ref.LEAKY)):
+        ref.assert_near(got, value, bound, name)
+    assert (y[nobody.cuda()] == 5).all() and (dx[nobody.cuda()] == 5).all()
