@@ -275,7 +275,10 @@ int pcc_grouped_linear_grad(const void *d_dz, size_t lddz, const void *d_x, size
  *   [count] fp32 or NULL (all 1).  A pixel of weight 0 (padding) is not looked
  *   at: its bits and gradients are 0 whatever its parameters hold.
  * Either of d_bits and d_grad may be NULL.  d_grad may be d_params where
- * grad_type is PCC_FP32 and the ld are equal. */
+ * grad_type is PCC_FP32 and the ld are equal.
+ * Arithmetic is in fp32 but for a level's distance from a mean (fp64), with the
+ * hardware's exponential and reciprocal: gradients are some 1.5e-7 of their size
+ * off, a term some 3e-5 of its own far out in a tail. */
 int pcc_mixture_loss(const float *d_params, size_t ldp, const uint8_t *d_rgb, const float *d_weight, size_t count,
                      int K, int dist, float scale, float *d_bits, void *d_grad, int grad_type, size_t ldg,
                      void *hip_stream);
@@ -283,7 +286,8 @@ int pcc_mixture_loss(const float *d_params, size_t ldp, const uint8_t *d_rgb, co
 /* AdamW over many tensors, all in one launch.  With t = *d_step + 1, written back:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g g,
  *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32, and the 16-bit copy of the new param where there is one (what the
+ * in fp32 (the last quotient as m times a reciprocal, 1.5 units in the last place
+ * off at most), and the 16-bit copy of the new param where there is one (what the
  * products read and a blob holds).
  * States in 32 bits: m, v fp32 [n].  States in 8 bits: m and the root of v as
  * e4m3 codes [n] and an fp32 scale for each 256 elements [ceil(n / 256)]; the
@@ -313,7 +317,8 @@ typedef struct pcc_adamw pcc_adamw;
 /* Lay out the list of tensors (host array, copied) on device `hip_device`.  The
  * tensors stay the caller's, where they are, and must outlive the plan; what a step
  * writes must not overlap, nor a gradient with it (PCC_E_ARG; an fp32 gradient may be
- * its own parameter).  Allocates device memory and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
+ * its own parameter).  So must the plan outlive graphs that have captured its steps.
+ * Allocates device memory and waits for the copy.  grad_type PCC_FP32, PCC_BF16 or PCC_FP16; copy_type
  * PCC_BF16 or PCC_FP16; state_bits 32 or 8. */
 int pcc_adamw_create(pcc_adamw **out, const pcc_adamw_tensor *h_tensors, int count, int grad_type, int copy_type,
                      int state_bits, int hip_device);

@@ -383,7 +383,10 @@ class AdamW:
     params fp32, grads all of one type (fp32, bf16, fp16), copies (16-bit copies of the new parameters) or None.  States are
     made here or handed in (a checkpoint's): m, v fp32, or with state_bits=8 torch.float8_e4m3fn codes of m and of the root of v
     with m_scale, v_scale fp32 [ceil(n / 256)].  `step` int64 [1] counts the steps on the device.  `lr_tensor` fp32 [1] on the
-    device is read at every step in place of lr."""
+    device is read at every step in place of lr.
+
+    The plan holds the tensors' addresses: gradients are written into the tensors given here (not allocated anew), and a graph that
+    captured a step is replayed only while this object lives.  States in 8 bits have a scale for 256 elements of a tensor."""
 
     def __init__(self, params, grads, copies=None, state_bits: int = 32, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, step=None, m=None, v=None, m_scale=None, v_scale=None, lr_tensor=None):

@@ -3,8 +3,8 @@
 // One launch for all: a list of pieces of 4,096 elements (1,024 where there are few), made when the plan is, says which tensor a
 // workgroup works on.  Every
 // element is read once and written once: 16 + 12 bytes with states in 32 bits, 10 + 6 in 8 bits, and what the copy takes.  33.5 million
-// elements with a bf16 copy: 205 us with 32 bits (4.9 TB/s, memory), 167 with 8 (3.6 TB/s: exact roots, quotients and codes cost as
-// much time as the memory does).
+// elements with a bf16 copy: 205 us with 32 bits (4.9 TB/s, memory), 166 with 8 (3.6 TB/s, and the vector ALU busy for 57 % of the time: a
+// wave's loads, then exact roots and codes, exchanges and stores come one after the other, so neither is full).
 //
 // 8-bit states.  A wave has a block of 256 elements, four a lane, and finds its largest magnitudes by exchanges.  Codes are e4m3: a
 // step of a code is 1/8 to 1/16 of the value, and one step of the second moment's average changes it by 1 - beta2, a

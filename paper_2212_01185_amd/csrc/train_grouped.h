@@ -230,7 +230,7 @@ __device__ __forceinline__ void store_eight(const Grouped& a, size_t at, f32x4 v
 
 // Rates: forward, four groups of 2,048 rows, 2048 to 2048, 71 us (970 TFLOP/s; a large library product of this card has 1,176) with tiles of 256;
 // sixteen of 512 rows, 1024 to 4096, 131 us (525), where a group's last tile is half empty and 656 tiles take three turns of 256 compute units.
-// dx and dw, sixteen of 512 rows, 1024 to 2048, 97 and 82 us (350 and 420): tiles of 256 would spill (their rows pass through registers).
+// dx and dw, sixteen of 512 rows, 1024 to 2048, 97 and 84 us (350 and 410): tiles of 256 would spill (their rows pass through registers).
 // TILE x TILE results of a workgroup: 128 by four waves with 64 x 64 each, 256 by eight with 128 x 64.  Two tiles in LDS for each
 // operand: the next step's is filled while this one's is multiplied.
 template <class T, int MODE, bool WIDE, int TILE>

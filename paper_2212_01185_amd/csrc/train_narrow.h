@@ -12,9 +12,10 @@ namespace pcc_train {
 // n, read from memory as MFMA operands (a lane 16 bytes of one row; four lanes have 64 bytes of it), the next 32 while
 // these are multiplied.  The weights are in LDS as operands.  Two blocks of 16 outputs are made together, their outputs
 // dealt so that a lane gets eight neighbours: block b, row 4 g + i is output 32 pair + 8 g + 4 b + i.  Finished rows go through LDS where
-// it has room, so that they leave in whole lines (160 to 160 on 393,216 rows, us: 72 without, 61 to 64 with: 3.9 TB/s, a large copy has
-// 5.2; 786,432 rows 4.4 TB/s).  One workgroup of 512 threads a compute unit: with 256 threads, or with registers for four waves a
-// SIMD, 79 to 87 us.  What is left is the start (the offsets, the weights: some 4 us) and reading 64 bytes of a row at a time.
+// it has room, so that they leave in whole lines (160 to 160 on 393,216 rows, us: 72 without, 64 with: 3.9 TB/s, a large copy has
+// 5.2; 786,432 rows 4.3 TB/s).  One workgroup of 512 threads a compute unit: with 256 threads, or with registers for four waves a
+// SIMD, 79 to 87 us.  What is left is the start (the offsets, the weights: some 4 us) and reading 64 bytes of a row at a time;
+// nothing is fetched or written twice, and the vector ALU is busy for 45 %, the matrix cores for 17 % of the time.
 // ---------------------------------------------------------------------------
 constexpr int kNarrowThreads = 512, kNarrowRowsWave = 32;
 
@@ -168,8 +169,9 @@ __global__ __launch_bounds__(kNarrowThreads) void grouped_narrow_forward_kernel(
 // quarters of the outputs).
 // A row in LDS has its chunks of 8 values, zeros up to a multiple of four chunks, and two more of nothing: a distance of 2 modulo 4
 // chunks puts the 32-byte pieces of eight rows, which ds_read_b64_tr_b16 reads together, into different banks.
-// 160 to 160 on 393,216 rows: 95 us (3.9 TB/s) and 7 for joining 256 chunks' sums; with loads straight to LDS 135 us, and as two passes
-// of the tile kernel 348.  LDS is busy for a third of the time; the rest is memory, and 24 us of start and end (a chunk's sums are 100 KB).
+// 160 to 160 on 393,216 rows: 99 us (3.8 TB/s), 5 of them for joining 256 chunks' sums; with loads straight to LDS 135 us, and as two passes
+// of the tile kernel 348.  LDS is busy for 36 % of the time, matrix cores and vector ALU for 26 and 30; the rest is memory, and 24 us of start and end
+// (a chunk's sums are 100 KB).
 // ---------------------------------------------------------------------------
 constexpr int kMaxLds = 160 * 1024;
 
