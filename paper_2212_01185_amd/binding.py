@@ -278,8 +278,9 @@ def _call(what: str, device, *args) -> None:
 
 def _unrecorded(*tensors) -> None:
     """Refuses tensors whose gradients autograd is asked for: the operators' backward passes are calls of their own."""
-    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
-        raise ValueError("autograd does not record these operators: call them under torch.no_grad() or on detached tensors")
+    for t in tensors:
+        if getattr(t, "requires_grad", False) and torch.is_grad_enabled():
+            raise ValueError("autograd does not record these operators: call them under torch.no_grad() or on detached tensors")
 
 
 def _ptr(t):
