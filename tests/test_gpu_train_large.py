@@ -269,3 +269,40 @@ def test_more_than_64_groups_behind_rows_of_none(fan_in, fan_out, first):
     for name, got, (value, bound) in zip(("dx", "dw", "db"), (dx, dw, db), ref.linear_grad(dz, x, w, offsets, ref.LEAKY)):
         ref.assert_near(got, value, bound, name)
     assert (y[nobody.cuda()] == 5).all() and (dx[nobody.cuda()] == 5).all()
+
+
+# ---------------------------------------------------------------------------------------------------- the widest and the furthest
+
+@pytest.mark.parametrize("fan_in,fan_out", [(65536, 24), (24, 65536)])
+def test_as_many_features_as_there_may_be(fan_in, fan_out):
+    lengths, tail = [20, 0, 13], 1
+    gen = torch.Generator().manual_seed(fan_in)
+    rows, offsets = sum(lengths) + tail, [0] + np.cumsum(lengths).tolist()
+    x, dz = (torch.randn(rows, n, generator=gen).to(BF16) for n in (fan_in, fan_out))
+    w = (torch.randn(3, fan_out, fan_in, generator=gen) / math.sqrt(fan_in)).to(BF16)
+    off = torch.tensor(offsets).cuda()
+    ref.assert_near(binding.pcc_grouped_linear(x.cuda(), w.cuda(), None, off, ref.LEAKY), *ref.linear(x, w, None, offsets, ref.LEAKY), "y")
+    got = binding.pcc_grouped_linear_grad(dz.cuda(), x.cuda(), w.cuda(), off, ref.RELU)
+    for name, part, (value, bound) in zip(("dx", "dw", "db"), got, ref.linear_grad(dz, x, w, offsets, ref.RELU)):
+        ref.assert_near(part, value, bound, name)
+
+
+@pytest.mark.parametrize("rows,fan_in,fan_out", [(600, 200, 21900), (300, 200, 264), (300, 201, 264), (300, 160, 128)])
+def test_rows_as_far_apart_as_they_may_be(rows, fan_in, fan_out):
+    """2^22 elements: a row's place in a tile is 31 bits of bytes from the tile's first."""
+    ld = 1 << 22
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, dz = (torch.randn(rows, n, generator=gen, device="cuda").to(BF16) for n in (fan_in, fan_out))
+    w, off = torch.randn(1, fan_out, fan_in, generator=gen, device="cuda").to(BF16), torch.tensor([0, rows], device="cuda")
+    far = lambda n: torch.empty((rows, ld), dtype=BF16, device="cuda")[:, :n]  # noqa: E731
+    x_far = far(fan_in)
+    x_far.copy_(x)
+    y = binding.pcc_grouped_linear(x_far, w, None, off, ref.RELU, out=far(fan_out))
+    assert torch.equal(y, binding.pcc_grouped_linear(x, w, None, off, ref.RELU))
+    del y
+    if fan_out > 10000:
+        return
+    dz_far = far(fan_out)
+    dz_far.copy_(dz)
+    got, want = binding.pcc_grouped_linear_grad(dz_far, x_far, w, off, ref.RELU, dx=far(fan_in)), binding.pcc_grouped_linear_grad(dz, x, w, off, ref.RELU)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
