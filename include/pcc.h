@@ -327,6 +327,112 @@ void pcc_adamw_destroy(pcc_adamw *plan);
  * the device, the number of steps taken so far.  One step of a plan at a time. */
 int pcc_adamw_step(pcc_adamw *plan, const pcc_adamw_hyper *h_hyper, int64_t *d_step, void *hip_stream);
 
+/* ---- Layers round the grouped products ---------------------------------
+ * What deeper networks and mixtures of networks need beside the products, with
+ * the conventions of the training operators above: they belong to no pcc_ctx,
+ * are asynchronous, allocate and keep nothing, may be captured into a HIP
+ * graph, and refuse outputs that overlap inputs or each other (PCC_E_ARG)
+ * unless said otherwise.  Sums are taken in an order that depends on the
+ * arguments alone.  A mixture runs as
+ *   pcc_layer_norm -> pcc_route -> pcc_expert_sort -> pcc_expert_rows ->
+ *   pcc_grouped_linear ... -> pcc_expert_join -> pcc_dropout
+ * where the sort's offsets are the groups of the products. */
+
+#define PCC_MAX_EXPERTS 1024
+#define PCC_MAX_CHOICES 16
+
+/* Layer norm of the rows of each group g:
+ *   y_i = gamma_g (x_i - mean) / sqrt(mean((x_i - mean)^2) + eps) + beta_g
+ *   d_x [rows][features] of `type`, d_y of y_type: the same, or of 16 bits where
+ *   x is fp32.  d_gamma, d_beta [groups][features] fp32, or NULL (1 and 0).
+ *   d_offsets [groups + 1] as above, or NULL for one group of all rows.  d_stats
+ *   [rows][2] fp32 or NULL: each row's mean and 1 / sqrt(...), which the backward
+ *   pass takes.  Rows of no group are neither read nor written.  eps is at least
+ *   2^-126. */
+int pcc_layer_norm(const void *d_x, size_t ldx, const float *d_gamma, const float *d_beta,
+                   const int64_t *d_offsets, int groups, size_t rows, int features, float eps,
+                   int type, void *d_y, int y_type, size_t ldy, float *d_stats, void *hip_stream);
+
+/* Its backward pass: d_dx [rows][features] of `type` (or NULL) from d_dy of
+ * y_type; d_dgamma, d_dbeta [groups][features] fp32 (both or neither): sums over
+ * the group's rows, 0 for a group without any.  d_workspace:
+ * pcc_layer_norm_grad_workspace_bytes(...) bytes (none without d_dgamma), aligned
+ * to 16, that no other call running at the same time uses; PCC_E_SCRATCH if it is
+ * smaller. */
+size_t pcc_layer_norm_grad_workspace_bytes(size_t rows, int groups, int features);
+int pcc_layer_norm_grad(const void *d_dy, int y_type, size_t lddy, const void *d_x, size_t ldx,
+                        const float *d_stats, const float *d_gamma, const int64_t *d_offsets, int groups,
+                        size_t rows, int features, int type, void *d_dx, size_t lddx, float *d_dgamma,
+                        float *d_dbeta, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The k experts with the largest logits of each token, by falling logit (equal
+ * ones: the lowest index first), and their weights: the softmax over the chosen, or
+ * with over_all = 1 the chosen's part of the softmax over all.
+ *   d_logits [tokens][experts] of `type`; d_expert [tokens][k], d_weight
+ *   [tokens][k] fp32.  1 <= k <= experts.
+ * A logit of -inf is never chosen: where fewer than k are left, the other
+ * choices are -1 with weight 0.  A NaN is above all numbers, and a NaN or +inf
+ * among those that are summed makes the token's weights NaN. */
+int pcc_route(const void *d_logits, size_t ldl, size_t tokens, int experts, int k, int type, int over_all,
+              int32_t *d_expert, float *d_weight, void *hip_stream);
+
+/* Its gradient d_dlogits [tokens][experts] of `type`, all of it written: from
+ * d_dweight [tokens][k] fp32 (not looked at where the choice is -1) and what the
+ * call above was given and wrote.  d_logits may be NULL where over_all is 0.  A
+ * logit of -inf has gradient 0. */
+int pcc_route_grad(const float *d_dweight, const void *d_logits, size_t ldl, const int32_t *d_expert,
+                   const float *d_weight, size_t tokens, int experts, int k, int type, int over_all,
+                   void *d_dlogits, size_t lddl, void *hip_stream);
+
+/* Rows by expert: d_place [tokens][k] is the row of each choice d_expert
+ * [tokens][k], those of lower experts first, those of one expert in the order of
+ * the tokens (and of a token's choices); d_offsets [experts + 1]: where each
+ * expert's rows begin, the groups of a grouped product.  A choice outside
+ * 0..experts - 1 has place -1 and no row.  d_workspace:
+ * pcc_expert_sort_workspace_bytes(...) bytes, aligned to 16, that no other call
+ * running at the same time uses; PCC_E_SCRATCH if it is smaller.  tokens k is
+ * below 2^31. */
+size_t pcc_expert_sort_workspace_bytes(size_t tokens, int k, int experts);
+int pcc_expert_sort(const int32_t *d_expert, size_t tokens, int k, int experts, int64_t *d_offsets,
+                    int32_t *d_place, void *d_workspace, size_t workspace_bytes, void *hip_stream);
+
+/* d_rows[place[t][j]] = d_x[t] for all choices with a place in 0..rows - 1; other
+ * rows are left as they are.  (Its gradient is pcc_expert_join without weights.)
+ * No place may stand twice. */
+int pcc_expert_rows(const void *d_x, size_t ldx, const int32_t *d_place, size_t tokens, int k, size_t rows,
+                    int features, int type, void *d_rows, size_t ldr, void *hip_stream);
+
+/* d_y[t] = sum over j of weight[t][j] d_z[place[t][j]], in fp32 and in the order of
+ * j; choices without a place in 0..rows - 1 are left out.  d_z [rows][features] of
+ * `type`, d_y [tokens][features] of `type` or fp32, d_weight [tokens][k] fp32 or
+ * NULL (all 1). */
+int pcc_expert_join(const void *d_z, size_t ldz, const int32_t *d_place, const float *d_weight, size_t tokens,
+                    int k, size_t rows, int features, int type, void *d_y, int y_type, size_t ldy,
+                    void *hip_stream);
+
+/* Its gradient:  d_dz[place[t][j]] = weight[t][j] d_dy[t] (rows without a choice are left as
+ * they are), d_dweight[t][j] = d_dy[t] . d_z[place[t][j]] in fp32, 0 without a place.
+ * Either may be NULL; d_z may be without d_dweight.  No place may stand twice. */
+int pcc_expert_join_grad(const void *d_dy, int y_type, size_t lddy, const void *d_z, size_t ldz,
+                         const int32_t *d_place, const float *d_weight, size_t tokens, int k, size_t rows,
+                         int features, int type, void *d_dz, size_t lddz, float *d_dweight,
+                         void *hip_stream);
+
+/* y = residual + x s where an element is kept, residual where it is dropped:
+ * s = 65536 / (65536 - b), b = round(65536 p), and an element is dropped if its 16
+ * bits are below b (all are with p = 1).  The bits are those of Philox4x32 with ten rounds whose key is the
+ * seed (low word first) and whose counter is {column / 8 | (row >> 32) << 16, row,
+ * step, step >> 32}: the (column % 8)-th half word of the result, low halves first.  So
+ * the same seed and step give the same mask in the backward pass (this call on the
+ * gradient, without a residual), whatever the types and strides.
+ *   d_x [rows][features] of `type`; d_residual [rows][features] of y_type or NULL
+ *   (0); d_y of y_type: the same type or one of them fp32.  d_step: int64 on the
+ *   device, or NULL for 0: a captured step has another mask each time.  d_y may
+ *   be d_x where type and ld are the same, and d_residual where ld is. */
+int pcc_dropout(const void *d_x, size_t ldx, const void *d_residual, size_t ldr, size_t rows, int features,
+                int type, double p, uint64_t seed, const int64_t *d_step, void *d_y, int y_type, size_t ldy,
+                void *hip_stream);
+
 const char *pcc_strerror(int code);
 
 #ifdef __cplusplus

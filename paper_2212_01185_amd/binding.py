@@ -26,6 +26,8 @@ EXPORTS = (
     "pcc_decode", "pcc_decode_static", "pcc_decode_static_scratch_bytes", "pcc_cdf_tables", "pcc_copy_intervals", "pcc_set_profiling", "pcc_last_timings", "pcc_strerror",
     "pcc_contexts", "pcc_grouped_linear", "pcc_grouped_linear_grad_workspace_bytes", "pcc_grouped_linear_grad", "pcc_mixture_loss",
     "pcc_adamw_create", "pcc_adamw_destroy", "pcc_adamw_step",
+    "pcc_layer_norm", "pcc_layer_norm_grad_workspace_bytes", "pcc_layer_norm_grad", "pcc_route", "pcc_route_grad",
+    "pcc_expert_sort_workspace_bytes", "pcc_expert_sort", "pcc_expert_rows", "pcc_expert_join", "pcc_expert_join_grad", "pcc_dropout",
 )
 PCC_BF16, PCC_FP16, PCC_FP32 = 0, 1, 2
 PCC_ACT_RELU, PCC_ACT_LEAKY, PCC_ACT_NONE = 0, 1, 2
@@ -97,6 +99,28 @@ def load():
     L.pcc_adamw_destroy.restype = None
     L.pcc_adamw_step.argtypes = [vp, C.POINTER(_AdamwHyper), vp, vp]
     L.pcc_adamw_step.restype = i32
+    L.pcc_layer_norm.argtypes = [vp, sz, vp, vp, vp, i32, sz, i32, C.c_float, i32, vp, i32, sz, vp, vp]
+    L.pcc_layer_norm.restype = i32
+    L.pcc_layer_norm_grad_workspace_bytes.argtypes = [sz, i32, i32]
+    L.pcc_layer_norm_grad_workspace_bytes.restype = sz
+    L.pcc_layer_norm_grad.argtypes = [vp, i32, sz, vp, sz, vp, vp, vp, i32, sz, i32, i32, vp, sz, vp, vp, vp, sz, vp]
+    L.pcc_layer_norm_grad.restype = i32
+    L.pcc_route.argtypes = [vp, sz, sz, i32, i32, i32, i32, vp, vp, vp]
+    L.pcc_route.restype = i32
+    L.pcc_route_grad.argtypes = [vp, vp, sz, vp, vp, sz, i32, i32, i32, i32, vp, sz, vp]
+    L.pcc_route_grad.restype = i32
+    L.pcc_expert_sort_workspace_bytes.argtypes = [sz, i32, i32]
+    L.pcc_expert_sort_workspace_bytes.restype = sz
+    L.pcc_expert_sort.argtypes = [vp, sz, i32, i32, vp, vp, vp, sz, vp]
+    L.pcc_expert_sort.restype = i32
+    L.pcc_expert_rows.argtypes = [vp, sz, vp, sz, i32, sz, i32, i32, vp, sz, vp]
+    L.pcc_expert_rows.restype = i32
+    L.pcc_expert_join.argtypes = [vp, sz, vp, vp, sz, i32, sz, i32, i32, vp, i32, sz, vp]
+    L.pcc_expert_join.restype = i32
+    L.pcc_expert_join_grad.argtypes = [vp, i32, sz, vp, sz, vp, vp, sz, i32, sz, i32, i32, vp, sz, vp, vp]
+    L.pcc_expert_join_grad.restype = i32
+    L.pcc_dropout.argtypes = [vp, sz, vp, sz, sz, i32, i32, C.c_double, C.c_uint64, vp, vp, i32, sz, vp]
+    L.pcc_dropout.restype = i32
     L.pcc_strerror.argtypes = [i32]
     L.pcc_strerror.restype = C.c_char_p
     _lib = L
@@ -376,6 +400,203 @@ def pcc_mixture_loss(params: torch.Tensor, rgb: torch.Tensor, dist: int = 0, sca
     _call("pcc_mixture_loss", params.device, params.data_ptr(), ldp, rgb.data_ptr(), _ptr(weight), count, outputs // 12, dist, scale,
           bits.data_ptr(), grad.data_ptr() if want_grad else None, _TYPES[grad.dtype] if want_grad else PCC_FP32, ldg)
     return bits, (grad if want_grad else None)
+
+
+# Layers round the grouped products.
+
+def _norm_groups(x, gamma, offsets):
+    """(distance of x's rows, groups) of a layer norm; gamma and offsets may be None."""
+    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    if offsets is not None:
+        _check("offsets", offsets, (torch.int64,), (None,), x.device)
+        groups = int(offsets.shape[0]) - 1
+    else:
+        groups = 1
+    if gamma is not None:
+        _check("gamma", gamma, (torch.float32,), (groups, int(x.shape[1])), x.device)
+    return ldx, groups
+
+
+def pcc_layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                   eps: float = 1e-5, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, stats: torch.Tensor | None = None,
+                   want_stats: bool = True):
+    """(y, stats) of the layer norm of the rows x [rows, features]; gamma, beta fp32 [groups, features] (None: 1 and 0), rows offsets[g] <= i <
+    offsets[g + 1] have the g-th (offsets None: one group of all rows).  y has x's type, or a 16-bit one where x is fp32; stats fp32 [rows, 2], for
+    the backward pass, are None without want_stats.  Rows of no group are left as they are in `out` and `stats`, and undefined in new tensors."""
+    _unrecorded(x, gamma, beta, out, stats)
+    ldx, groups = _norm_groups(x, gamma, offsets)
+    rows, features = int(x.shape[0]), int(x.shape[1])
+    if beta is not None:
+        _check("beta", beta, (torch.float32,), (groups, features), x.device)
+    if out is None:
+        out = torch.empty((rows, features), dtype=out_dtype or x.dtype, device=x.device)
+    ldy = _check("out", out, (tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype,)) if out_dtype is None else (out_dtype,), (rows, features), x.device,
+                 rows=True)
+    if stats is None and want_stats:
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
+    if stats is not None:
+        _check("stats", stats, (torch.float32,), (rows, 2), x.device)
+    _call("pcc_layer_norm", x.device, x.data_ptr(), ldx, _ptr(gamma), _ptr(beta), _ptr(offsets), groups, rows, features, eps, _TYPES[x.dtype],
+          out.data_ptr(), _TYPES[out.dtype], ldy, _ptr(stats))
+    return out, stats
+
+
+def pcc_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, gamma: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                        dx: torch.Tensor | None = None, want_dx: bool = True, want_weights: bool = True, dgamma: torch.Tensor | None = None,
+                        dbeta: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(dx, dgamma, dbeta) of pcc_layer_norm: dx has x's type (None without want_dx), dgamma and dbeta fp32 [groups, features] (None without
+    want_weights).  dy has y's type.  Rows of no group are left as they are in `dx`, and undefined in a new tensor."""
+    _unrecorded(dy, x, stats, gamma, dx, dgamma, dbeta)
+    ldx, groups = _norm_groups(x, gamma, offsets)
+    rows, features = int(x.shape[0]), int(x.shape[1])
+    lddy = _check("dy", dy, tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype,), (rows, features), x.device, rows=True)
+    _check("stats", stats, (torch.float32,), (rows, 2), x.device)
+    if want_dx and dx is None:
+        dx = torch.empty((rows, features), dtype=x.dtype, device=x.device)
+    lddx = _check("dx", dx, (x.dtype,), (rows, features), x.device, rows=True) if want_dx else features
+    if want_weights:
+        dgamma = torch.empty((groups, features), dtype=torch.float32, device=x.device) if dgamma is None else dgamma
+        dbeta = torch.empty((groups, features), dtype=torch.float32, device=x.device) if dbeta is None else dbeta
+        _check("dgamma", dgamma, (torch.float32,), (groups, features), x.device)
+        _check("dbeta", dbeta, (torch.float32,), (groups, features), x.device)
+        if workspace is None:
+            workspace = torch.empty(int((_lib or load()).pcc_layer_norm_grad_workspace_bytes(rows, groups, features)), dtype=torch.uint8, device=x.device)
+        else:
+            _check("workspace", workspace, (torch.uint8,), (None,), x.device)
+    else:
+        dgamma = dbeta = workspace = None
+    _call("pcc_layer_norm_grad", x.device, dy.data_ptr(), _TYPES[dy.dtype], lddy, x.data_ptr(), ldx, stats.data_ptr(), _ptr(gamma), _ptr(offsets), groups,
+          rows, features, _TYPES[x.dtype], dx.data_ptr() if want_dx else None, lddx, _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
+          workspace.numel() if workspace is not None else 0)
+    return (dx if want_dx else None), dgamma, dbeta
+
+
+def pcc_route(logits: torch.Tensor, k: int, over_all: bool = False, expert: torch.Tensor | None = None, weight: torch.Tensor | None = None):
+    """(expert int32 [tokens, k], weight fp32 [tokens, k]): the experts with the k largest logits [tokens, experts] of each token, the largest first, and
+    the softmax over them, or with over_all their part of the softmax over all.  A logit of -inf is never chosen: the choice is -1 then, its weight 0."""
+    _unrecorded(logits, weight)
+    ldl = _check("logits", logits, tuple(_TYPES), (None, None), rows=True)
+    tokens, experts = int(logits.shape[0]), int(logits.shape[1])
+    expert = torch.empty((tokens, k), dtype=torch.int32, device=logits.device) if expert is None else expert
+    weight = torch.empty((tokens, k), dtype=torch.float32, device=logits.device) if weight is None else weight
+    _check("expert", expert, (torch.int32,), (tokens, k), logits.device)
+    _check("weight", weight, (torch.float32,), (tokens, k), logits.device)
+    _call("pcc_route", logits.device, logits.data_ptr(), ldl, tokens, experts, k, _TYPES[logits.dtype], int(over_all), expert.data_ptr(), weight.data_ptr())
+    return expert, weight
+
+
+def pcc_route_grad(dweight: torch.Tensor, logits: torch.Tensor, expert: torch.Tensor, weight: torch.Tensor, over_all: bool = False,
+                   dlogits: torch.Tensor | None = None) -> torch.Tensor:
+    """The logits' gradient, of their type, from that of the weights fp32 [tokens, k] and what pcc_route gave."""
+    _unrecorded(dweight, logits, weight, dlogits)
+    ldl = _check("logits", logits, tuple(_TYPES), (None, None), rows=True)
+    tokens, experts = int(logits.shape[0]), int(logits.shape[1])
+    _check("expert", expert, (torch.int32,), (tokens, None), logits.device)
+    k = int(expert.shape[1])
+    _check("weight", weight, (torch.float32,), (tokens, k), logits.device)
+    _check("dweight", dweight, (torch.float32,), (tokens, k), logits.device)
+    dlogits = torch.empty((tokens, experts), dtype=logits.dtype, device=logits.device) if dlogits is None else dlogits
+    lddl = _check("dlogits", dlogits, (logits.dtype,), (tokens, experts), logits.device, rows=True)
+    _call("pcc_route_grad", logits.device, dweight.data_ptr(), logits.data_ptr(), ldl, expert.data_ptr(), weight.data_ptr(), tokens, experts, k,
+          _TYPES[logits.dtype], int(over_all), dlogits.data_ptr(), lddl)
+    return dlogits
+
+
+def pcc_expert_sort(expert: torch.Tensor, experts: int, offsets: torch.Tensor | None = None, place: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None):
+    """(offsets int64 [experts + 1], place int32 [tokens, k]): the rows of the choices expert int32 [tokens, k], sorted by expert and within one by
+    token.  A choice outside 0..experts - 1 has place -1."""
+    _check("expert", expert, (torch.int32,), (None, None))
+    tokens, k = int(expert.shape[0]), int(expert.shape[1])
+    offsets = torch.empty(experts + 1, dtype=torch.int64, device=expert.device) if offsets is None else offsets
+    place = torch.empty((tokens, k), dtype=torch.int32, device=expert.device) if place is None else place
+    _check("offsets", offsets, (torch.int64,), (experts + 1,), expert.device)
+    _check("place", place, (torch.int32,), (tokens, k), expert.device)
+    if workspace is None:
+        need = int((_lib or load()).pcc_expert_sort_workspace_bytes(tokens, k, experts))
+        workspace = torch.empty(need, dtype=torch.uint8, device=expert.device) if need else None
+    else:
+        _check("workspace", workspace, (torch.uint8,), (None,), expert.device)
+    _call("pcc_expert_sort", expert.device, expert.data_ptr(), tokens, k, experts, offsets.data_ptr(), place.data_ptr(), _ptr(workspace),
+          workspace.numel() if workspace is not None else 0)
+    return offsets, place
+
+
+def _check_place(place, device):
+    _check("place", place, (torch.int32,), (None, None), device)
+    return int(place.shape[0]), int(place.shape[1])
+
+
+def pcc_expert_rows(x: torch.Tensor, place: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Rows of each expert, one behind the other: out[place[t, j]] = x[t].  out [rows, features] has tokens * k rows by default; rows that no choice has
+    are left as they are in `out`, and undefined in a new tensor.  (The gradient is pcc_expert_join without weights.)"""
+    _unrecorded(x, out)
+    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    tokens, k = _check_place(place, x.device)
+    features = int(x.shape[1])
+    if int(x.shape[0]) != tokens:
+        raise ValueError("x and place must have one row for each token")
+    out = torch.empty((tokens * k, features), dtype=x.dtype, device=x.device) if out is None else out
+    ldr = _check("out", out, (x.dtype,), (None, features), x.device, rows=True)
+    _call("pcc_expert_rows", x.device, x.data_ptr(), ldx, place.data_ptr(), tokens, k, out.shape[0], features, _TYPES[x.dtype], out.data_ptr(), ldr)
+    return out
+
+
+def pcc_expert_join(z: torch.Tensor, place: torch.Tensor, weight: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                    out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """y[t] = sum over j of weight[t, j] z[place[t, j]] (None: weights of 1), summed in fp32.  z [rows, features]; y has its type or fp32."""
+    _unrecorded(z, weight, out)
+    ldz = _check("z", z, tuple(_TYPES), (None, None), rows=True)
+    tokens, k = _check_place(place, z.device)
+    rows, features = int(z.shape[0]), int(z.shape[1])
+    if weight is not None:
+        _check("weight", weight, (torch.float32,), (tokens, k), z.device)
+    out = torch.empty((tokens, features), dtype=out_dtype or z.dtype, device=z.device) if out is None else out
+    ldy = _check("out", out, (z.dtype, torch.float32) if out_dtype is None else (out_dtype,), (tokens, features), z.device, rows=True)
+    _call("pcc_expert_join", z.device, z.data_ptr(), ldz, place.data_ptr(), _ptr(weight), tokens, k, rows, features, _TYPES[z.dtype], out.data_ptr(),
+          _TYPES[out.dtype], ldy)
+    return out
+
+
+def pcc_expert_join_grad(dy: torch.Tensor, z: torch.Tensor, place: torch.Tensor, weight: torch.Tensor | None = None, dz: torch.Tensor | None = None,
+                         want_dweight: bool = True, dweight: torch.Tensor | None = None):
+    """(dz, dweight) of pcc_expert_join: dz has z's type, dweight fp32 [tokens, k] (None without want_dweight).  Rows that no choice has are left as they are
+    in `dz`, and undefined in a new tensor."""
+    _unrecorded(dy, z, weight, dz, dweight)
+    ldz = _check("z", z, tuple(_TYPES), (None, None), rows=True)
+    tokens, k = _check_place(place, z.device)
+    rows, features = int(z.shape[0]), int(z.shape[1])
+    lddy = _check("dy", dy, (z.dtype, torch.float32), (tokens, features), z.device, rows=True)
+    if weight is not None:
+        _check("weight", weight, (torch.float32,), (tokens, k), z.device)
+    dz = torch.empty((rows, features), dtype=z.dtype, device=z.device) if dz is None else dz
+    lddz = _check("dz", dz, (z.dtype,), (rows, features), z.device, rows=True)
+    if want_dweight:
+        dweight = torch.empty((tokens, k), dtype=torch.float32, device=z.device) if dweight is None else dweight
+        _check("dweight", dweight, (torch.float32,), (tokens, k), z.device)
+    _call("pcc_expert_join_grad", z.device, dy.data_ptr(), _TYPES[dy.dtype], lddy, z.data_ptr(), ldz, place.data_ptr(), _ptr(weight), tokens, k, rows, features,
+          _TYPES[z.dtype], dz.data_ptr(), lddz, dweight.data_ptr() if want_dweight else None)
+    return dz, (dweight if want_dweight else None)
+
+
+def pcc_dropout(x: torch.Tensor, p: float, seed: int, step: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """residual + x / (1 - p) for the elements of x [rows, features] that are kept, residual (None: 0) for the others.  Which ones is a function of seed
+    (64 bits), step (int64 [1] on the device, None: 0), row and column alone: the same call on the gradient is the backward pass.  p is taken to the
+    nearest 1/65536.  The result has x's type, or one of the two is fp32; residual has the result's.  `out` may be x or residual."""
+    _unrecorded(x, residual, out)
+    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    shape = (int(x.shape[0]), int(x.shape[1]))
+    if not 0 <= seed < 1 << 64:
+        raise ValueError("seed must be a whole number of 64 bits")
+    if step is not None:
+        _check("step", step, (torch.int64,), (1,), x.device)
+    out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device) if out is None else out
+    ldy = _check("out", out, (tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype, torch.float32)) if out_dtype is None else (out_dtype,), shape, x.device, rows=True)
+    ldr = _check("residual", residual, (out.dtype,), shape, x.device, rows=True) if residual is not None else shape[1]
+    _call("pcc_dropout", x.device, x.data_ptr(), ldx, _ptr(residual), ldr, shape[0], shape[1], _TYPES[x.dtype], p, seed, _ptr(step), out.data_ptr(),
+          _TYPES[out.dtype], ldy)
+    return out
 
 
 class AdamW:

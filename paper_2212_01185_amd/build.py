@@ -4,11 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "pcc.hip")                # the codec
 TRAIN_SRC = os.path.join(_HERE, "csrc", "pcc_train.hip")    # the operators of a training step
+ROUTED_SRC = os.path.join(_HERE, "csrc", "pcc_routed.hip")  # the operators round the grouped products
 LIB = os.path.join(_HERE, "libpcc.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -26,22 +28,37 @@ FLAGS = [
 ]
 
 
-def build(verbose: bool = False, extra=(), lib: str = LIB, src=(SRC, TRAIN_SRC)) -> str:
+def _start(cmd, verbose: bool):
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(process):
+    out, _ = process.communicate()
+    return process.returncode, "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
+
+
+def build(verbose: bool = False, extra=(), lib: str = LIB, src=(SRC, TRAIN_SRC, ROUTED_SRC)) -> str:
     """Compile the library to `lib` (default: libpcc.so next to the package).  `extra` are more hipcc flags, e.g.
     -DPCC_PHASE_TIMING for the measurement build that counts the decode step's cycles per phase.  `src` is another HIP
     source, or several, to compile with the library's flags."""
     LIB = lib
     os.makedirs(os.path.dirname(os.path.abspath(LIB)), exist_ok=True)
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + list(extra) + ["-o", tmp] + ([src] if isinstance(src, str) else list(src))
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    sources = [src] if isinstance(src, str) else list(src)
+    # each source by itself, side by side, then all together
+    with tempfile.TemporaryDirectory(dir=os.path.dirname(os.path.abspath(LIB))) as d:
+        objects = [os.path.join(d, "%d.o" % i) for i in range(len(sources))]
+        running = [_start([HIPCC] + [f for f in FLAGS if f != "-shared"] + list(extra) + ["-c", "-o", o, s], verbose) for o, s in zip(objects, sources)]
+        out = [_finish(p) for p in running]
+        if all(rc == 0 for rc, _ in out):
+            out.append(_finish(_start([HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared"] + list(extra) + ["-o", tmp] + objects, verbose)))
+    text = "\n".join(t for _, t in out if t)
+    if any(rc != 0 for rc, _ in out):
+        raise RuntimeError("hipcc failed:\n" + text)
+    if verbose and text.strip():
+        print(text)
     os.replace(tmp, LIB)
     return LIB
 

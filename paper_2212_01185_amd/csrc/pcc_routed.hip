@@ -1,0 +1,365 @@
+// Host side of the operators of include/pcc.h that stand round the grouped products: layer norm, routing, rows by expert, dropout.
+#include "pcc.h"
+#include "train_dropout.h"
+#include "train_experts.h"
+#include "train_host.h"
+#include "train_norm.h"
+#include "train_route.h"
+
+using namespace pcc_train;
+
+namespace {
+
+bool type_ok(int type) { return type >= PCC_BF16 && type <= PCC_FP32; }
+Span matrix(const void* p, size_t rows, size_t ld, size_t features, int type) { return {p, rows, ld * size_of(type), features * size_of(type)}; }
+
+// f(type of the rows) and f(type, other type), as tags.
+template <class F>
+int with_type(int type, F&& f) { return type == PCC_BF16 ? f(Bf16{}) : type == PCC_FP16 ? f(Fp16{}) : f(Fp32{}); }
+
+// ---------------------------------------------------------------------------
+// Layer norm.
+// ---------------------------------------------------------------------------
+template <int LANES, int N>
+struct RowShape {
+    static constexpr int kLanes = LANES, kChunks = N;
+};
+// How many lanes have a row, and how many eights of it each.
+template <class F>
+int with_row_shape(int features, F&& f) {
+    const int chunks = (features + 7) / 8;
+    if (chunks <= 8) return f(RowShape<4, 2>{});
+    if (chunks <= 24) return f(RowShape<4, 6>{});
+    if (chunks <= 32) return f(RowShape<8, 4>{});
+    if (chunks <= 64) return f(RowShape<16, 4>{});
+    if (chunks <= 128) return f(RowShape<32, 4>{});
+    if (chunks <= 256) return f(RowShape<64, 4>{});
+    if (chunks <= 512) return f(RowShape<128, 4>{});
+    if (chunks <= 1024) return f(RowShape<256, 4>{});
+    if (chunks <= 2048) return f(RowShape<512, 4>{});
+    return f(RowShape<kLongThreads, 0>{});      // read again for each sum
+}
+// x and y have one type, or x is fp32 and y a 16-bit one.
+template <class F>
+int with_norm_types(int type, int y_type, F&& f) {
+    if (type == PCC_BF16) return f(Bf16{}, Bf16{});
+    if (type == PCC_FP16) return f(Fp16{}, Fp16{});
+    return y_type == PCC_BF16 ? f(Fp32{}, Bf16{}) : y_type == PCC_FP16 ? f(Fp32{}, Fp16{}) : f(Fp32{}, Fp32{});
+}
+bool norm_ok(const int64_t* d_offsets, int groups, size_t rows, int features, int type, int y_type) {
+    return type_ok(type) && type_ok(y_type) && (type == y_type || type == PCC_FP32) && features >= 1 && features <= PCC_MAX_FEATURES && groups >= 1 &&
+           groups <= PCC_MAX_GROUPS && rows <= kMaxRows && (d_offsets || groups == 1) && aligned(d_offsets, 8);
+}
+int log2_of(int v) { return v <= 1 ? 0 : 1 + log2_of(v / 2); }
+
+// Rows of the chunks whose sums are joined.
+void sums_chunks(size_t rows, int groups, int& log2, uint32_t& mult) { chunk_rows((int64_t)rows, groups, 512, 3, log2, mult); }
+
+}  // namespace
+
+extern "C" {
+
+int pcc_layer_norm(const void* d_x, size_t ldx, const float* d_gamma, const float* d_beta, const int64_t* d_offsets, int groups, size_t rows,
+                   int features, float eps, int type, void* d_y, int y_type, size_t ldy, float* d_stats, void* hip_stream) {
+    if ((rows && (!d_x || !d_y)) || !norm_ok(d_offsets, groups, rows, features, type, y_type) || !ld_ok(ldx, features) || !ld_ok(ldy, features)) return PCC_E_ARG;
+    if (!(eps >= 0x1p-126f && eps < __builtin_inff())) return PCC_E_ARG;
+    if (!aligned(d_x, size_of(type)) || !aligned(d_y, size_of(y_type)) || !aligned(d_gamma, 4) || !aligned(d_beta, 4) || !aligned(d_stats, 4)) return PCC_E_ARG;
+    if (rows == 0) return PCC_OK;
+    const size_t weights = (size_t)groups * features * 4;
+    const Span x = matrix(d_x, rows, ldx, features, type), gamma = piece(d_gamma, weights), beta = piece(d_beta, weights),
+               offsets = piece(d_offsets, (size_t)(groups + 1) * 8), y = matrix(d_y, rows, ldy, features, y_type), stats = piece(d_stats, rows * 8);
+    if (overlap(y, {x, gamma, beta, offsets, stats}) || overlap(stats, {x, gamma, beta, offsets})) return PCC_E_ARG;
+    Norm a = {};
+    a.x = d_x; a.gamma = d_gamma; a.beta = d_beta; a.off = d_offsets; a.y = d_y; a.stats = d_stats;
+    a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.eps = eps; a.inverse = 1.0f / (float)features;
+    return with_row_shape(features, [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        chunk_rows(a.rows, groups, 2048, log2_of(norm_teams(L)), a.log2, a.mult);
+        const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+        if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
+        return with_norm_types(type, y_type, [&](auto tx, auto ty) {
+            return launch([&] {
+                const dim3 grid((uint32_t)((blocks + 7) / 8 * 8)), threads(norm_threads(L));
+                if constexpr (N == 0) hipLaunchKernelGGL((layer_norm_long_kernel<decltype(tx), decltype(ty)>), grid, threads, 0, (hipStream_t)hip_stream, a);
+                else hipLaunchKernelGGL((layer_norm_kernel<decltype(tx), decltype(ty), L, N>), grid, threads, 0, (hipStream_t)hip_stream, a);
+            });
+        });
+    });
+}
+
+size_t pcc_layer_norm_grad_workspace_bytes(size_t rows, int groups, int features) {
+    if (features < 1 || features > PCC_MAX_FEATURES || groups < 1 || groups > PCC_MAX_GROUPS || rows > kMaxRows) return 0;
+    int log2;
+    uint32_t mult;
+    sums_chunks(rows, groups, log2, mult);
+    return shared_chunks(rows, groups, (size_t)mult << log2) * 2 * features * sizeof(float);
+}
+
+int pcc_layer_norm_grad(const void* d_dy, int y_type, size_t lddy, const void* d_x, size_t ldx, const float* d_stats, const float* d_gamma,
+                        const int64_t* d_offsets, int groups, size_t rows, int features, int type, void* d_dx, size_t lddx, float* d_dgamma,
+                        float* d_dbeta, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+    if ((rows && (!d_dy || !d_x || !d_stats)) || (!d_dx && !d_dgamma) || !d_dgamma != !d_dbeta) return PCC_E_ARG;
+    if (!norm_ok(d_offsets, groups, rows, features, type, y_type) || !ld_ok(lddy, features) || !ld_ok(ldx, features) || (d_dx && !ld_ok(lddx, features))) return PCC_E_ARG;
+    if (!aligned(d_dy, size_of(y_type)) || !aligned(d_x, size_of(type)) || !aligned(d_dx, size_of(type)) || !aligned(d_stats, 4) || !aligned(d_gamma, 4) ||
+        !aligned(d_dgamma, 4) || !aligned(d_dbeta, 4)) return PCC_E_ARG;
+    const size_t need = d_dgamma ? pcc_layer_norm_grad_workspace_bytes(rows, groups, features) : 0;
+    if (need && (!d_workspace || workspace_bytes < need)) return PCC_E_SCRATCH;
+    if (need && !aligned(d_workspace, 16)) return PCC_E_ARG;
+    const size_t weights = (size_t)groups * features * 4;
+    const Span dy = matrix(d_dy, rows, lddy, features, y_type), x = matrix(d_x, rows, ldx, features, type), stats = piece(d_stats, rows * 8),
+               gamma = piece(d_gamma, weights), offsets = piece(d_offsets, (size_t)(groups + 1) * 8), dx = matrix(d_dx, rows, lddx, features, type),
+               dgamma = piece(d_dgamma, weights), dbeta = piece(d_dbeta, weights), space = piece(d_workspace, need);
+    if (overlap(dx, {dy, x, stats, gamma, offsets, dgamma, dbeta, space}) || overlap(dgamma, {dy, x, stats, gamma, offsets, dbeta, space}) ||
+        overlap(dbeta, {dy, x, stats, gamma, offsets, space}) || overlap(space, {dy, x, stats, gamma, offsets})) return PCC_E_ARG;
+    Norm a = {};
+    a.x = d_x; a.dy = d_dy; a.gamma = d_gamma; a.off = d_offsets; a.y = d_dx; a.stats = const_cast<float*>(d_stats); a.dgamma = d_dgamma; a.dbeta = d_dbeta;
+    a.partial = (float*)d_workspace;
+    a.ldx = ldx; a.lddy = lddy; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.inverse = 1.0f / (float)features;
+    a.shared_max = (uint32_t)std::min<size_t>(need / (2 * features * sizeof(float)), 0xFFFFFFFFu);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (d_dx && rows) {
+        const int rc = with_row_shape(features, [&](auto shape) {
+            constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+            chunk_rows(a.rows, groups, 2048, log2_of(norm_teams(L)), a.log2, a.mult);
+            const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+            if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
+            return with_norm_types(type, y_type, [&](auto tx, auto ty) {
+                return launch([&] {
+                    const dim3 grid((uint32_t)((blocks + 7) / 8 * 8)), threads(norm_threads(L));
+                    if constexpr (N == 0) hipLaunchKernelGGL((layer_norm_long_dx_kernel<decltype(tx), decltype(ty)>), grid, threads, 0, st, a);
+                    else hipLaunchKernelGGL((layer_norm_dx_kernel<decltype(tx), decltype(ty), L, N>), grid, threads, 0, st, a);
+                });
+            });
+        });
+        if (rc != PCC_OK) return rc;
+    }
+    if (!d_dgamma) return PCC_OK;
+    sums_chunks(rows, groups, a.log2, a.mult);
+    const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+    if (!launchable(blocks, 256)) return PCC_E_ARG;
+    const int rc = with_norm_types(type, y_type, [&](auto tx, auto ty) {
+        return launch([&] {
+            hipLaunchKernelGGL((layer_norm_sums_kernel<decltype(tx), decltype(ty)>), dim3((uint32_t)((blocks + 7) / 8 * 8), std::min((features + 255) / 256, 8)), dim3(256), 0, st, a);
+        });
+    });
+    if (rc != PCC_OK || rows <= (size_t)a.mult << a.log2) return rc;        // no group can have two chunks
+    return launch([&] {
+        hipLaunchKernelGGL(layer_norm_join_kernel, dim3(std::min((2 * features + 63) / 64, std::max(4, 4096 / groups)), groups), dim3(256), 0, st, a);
+    });
+}
+
+// ---------------------------------------------------------------------------
+// Routing.
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+bool choices_ok(size_t tokens, int k, int experts) {
+    return k >= 1 && k <= PCC_MAX_CHOICES && experts >= 1 && experts <= PCC_MAX_EXPERTS && tokens < ((size_t)1 << 31) / k;
+}
+template <class F>
+int with_lanes(int experts, F&& f) {
+    const int chunks = (experts + 7) / 8;
+    if (chunks <= 1) return f(RowShape<1, 1>{});
+    if (chunks <= 2) return f(RowShape<2, 1>{});
+    if (chunks <= 4) return f(RowShape<4, 1>{});
+    if (chunks <= 8) return f(RowShape<8, 1>{});
+    if (chunks <= 16) return f(RowShape<16, 1>{});
+    if (chunks <= 32) return f(RowShape<32, 1>{});
+    if (chunks <= 64) return f(RowShape<64, 1>{});
+    return f(RowShape<64, 2>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int pcc_route(const void* d_logits, size_t ldl, size_t tokens, int experts, int k, int type, int over_all, int32_t* d_expert, float* d_weight,
+              void* hip_stream) {
+    if ((tokens && (!d_logits || !d_expert || !d_weight)) || !choices_ok(tokens, k, experts) || k > experts || !type_ok(type) || !ld_ok(ldl, experts)) return PCC_E_ARG;
+    if ((over_all != 0 && over_all != 1) || !aligned(d_logits, size_of(type)) || !aligned(d_expert, 4) || !aligned(d_weight, 4)) return PCC_E_ARG;
+    if (tokens == 0) return PCC_OK;
+    const Span logits = matrix(d_logits, tokens, ldl, experts, type), expert = piece(d_expert, tokens * k * 4), weight = piece(d_weight, tokens * k * 4);
+    if (overlap(expert, {logits, weight}) || overlap(weight, logits)) return PCC_E_ARG;
+    Route a = {};
+    a.logits = d_logits; a.expert = d_expert; a.weight = d_weight; a.ldl = ldl; a.tokens = tokens; a.experts = experts; a.k = k; a.over_all = over_all;
+    return with_lanes(experts, [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        const uint64_t blocks = (tokens + kRouteThreads / L - 1) / (kRouteThreads / L);
+        if (!launchable(blocks, kRouteThreads)) return PCC_E_ARG;
+        return with_type(type, [&](auto t) {
+            return launch([&] { hipLaunchKernelGGL((route_kernel<decltype(t), L, N>), dim3((uint32_t)blocks), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, a); });
+        });
+    });
+}
+
+int pcc_route_grad(const float* d_dweight, const void* d_logits, size_t ldl, const int32_t* d_expert, const float* d_weight, size_t tokens, int experts,
+                   int k, int type, int over_all, void* d_dlogits, size_t lddl, void* hip_stream) {
+    if ((tokens && (!d_dweight || (over_all && !d_logits) || !d_expert || !d_weight || !d_dlogits)) || !choices_ok(tokens, k, experts) || k > experts) return PCC_E_ARG;
+    if (!type_ok(type) || !ld_ok(ldl, experts) || !ld_ok(lddl, experts) || (over_all != 0 && over_all != 1)) return PCC_E_ARG;
+    if (!aligned(d_dweight, 4) || !aligned(d_logits, size_of(type)) || !aligned(d_expert, 4) || !aligned(d_weight, 4) || !aligned(d_dlogits, size_of(type))) return PCC_E_ARG;
+    if (tokens == 0) return PCC_OK;
+    const size_t chosen = tokens * k * 4;
+    if (overlap(matrix(d_dlogits, tokens, lddl, experts, type),
+                {matrix(d_logits, tokens, ldl, experts, type), piece(d_dweight, chosen), piece(d_expert, chosen), piece(d_weight, chosen)})) return PCC_E_ARG;
+    Route a = {};
+    a.logits = d_logits; a.dweight = d_dweight; a.expert = const_cast<int32_t*>(d_expert); a.weight = const_cast<float*>(d_weight); a.dlogits = d_dlogits;
+    a.ldl = ldl; a.lddl = lddl; a.tokens = tokens; a.experts = experts; a.k = k; a.over_all = over_all;
+    return with_lanes(experts, [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        const uint64_t blocks = (tokens + kRouteThreads / L - 1) / (kRouteThreads / L);
+        if (!launchable(blocks, kRouteThreads)) return PCC_E_ARG;
+        return with_type(type, [&](auto t) {
+            return launch([&] { hipLaunchKernelGGL((route_grad_kernel<decltype(t), L, N>), dim3((uint32_t)blocks), dim3(kRouteThreads), 0, (hipStream_t)hip_stream, a); });
+        });
+    });
+}
+
+// ---------------------------------------------------------------------------
+// Rows by expert.
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+// Segments of the sort: whole rounds of its waves, as many as there are workgroups of 1024 threads on the chip at most.
+uint32_t sort_segment(size_t entries) {
+    const size_t least = (entries + 255) / 256;
+    return (uint32_t)std::max<size_t>(4096, (least + 1023) / 1024 * 1024);
+}
+uint32_t sort_segments(size_t entries) { return (uint32_t)std::max<size_t>(1, (entries + sort_segment(entries) - 1) / sort_segment(entries)); }
+
+// Rows of `features` values, their places and weights.
+bool rows_ok(size_t tokens, int k, size_t rows, int features, int type) {
+    return k >= 1 && k <= PCC_MAX_CHOICES && tokens < ((size_t)1 << 31) / k && rows < (size_t)1 << 31 && features >= 1 && features <= PCC_MAX_FEATURES && type_ok(type);
+}
+// The tokens' side has the rows' type or fp32.
+template <class F>
+int with_row_types(int type, int y_type, F&& f) {
+    if (type == PCC_BF16) return y_type == PCC_BF16 ? f(Bf16{}, Bf16{}) : f(Bf16{}, Fp32{});
+    if (type == PCC_FP16) return y_type == PCC_FP16 ? f(Fp16{}, Fp16{}) : f(Fp16{}, Fp32{});
+    return f(Fp32{}, Fp32{});
+}
+uint64_t chunk_blocks(uint64_t rows, uint32_t chunks, int threads) { return (rows * chunks + threads - 1) / threads; }
+
+}  // namespace
+
+extern "C" {
+
+size_t pcc_expert_sort_workspace_bytes(size_t tokens, int k, int experts) {
+    if (!choices_ok(tokens, k, experts)) return 0;
+    const uint32_t segments = sort_segments(tokens * k);
+    return segments > 1 ? (size_t)segments * experts * sizeof(uint32_t) : 0;
+}
+
+int pcc_expert_sort(const int32_t* d_expert, size_t tokens, int k, int experts, int64_t* d_offsets, int32_t* d_place, void* d_workspace,
+                    size_t workspace_bytes, void* hip_stream) {
+    if ((tokens && (!d_expert || !d_place)) || !d_offsets || !choices_ok(tokens, k, experts)) return PCC_E_ARG;
+    if (!aligned(d_expert, 4) || !aligned(d_place, 4) || !aligned(d_offsets, 8)) return PCC_E_ARG;
+    const size_t need = pcc_expert_sort_workspace_bytes(tokens, k, experts);
+    if (need && (!d_workspace || workspace_bytes < need)) return PCC_E_SCRATCH;
+    if (need && !aligned(d_workspace, 16)) return PCC_E_ARG;
+    const size_t entries = tokens * k;
+    const Span expert = piece(d_expert, entries * 4), place = piece(d_place, entries * 4), offsets = piece(d_offsets, (size_t)(experts + 1) * 8),
+               space = piece(d_workspace, need);
+    if (overlap(place, {expert, offsets, space}) || overlap(offsets, {expert, space}) || overlap(space, expert)) return PCC_E_ARG;
+    Sort a = {};
+    a.expert = d_expert; a.offsets = d_offsets; a.place = d_place; a.counts = (uint32_t*)d_workspace;
+    a.entries = (uint32_t)entries; a.segment = sort_segment(entries); a.segments = sort_segments(entries); a.experts = experts; a.bits = log2_of(experts) + 1;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (a.segments > 1) {
+        const int rc = launch([&] { hipLaunchKernelGGL(expert_count_kernel, dim3(a.segments), dim3(kSortThreads), (size_t)experts * sizeof(uint32_t), st, a); });
+        if (rc != PCC_OK) return rc;
+    }
+    const size_t lds = sort_lds(experts);
+    if (!allow_lds(expert_place_kernel, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
+    return launch([&] { hipLaunchKernelGGL(expert_place_kernel, dim3(a.segments), dim3(kSortThreads), lds, st, a); });
+}
+
+int pcc_expert_rows(const void* d_x, size_t ldx, const int32_t* d_place, size_t tokens, int k, size_t rows, int features, int type, void* d_rows,
+                    size_t ldr, void* hip_stream) {
+    if ((tokens && (!d_x || !d_place)) || (tokens && rows && !d_rows) || !rows_ok(tokens, k, rows, features, type) || !ld_ok(ldx, features) || !ld_ok(ldr, features)) return PCC_E_ARG;
+    if (!aligned(d_x, size_of(type)) || !aligned(d_rows, size_of(type)) || !aligned(d_place, 4)) return PCC_E_ARG;
+    if (tokens == 0 || rows == 0) return PCC_OK;
+    if (overlap(matrix(d_rows, rows, ldr, features, type), {matrix(d_x, tokens, ldx, features, type), piece(d_place, tokens * k * 4)})) return PCC_E_ARG;
+    Experts a = {};
+    a.x = d_x; a.place = d_place; a.y = d_rows; a.ldx = ldx; a.ldy = ldr; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
+    a.chunks = (uint32_t)(features + 7) / 8;
+    const uint64_t blocks = chunk_blocks(tokens, a.chunks, kExpertThreads);
+    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
+    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); }); };
+    return type == PCC_FP32 ? go(expert_rows_kernel<Fp32>) : go(expert_rows_kernel<Bf16>);      // bits are copied
+}
+
+int pcc_expert_join(const void* d_z, size_t ldz, const int32_t* d_place, const float* d_weight, size_t tokens, int k, size_t rows, int features, int type,
+                    void* d_y, int y_type, size_t ldy, void* hip_stream) {
+    if ((tokens && (!d_place || !d_y)) || (tokens && rows && !d_z) || !rows_ok(tokens, k, rows, features, type) || (y_type != type && y_type != PCC_FP32)) return PCC_E_ARG;
+    if (!ld_ok(ldz, features) || !ld_ok(ldy, features) || !aligned(d_z, size_of(type)) || !aligned(d_y, size_of(y_type)) || !aligned(d_place, 4) || !aligned(d_weight, 4)) return PCC_E_ARG;
+    if (tokens == 0) return PCC_OK;
+    if (overlap(matrix(d_y, tokens, ldy, features, y_type), {matrix(d_z, rows, ldz, features, type), piece(d_place, tokens * k * 4), piece(d_weight, tokens * k * 4)})) return PCC_E_ARG;
+    Experts a = {};
+    a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_y; a.ldz = ldz; a.ldy = ldy; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
+    a.chunks = (uint32_t)(features + 7) / 8;
+    const uint64_t blocks = chunk_blocks(tokens, a.chunks, kExpertThreads);
+    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
+    return with_row_types(type, y_type, [&](auto t, auto ty) {
+        return launch([&] {
+            hipLaunchKernelGGL((expert_join_kernel<decltype(t), decltype(ty)>), dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a);
+        });
+    });
+}
+
+int pcc_expert_join_grad(const void* d_dy, int y_type, size_t lddy, const void* d_z, size_t ldz, const int32_t* d_place, const float* d_weight,
+                         size_t tokens, int k, size_t rows, int features, int type, void* d_dz, size_t lddz, float* d_dweight, void* hip_stream) {
+    if ((tokens && (!d_dy || !d_place || (!d_dz && !d_dweight))) || (tokens && rows && d_dweight && !d_z) || !rows_ok(tokens, k, rows, features, type)) return PCC_E_ARG;
+    if ((y_type != type && y_type != PCC_FP32) || !ld_ok(lddy, features) || (d_dweight && !ld_ok(ldz, features)) || (d_dz && !ld_ok(lddz, features))) return PCC_E_ARG;
+    if (!aligned(d_dy, size_of(y_type)) || !aligned(d_z, size_of(type)) || !aligned(d_dz, size_of(type)) || !aligned(d_place, 4) || !aligned(d_weight, 4) ||
+        !aligned(d_dweight, 4)) return PCC_E_ARG;
+    if (tokens == 0) return PCC_OK;
+    const Span dy = matrix(d_dy, tokens, lddy, features, y_type), z = matrix(d_dweight ? d_z : nullptr, rows, ldz, features, type), place = piece(d_place, tokens * k * 4),
+               weight = piece(d_weight, tokens * k * 4), dz = matrix(d_dz, rows, lddz, features, type), dweight = piece(d_dweight, tokens * k * 4);
+    if (overlap(dz, {dy, z, place, weight, dweight}) || overlap(dweight, {dy, z, place, weight})) return PCC_E_ARG;
+    Experts a = {};
+    a.x = d_dy; a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_dz; a.dweight = d_dweight;
+    a.ldx = lddy; a.ldz = ldz; a.ldy = lddz; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
+    const uint64_t blocks = (tokens + kExpertThreads / 64 - 1) / (kExpertThreads / 64);
+    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
+    return with_row_types(type, y_type, [&](auto t, auto ty) {
+        return launch([&] {
+            hipLaunchKernelGGL((expert_join_grad_kernel<decltype(t), decltype(ty)>), dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a);
+        });
+    });
+}
+
+// ---------------------------------------------------------------------------
+// Dropout.
+// ---------------------------------------------------------------------------
+int pcc_dropout(const void* d_x, size_t ldx, const void* d_residual, size_t ldr, size_t rows, int features, int type, double p, uint64_t seed,
+                const int64_t* d_step, void* d_y, int y_type, size_t ldy, void* hip_stream) {
+    if ((rows && (!d_x || !d_y)) || rows > kMaxRows || features < 1 || features > PCC_MAX_FEATURES || !(p >= 0.0 && p <= 1.0)) return PCC_E_ARG;
+    if (!type_ok(type) || !type_ok(y_type) || (type != y_type && type != PCC_FP32 && y_type != PCC_FP32)) return PCC_E_ARG;
+    if (!ld_ok(ldx, features) || !ld_ok(ldy, features) || (d_residual && !ld_ok(ldr, features))) return PCC_E_ARG;
+    if (!aligned(d_x, size_of(type)) || !aligned(d_residual, size_of(y_type)) || !aligned(d_y, size_of(y_type)) || !aligned(d_step, 8)) return PCC_E_ARG;
+    if (rows == 0) return PCC_OK;
+    const Span x = matrix(d_x, rows, ldx, features, type), residual = matrix(d_residual, rows, ldr, features, y_type), y = matrix(d_y, rows, ldy, features, y_type);
+    // an element is read before it is written, by the same thread
+    const bool over_x = d_y == d_x && type == y_type && ldx == ldy, over_residual = d_y == d_residual && ldr == ldy;
+    if ((!over_x && overlap(y, x)) || (!over_residual && overlap(y, residual)) || overlap(y, piece(d_step, 8))) return PCC_E_ARG;
+    Dropout a = {};
+    a.x = d_x; a.residual = d_residual; a.y = d_y; a.ldx = ldx; a.ldr = ldr; a.ldy = ldy; a.rows = rows; a.seed = seed; a.step = d_step;
+    a.border = (uint32_t)(p * 65536.0 + 0.5);
+    a.scale = a.border < 65536 ? (float)(65536.0 / (65536 - a.border)) : 0.0f;
+    a.features = features;
+    a.chunks = (uint32_t)(features + 7) / 8;
+    const uint64_t blocks = chunk_blocks(rows, a.chunks, kDropoutThreads);
+    if (!launchable(blocks, kDropoutThreads)) return PCC_E_ARG;
+    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(kDropoutThreads), 0, (hipStream_t)hip_stream, a); }); };
+    return with_type(type, [&](auto t) {
+        using T = decltype(t);
+        if constexpr (kIs32<T>) return y_type == PCC_BF16 ? go(dropout_kernel<Fp32, Bf16>) : y_type == PCC_FP16 ? go(dropout_kernel<Fp32, Fp16>) : go(dropout_kernel<Fp32, Fp32>);
+        else return y_type == PCC_FP32 ? go(dropout_kernel<T, Fp32>) : go(dropout_kernel<T, T>);
+    });
+}
+
+}  // extern "C"

@@ -1,6 +1,5 @@
 // Host side of the training operators of include/pcc.h.
 #include <algorithm>
-#include <initializer_list>
 #include <iterator>
 #include <new>
 #include <utility>
@@ -10,6 +9,7 @@
 #include "train_adamw.h"
 #include "train_contexts.h"
 #include "train_grouped.h"
+#include "train_host.h"
 #include "train_loss.h"
 #include "train_narrow.h"
 
@@ -17,59 +17,12 @@ using namespace pcc_train;
 
 namespace {
 
-// The status of a launch.  An error that another call left is not this one's: it is taken away before.
-template <class F>
-int launch(F&& f) {
-    (void)hipGetLastError();
-    f();
-    return hipGetLastError() == hipSuccess ? PCC_OK : PCC_E_HIP;
-}
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = hipSetDevice(dev) == hipSuccess;
-    }
-    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
-};
-
-constexpr size_t kMaxLd = (size_t)1 << 22;
-constexpr size_t kMaxRows = (size_t)1 << 40;
-
-// A launch has fewer than 2^32 threads (some grids are rounded up to a multiple of eight workgroups).
-bool launchable(uint64_t blocks, int threads) { return blocks < ((uint64_t)1 << 32) / threads - 8; }
-
-bool aligned(const void* p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
-size_t size_of(int type) { return type == PCC_FP32 ? 4 : 2; }
-
-// `count` rows of `length` bytes, `pitch` apart; what is one piece is one row.
-struct Span {
-    const void* p;
-    size_t count, pitch, length;
-};
-Span piece(const void* p, size_t bytes) { return {p, 1, bytes, bytes}; }
-// Whether they share bytes.  Rows at one distance may lie beside each other (columns of one buffer).
-bool overlap(const Span& a, const Span& b) {
-    if (!a.p || !b.p || !a.count || !b.count || !a.length || !b.length) return false;
-    const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-    if (a0 + (a.count - 1) * a.pitch + a.length <= b0 || b0 + (b.count - 1) * b.pitch + b.length <= a0) return false;
-    if (a.pitch != b.pitch || a.count == 1 || b.count == 1) return true;
-    const size_t apart = a0 <= b0 ? (b0 - a0) % a.pitch : (a.pitch - (a0 - b0) % a.pitch) % a.pitch;    // of b's row from a's in front of it
-    return apart < a.length || a.pitch - apart < b.length;
-}
-bool overlap(const Span& a, std::initializer_list<Span> others) {
-    return std::any_of(others.begin(), others.end(), [&](const Span& b) { return overlap(a, b); });
-}
-
 // ---------------------------------------------------------------------------
 // Grouped products.
 // ---------------------------------------------------------------------------
 bool features_ok(int in, int out, int groups, size_t rows) {
     return in >= 1 && out >= 1 && in <= PCC_MAX_FEATURES && out <= PCC_MAX_FEATURES && groups >= 1 && groups <= PCC_MAX_GROUPS && rows <= kMaxRows;
 }
-bool ld_ok(size_t ld, int features) { return ld >= (size_t)features && ld <= kMaxLd; }
 
 // Rows of a chunk of the weights' gradient.  A chunk's sums go to the workspace and are added up by another kernel, so
 // there are no more chunks than fill the chip (512 workgroups at a time), none of less than 256 rows, and where the groups fill it by themselves
@@ -81,19 +34,8 @@ int weights_log2(size_t rows, int groups, int in, int out) {
     while (((size_t)1 << log2) < least) ++log2;
     return log2;
 }
-// Chunks that can be in groups of more than one: such a group of n has more than (n - 1) chunks' rows, n/2 at least.
-size_t shared_chunks(size_t rows, int groups, size_t chunk) {
-    return rows <= chunk ? 0 : std::min(rows / chunk + groups, 2 * (rows / chunk));
-}
-
 // Rows of an operand can be read in pieces of 16 bytes, which have to begin at a multiple of four.
 bool even_rows(const void* p, size_t ld) { return aligned(p, 4) && ld % 2 == 0; }
-
-// More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
-template <class K>
-bool allow_lds(K kernel, size_t bytes) {
-    return bytes <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
-}
 
 template <class T, int MODE, int TILE>
 int launch_tiles_of(Grouped& a, hipStream_t st) {
@@ -131,16 +73,8 @@ int launch_forward_tiles(Grouped& a, hipStream_t st) {
     return launch_tiles_of<T, kForward, 256>(a, st);
 }
 
-// Chunks of about rows / want rows, in steps of 1/4 to 1/8 of a power of two, and a multiple of `unit` (a power of two).  The
-// number of chunks (with one more for each group's part) is at most `want`, if there are not too many groups for that.
-void chunk_rows(Grouped& a, uint64_t want, int unit_log2) {
-    const uint64_t whole = want > 2 * (uint64_t)a.groups ? want - a.groups : std::max<uint64_t>(want, 1) / 2 + 1;
-    const uint64_t rows = std::max<uint64_t>(((uint64_t)a.rows + whole - 1) / whole, 1);
-    a.log2 = unit_log2;
-    while (a.log2 < 24 && ((uint64_t)8 << a.log2) < rows) ++a.log2;     // rows of a chunk are counted in 32 bits
-    a.mult = (uint32_t)std::min<uint64_t>((rows + ((uint64_t)1 << a.log2) - 1) >> a.log2, 8);
-}
-uint64_t chunk_count(const Grouped& a) { return (uint64_t)a.rows / ((uint64_t)a.mult << a.log2) + a.groups; }
+void chunk_rows(Grouped& a, uint64_t want, int unit_log2) { pcc_train::chunk_rows(a.rows, a.groups, want, unit_log2, a.log2, a.mult); }
+uint64_t chunk_count(const Grouped& a) { return pcc_train::chunk_count(a.rows, a.groups, a.log2, a.mult); }
 
 // The forward pass with the weights in LDS: for inputs of up to 192 features, a multiple of eight, in rows that begin at even
 // elements, and weights of up to 80 KB.  us for 393,216 rows with tiles and so: 32 to 160 132 and 39, 128 to 60 68 and 41, 64 to 64

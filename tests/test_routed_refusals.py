@@ -1,0 +1,168 @@
+"""Arguments that the operators round the grouped products refuse, before anything touches a GPU; and the published outputs of Philox4x32."""
+import pytest
+import torch
+
+import routed_reference as ref
+from paper_2212_01185_amd import binding
+
+ARG, SCRATCH, OK = binding.PCC_E_ARG, binding.PCC_E_SCRATCH, binding.PCC_OK
+# stand for device pointers, far from each other: a refused call never follows them
+A, B, D, E, F, G, H, I = (0x10000000 * i for i in range(1, 9))
+
+
+def call(name, defaults, **changes):
+    args = dict(defaults)
+    assert set(changes) <= set(args)
+    args.update(changes)
+    return getattr(binding.load(), name)(*args.values())
+
+
+NORM = dict(x=A, ldx=40, gamma=B, beta=D, off=E, groups=2, rows=100, features=40, eps=1e-5, type=0, y=F, y_type=0, ldy=40, stats=G, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(x=None), dict(y=None), dict(groups=0), dict(groups=65536), dict(features=0), dict(features=65537, ldx=1 << 17, ldy=1 << 17),
+                                     dict(rows=1 << 41), dict(off=None), dict(off=E + 4), dict(ldx=39), dict(ldy=39), dict(ldx=1 << 23), dict(eps=0.0), dict(eps=-1.0),
+                                     dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=1e-40), dict(type=3), dict(type=-1), dict(y_type=1), dict(y_type=2),
+                                     dict(type=1), dict(x=A + 1), dict(type=2, x=A + 2), dict(y=F + 1), dict(gamma=B + 2), dict(beta=D + 1), dict(stats=G + 2),
+                                     dict(y=A), dict(y=A + 7998), dict(y=B + 318), dict(y=D), dict(y=E + 22), dict(stats=A), dict(stats=F + 4), dict(stats=B), dict(stats=E)])
+def test_layer_norm(changes):
+    assert call("pcc_layer_norm", NORM, **changes) == ARG
+
+
+def test_layer_norm_without_rows_does_nothing():
+    assert call("pcc_layer_norm", NORM, rows=0) == OK
+    assert call("pcc_layer_norm", NORM, rows=0, x=None, y=None, stats=None) == OK
+
+
+NORM_GRAD = dict(dy=A, y_type=0, lddy=40, x=B, ldx=40, stats=D, gamma=E, off=F, groups=2, rows=100, features=40, type=0, dx=G, lddx=40, dgamma=H, dbeta=H + 4096,
+                 workspace=I, workspace_bytes=1 << 24, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(dy=None), dict(x=None), dict(stats=None), dict(dx=None, dgamma=None, dbeta=None), dict(dgamma=None), dict(dbeta=None), dict(groups=0),
+                                     dict(off=None), dict(features=0), dict(lddy=39), dict(ldx=39), dict(lddx=39), dict(type=1), dict(y_type=2), dict(type=4, y_type=4),
+                                     dict(dy=A + 1), dict(stats=D + 2), dict(dgamma=H + 2), dict(workspace=I + 8), dict(rows=1 << 41), dict(dx=A), dict(dx=B), dict(dx=D),
+                                     dict(dx=E), dict(dx=F), dict(dx=H), dict(dx=I), dict(dgamma=A), dict(dgamma=H + 4096), dict(dbeta=B), dict(dbeta=I), dict(workspace=A),
+                                     dict(workspace=E)])
+def test_layer_norm_grad(changes):
+    assert call("pcc_layer_norm_grad", NORM_GRAD, **changes) == ARG
+
+
+def test_layer_norm_grad_wants_its_workspace():
+    need = binding.load().pcc_layer_norm_grad_workspace_bytes(100000, 2, 40)
+    assert need > 0
+    assert call("pcc_layer_norm_grad", NORM_GRAD, rows=100000, workspace=None) == SCRATCH
+    assert call("pcc_layer_norm_grad", NORM_GRAD, rows=100000, workspace_bytes=need - 1) == SCRATCH
+    assert binding.load().pcc_layer_norm_grad_workspace_bytes(100, 0, 40) == 0
+    assert binding.load().pcc_layer_norm_grad_workspace_bytes(100, 1, 70000) == 0
+
+
+ROUTE = dict(logits=A, ldl=8, tokens=100, experts=8, k=2, type=2, over_all=0, expert=B, weight=D, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(logits=None), dict(expert=None), dict(weight=None), dict(k=0), dict(k=9), dict(experts=0, k=1), dict(experts=1025, ldl=1025), dict(ldl=7),
+                                     dict(k=17, experts=32, ldl=32), dict(type=3), dict(over_all=2), dict(over_all=-1), dict(logits=A + 2), dict(expert=B + 2),
+                                     dict(weight=D + 1), dict(tokens=1 << 31), dict(tokens=1 << 30), dict(expert=A), dict(weight=A + 3196), dict(expert=D + 4), dict(ldl=1 << 23)])
+def test_route(changes):
+    assert call("pcc_route", ROUTE, **changes) == ARG
+
+
+ROUTE_GRAD = dict(dweight=A, logits=B, ldl=8, expert=D, weight=E, tokens=100, experts=8, k=2, type=2, over_all=1, dlogits=F, lddl=8, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(dweight=None), dict(logits=None), dict(expert=None), dict(weight=None), dict(dlogits=None), dict(k=0), dict(k=9), dict(experts=0, k=1),
+                                     dict(ldl=7), dict(lddl=7), dict(type=-1), dict(over_all=3), dict(dlogits=F + 2), dict(dlogits=B), dict(dlogits=A), dict(dlogits=D + 796),
+                                     dict(dlogits=E), dict(tokens=1 << 31)])
+def test_route_grad(changes):
+    assert call("pcc_route_grad", ROUTE_GRAD, **changes) == ARG
+
+
+SORT = dict(expert=A, tokens=100, k=2, experts=8, offsets=B, place=D, workspace=E, workspace_bytes=1 << 20, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(expert=None), dict(offsets=None), dict(place=None), dict(k=0), dict(k=17), dict(experts=0), dict(experts=1025), dict(tokens=1 << 31),
+                                     dict(tokens=1 << 30), dict(expert=A + 2), dict(offsets=B + 4), dict(place=D + 2), dict(place=A), dict(place=B - 796), dict(offsets=A),
+                                     dict(tokens=100000, workspace=E + 8), dict(tokens=100000, workspace=A), dict(tokens=100000, workspace=D), dict(tokens=100000, workspace=B)])
+def test_expert_sort(changes):
+    assert call("pcc_expert_sort", SORT, **changes) == ARG
+
+
+def test_expert_sort_wants_its_workspace():
+    need = binding.load().pcc_expert_sort_workspace_bytes(100000, 2, 8)
+    assert need > 0
+    assert call("pcc_expert_sort", SORT, tokens=100000, workspace=None) == SCRATCH
+    assert call("pcc_expert_sort", SORT, tokens=100000, workspace_bytes=need - 1) == SCRATCH
+    assert binding.load().pcc_expert_sort_workspace_bytes(100000, 2, 0) == 0
+
+
+ROWS = dict(x=A, ldx=40, place=B, tokens=100, k=2, rows=200, features=40, type=0, out=D, ldr=40, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(x=None), dict(place=None), dict(out=None), dict(k=0), dict(k=17), dict(rows=1 << 31), dict(features=0), dict(features=65537, ldx=1 << 17, ldr=1 << 17),
+                                     dict(type=3), dict(ldx=39), dict(ldr=39), dict(x=A + 1), dict(out=D + 1), dict(place=B + 2), dict(out=A), dict(out=B), dict(tokens=1 << 31)])
+def test_expert_rows(changes):
+    assert call("pcc_expert_rows", ROWS, **changes) == ARG
+
+
+def test_expert_rows_of_nothing():
+    assert call("pcc_expert_rows", ROWS, tokens=0, x=None, place=None) == OK
+    assert call("pcc_expert_rows", ROWS, rows=0, out=None) == OK
+
+
+JOIN = dict(z=A, ldz=40, place=B, weight=D, tokens=100, k=2, rows=200, features=40, type=0, y=E, y_type=2, ldy=40, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(z=None), dict(place=None), dict(y=None), dict(k=0), dict(rows=1 << 31), dict(features=0), dict(type=3, y_type=3), dict(y_type=1), dict(type=2, y_type=0),
+                                     dict(ldz=39), dict(ldy=39), dict(z=A + 1), dict(y=E + 2), dict(weight=D + 2), dict(y=A), dict(y=B), dict(y=D), dict(tokens=1 << 31)])
+def test_expert_join(changes):
+    assert call("pcc_expert_join", JOIN, **changes) == ARG
+
+
+JOIN_GRAD = dict(dy=A, y_type=2, lddy=40, z=B, ldz=40, place=D, weight=E, tokens=100, k=2, rows=200, features=40, type=0, dz=F, lddz=40, dweight=G, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(dy=None), dict(z=None), dict(place=None), dict(dz=None, dweight=None), dict(k=17), dict(rows=1 << 31), dict(features=0), dict(y_type=1), dict(type=2, y_type=1),
+                                     dict(lddy=39), dict(ldz=39), dict(lddz=39), dict(dy=A + 2), dict(z=B + 1), dict(dweight=G + 2), dict(dz=A), dict(dz=B), dict(dz=D), dict(dz=E),
+                                     dict(dz=G), dict(dweight=A), dict(dweight=D), dict(dweight=E)])
+def test_expert_join_grad(changes):
+    assert call("pcc_expert_join_grad", JOIN_GRAD, **changes) == ARG
+
+
+DROPOUT = dict(x=A, ldx=40, residual=B, ldr=40, rows=100, features=40, type=0, p=0.5, seed=1, step=D, y=E, y_type=0, ldy=40, stream=None)
+
+
+@pytest.mark.parametrize("changes", [dict(x=None), dict(y=None), dict(features=0), dict(features=65537, ldx=1 << 17, ldr=1 << 17, ldy=1 << 17), dict(rows=1 << 41), dict(type=3), dict(y_type=1),
+                                     dict(type=1), dict(p=-0.1), dict(p=1.1), dict(p=float("nan")), dict(ldx=39), dict(ldr=39), dict(ldy=39), dict(x=A + 1), dict(residual=B + 1),
+                                     dict(step=D + 4), dict(y=A + 2), dict(y=A, ldy=41), dict(y=A, y_type=2), dict(y=B, ldy=41), dict(y=B + 80), dict(y=D), dict(rows=1 << 40, features=512, ldx=512, ldr=512, ldy=512, y=1 << 60)])
+def test_dropout(changes):
+    assert call("pcc_dropout", DROPOUT, **changes) == ARG
+
+
+def test_dropout_without_rows_does_nothing():
+    assert call("pcc_dropout", DROPOUT, rows=0) == OK
+    assert call("pcc_dropout", DROPOUT, rows=0, x=None, y=None) == OK
+
+
+def test_python_arguments():
+    x, w = torch.zeros(4, 8), torch.zeros(1, 8)
+    i = torch.zeros(4, 2, dtype=torch.int32)
+    for bad in (lambda: binding.pcc_layer_norm(x), lambda: binding.pcc_layer_norm_grad(x, x, torch.zeros(4, 2)), lambda: binding.pcc_route(x, 2),
+                lambda: binding.pcc_route_grad(x[:, :2], x, i, x[:, :2]), lambda: binding.pcc_expert_sort(i, 4), lambda: binding.pcc_expert_rows(x, i),
+                lambda: binding.pcc_expert_join(x, i), lambda: binding.pcc_expert_join_grad(x, x, i), lambda: binding.pcc_dropout(x, 0.1, 1)):
+        with pytest.raises(ValueError):             # not on a GPU
+            bad()
+    asks = lambda t: t.clone().requires_grad_(True)  # noqa: E731
+    for bad in (lambda: binding.pcc_layer_norm(asks(x)), lambda: binding.pcc_layer_norm(x, asks(w)), lambda: binding.pcc_layer_norm(x, None, asks(w)),
+                lambda: binding.pcc_layer_norm_grad(asks(x), x, torch.zeros(4, 2)), lambda: binding.pcc_route(asks(x), 2),
+                lambda: binding.pcc_route_grad(asks(x[:, :2]), x, i, x[:, :2]), lambda: binding.pcc_expert_rows(asks(x), i), lambda: binding.pcc_expert_join(asks(x), i),
+                lambda: binding.pcc_expert_join(x, i, asks(x[:, :2])), lambda: binding.pcc_expert_join_grad(x, asks(x), i), lambda: binding.pcc_dropout(asks(x), 0.1, 1),
+                lambda: binding.pcc_dropout(x, 0.1, 1, residual=asks(x))):
+        with pytest.raises(ValueError, match="autograd"):
+            bad()
+
+
+def test_the_reference_makes_philox_published_outputs():
+    """Known answers that come with the paper's generator: Philox4x32 with ten rounds."""
+    assert ref.philox((0, 0, 0, 0), (0, 0)) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    ones = 0xFFFFFFFF
+    assert ref.philox((ones,) * 4, (ones,) * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+    assert ref.philox((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0)) == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
