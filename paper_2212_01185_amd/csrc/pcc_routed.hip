@@ -27,16 +27,16 @@ struct RowShape {
 // How many lanes have a row, and how many eights of it each.
 template <class F>
 int with_row_shape(int features, F&& f) {
-    const int chunks = (features + 7) / 8;
-    if (chunks <= 8) return f(RowShape<4, 2>{});
-    if (chunks <= 24) return f(RowShape<4, 6>{});
-    if (chunks <= 32) return f(RowShape<8, 4>{});
-    if (chunks <= 64) return f(RowShape<16, 4>{});
-    if (chunks <= 128) return f(RowShape<32, 4>{});
-    if (chunks <= 256) return f(RowShape<64, 4>{});
-    if (chunks <= 512) return f(RowShape<128, 4>{});
-    if (chunks <= 1024) return f(RowShape<256, 4>{});
-    if (chunks <= 2048) return f(RowShape<512, 4>{});
+    const int eights = features / 8;
+    if (eights <= 8) return f(RowShape<8, 1>{});
+    if (eights <= 24) return f(RowShape<8, 3>{});
+    if (eights <= 32) return f(RowShape<8, 4>{});
+    if (eights <= 64) return f(RowShape<16, 4>{});
+    if (eights <= 128) return f(RowShape<32, 4>{});
+    if (eights <= 256) return f(RowShape<64, 4>{});
+    if (eights <= 512) return f(RowShape<128, 4>{});
+    if (eights <= 1024) return f(RowShape<256, 4>{});
+    if (eights <= 2048) return f(RowShape<512, 4>{});
     return f(RowShape<kLongThreads, 0>{});      // read again for each sum
 }
 // x and y have one type, or x is fp32 and y a 16-bit one.
@@ -52,8 +52,19 @@ bool norm_ok(const int64_t* d_offsets, int groups, size_t rows, int features, in
 }
 int log2_of(int v) { return v <= 1 ? 0 : 1 + log2_of(v / 2); }
 
-// Rows of the chunks whose sums are joined.
-void sums_chunks(size_t rows, int groups, int& log2, uint32_t& mult) { chunk_rows((int64_t)rows, groups, 512, 3, log2, mult); }
+// Chunks of whole turns of a workgroup's teams, `want` of them at most if there are not too many groups for that: as many as run at once, for a
+// workgroup's start (weights) and end (sums) are worth some rows.
+void norm_chunks(size_t rows, int groups, int want, int lanes, int& log2, uint32_t& mult) {
+    const size_t whole = groups == 1 ? want : want > 2 * groups ? want - groups : want / 2 + 1, least = (rows + whole - 1) / whole;
+    log2 = log2_of(norm_teams(lanes));
+    while (log2 < 24 && ((size_t)64 << log2) < least) ++log2;
+    mult = (uint32_t)std::min<size_t>(std::max<size_t>((least + ((size_t)1 << log2) - 1) >> log2, 1), 64);
+}
+// Chunks whose sums are joined: two workgroups of 256 threads a compute unit by their registers.
+void sums_chunks(size_t rows, int groups, int features, int& log2, uint32_t& mult) {
+    const int lanes = with_row_shape(features, [](auto shape) { return decltype(shape)::kLanes; });
+    norm_chunks(rows, groups, features < 72 ? 1280 : lanes <= 256 ? 512 : 256, lanes, log2, mult);
+}
 
 }  // namespace
 
@@ -74,14 +85,16 @@ int pcc_layer_norm(const void* d_x, size_t ldx, const float* d_gamma, const floa
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.eps = eps; a.inverse = 1.0f / (float)features;
     return with_row_shape(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        chunk_rows(a.rows, groups, 2048, log2_of(norm_teams(L)), a.log2, a.mult);
+        norm_chunks(rows, groups, L <= 64 ? 2048 : L == 128 ? 1024 : L == 256 ? 512 : 256, L, a.log2, a.mult);
         const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
         if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
         return with_norm_types(type, y_type, [&](auto tx, auto ty) {
+            if constexpr (N > 0)
+                if (!allow_lds(layer_norm_kernel<decltype(tx), decltype(ty), L, N>, 2 * Weights::values(features) * sizeof(float))) { (void)hipGetLastError(); return PCC_E_HIP; }
             return launch([&] {
                 const dim3 grid((uint32_t)((blocks + 7) / 8 * 8)), threads(norm_threads(L));
                 if constexpr (N == 0) hipLaunchKernelGGL((layer_norm_long_kernel<decltype(tx), decltype(ty)>), grid, threads, 0, (hipStream_t)hip_stream, a);
-                else hipLaunchKernelGGL((layer_norm_kernel<decltype(tx), decltype(ty), L, N>), grid, threads, 0, (hipStream_t)hip_stream, a);
+                else hipLaunchKernelGGL((layer_norm_kernel<decltype(tx), decltype(ty), L, N>), grid, threads, 2 * Weights::values(features) * sizeof(float), (hipStream_t)hip_stream, a);
             });
         });
     });
@@ -91,7 +104,7 @@ size_t pcc_layer_norm_grad_workspace_bytes(size_t rows, int groups, int features
     if (features < 1 || features > PCC_MAX_FEATURES || groups < 1 || groups > PCC_MAX_GROUPS || rows > kMaxRows) return 0;
     int log2;
     uint32_t mult;
-    sums_chunks(rows, groups, log2, mult);
+    sums_chunks(rows, groups, features, log2, mult);
     return shared_chunks(rows, groups, (size_t)mult << log2) * 2 * features * sizeof(float);
 }
 
@@ -117,34 +130,43 @@ int pcc_layer_norm_grad(const void* d_dy, int y_type, size_t lddy, const void* d
     a.ldx = ldx; a.lddy = lddy; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.inverse = 1.0f / (float)features;
     a.shared_max = (uint32_t)std::min<size_t>(need / (2 * features * sizeof(float)), 0xFFFFFFFFu);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (d_dx && rows) {
-        const int rc = with_row_shape(features, [&](auto shape) {
-            constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-            chunk_rows(a.rows, groups, 2048, log2_of(norm_teams(L)), a.log2, a.mult);
-            const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
-            if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
-            return with_norm_types(type, y_type, [&](auto tx, auto ty) {
+    const int rc = with_row_shape(features, [&](auto shape) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        return with_norm_types(type, y_type, [&](auto tx, auto ty) {
+            using X = decltype(tx);
+            using Y = decltype(ty);
+            if constexpr (N == 0) {
+                if (d_dx && rows) {
+                    norm_chunks(rows, groups, 2048, kLongThreads, a.log2, a.mult);
+                    const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+                    if (!launchable(blocks, kLongThreads)) return PCC_E_ARG;
+                    const int rc = launch([&] {
+                        hipLaunchKernelGGL((layer_norm_long_dx_kernel<X, Y>), dim3((uint32_t)((blocks + 7) / 8 * 8)), dim3(kLongThreads), 0, st, a);
+                    });
+                    if (rc != PCC_OK) return rc;
+                }
+                sums_chunks(rows, groups, features, a.log2, a.mult);
+                const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+                if (!d_dgamma) return PCC_OK;
+                if (!launchable(blocks * 8, 256)) return PCC_E_ARG;
                 return launch([&] {
-                    const dim3 grid((uint32_t)((blocks + 7) / 8 * 8)), threads(norm_threads(L));
-                    if constexpr (N == 0) hipLaunchKernelGGL((layer_norm_long_dx_kernel<decltype(tx), decltype(ty)>), grid, threads, 0, st, a);
-                    else hipLaunchKernelGGL((layer_norm_dx_kernel<decltype(tx), decltype(ty), L, N>), grid, threads, 0, st, a);
+                    hipLaunchKernelGGL((layer_norm_sums_kernel<X, Y>), dim3((uint32_t)((blocks + 7) / 8 * 8), std::min((features + 255) / 256, 8)), dim3(256), 0, st, a);
                 });
-            });
-        });
-        if (rc != PCC_OK) return rc;
-    }
-    if (!d_dgamma) return PCC_OK;
-    sums_chunks(rows, groups, a.log2, a.mult);
-    const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
-    if (!launchable(blocks, 256)) return PCC_E_ARG;
-    const int rc = with_norm_types(type, y_type, [&](auto tx, auto ty) {
-        return launch([&] {
-            hipLaunchKernelGGL((layer_norm_sums_kernel<decltype(tx), decltype(ty)>), dim3((uint32_t)((blocks + 7) / 8 * 8), std::min((features + 255) / 256, 8)), dim3(256), 0, st, a);
+            } else {
+                sums_chunks(rows, groups, features, a.log2, a.mult);
+                const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
+                if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
+                const size_t lds = Weights::values(features) * sizeof(float) * (L <= 64 ? 8 : L < 256 ? 2 * norm_teams(L) : 1);    // sums take the weights' place
+                if (!allow_lds(layer_norm_grad_kernel<X, Y, L, N>, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
+                return launch([&] {
+                    hipLaunchKernelGGL((layer_norm_grad_kernel<X, Y, L, N>), dim3((uint32_t)((blocks + 7) / 8 * 8)), dim3(norm_threads(L)), lds, st, a);
+                });
+            }
         });
     });
-    if (rc != PCC_OK || rows <= (size_t)a.mult << a.log2) return rc;        // no group can have two chunks
+    if (rc != PCC_OK || !d_dgamma || rows <= (size_t)a.mult << a.log2) return rc;        // no group can have two chunks
     return launch([&] {
-        hipLaunchKernelGGL(layer_norm_join_kernel, dim3(std::min((2 * features + 63) / 64, std::max(4, 4096 / groups)), groups), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(layer_norm_join_kernel, dim3(std::min((2 * features + 63) / 64, std::max(4, 4096 / groups)), groups), dim3(kJoinThreads), 0, st, a);
     });
 }
 

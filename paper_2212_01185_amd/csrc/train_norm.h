@@ -4,7 +4,9 @@
 //   with u = gamma dy:  dx = s (u - mean(u) - h mean(u h)),  dgamma = sum over rows of dy h,  dbeta = sum of dy
 //
 // A row is read once: LANES lanes have it in registers, eight neighbours at a time, so the variance is that of the distances from the
-// mean and not a difference of two large sums.
+// mean and not a difference of two large sums.  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
+// forward 62 us, 4.3 TB/s (a large copy has 5.2); backward 393,216 rows of 160 87 us, 4.4 TB/s, of which 5 join the chunks' sums, and the vector ALU
+// is busy for about half of it.
 #pragma once
 
 #include "train_rows.h"
@@ -40,136 +42,274 @@ __device__ __forceinline__ Chunk norm_chunk(const Norm& a, uint32_t b, bool empt
 }
 
 // Threads of a workgroup, and rows that it has at a time.
-constexpr int norm_threads(int lanes) { return lanes <= 64 ? 256 : lanes; }
+constexpr int norm_threads(int lanes) { return lanes <= 256 ? 256 : lanes; }
 constexpr int norm_teams(int lanes) { return norm_threads(lanes) / lanes; }
 
-// Sums over a row's lanes, the same in all of them.  More than a wave meet in LDS; `turn` tells the place, of two, so that one barrier is enough.
+// Sums over a row's lanes, the same in all of them, of a workgroup with one row.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float (*meet)[16], int turn) {
-    if constexpr (LANES <= 64) {
-        return lanes_sum<LANES>(v);
-    } else {
-        v = lanes_sum<64>(v);
-        if ((threadIdx.x & 63) == 0) meet[turn][threadIdx.x >> 6] = v;
-        __syncthreads();
-        float s = 0.0f;
+    v = lanes_sum<64>(v);
+    if ((threadIdx.x & 63) == 0) meet[turn][threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < LANES / 64; ++w) s += meet[turn][w];
-        return s;
-    }
+    for (int w = 0; w < LANES / 64; ++w) s += meet[turn][w];
+    return s;
 }
+
+// The weights of a group's features in LDS, for registers are what decides how many rows are on their way: first halves of all eights, then second
+// halves, so that neighbouring lanes read neighbouring 16 bytes, then the rest.
+struct Weights {
+    float* at;
+    int eights;
+
+    static __host__ __device__ constexpr size_t values(int features) { return (size_t)features / 8 * 8 + 8; }
+    __device__ __forceinline__ void fill(float* lds, const float* from, int features, float none) {
+        at = lds;
+        eights = features >> 3;
+        for (int c = threadIdx.x; c < eights; c += blockDim.x) {
+            Eight<Fp32> w;
+            if (from) __builtin_memcpy(w.v, from + 8 * c, sizeof(w.v));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w.v[e] = from ? w.v[e] : none;
+            *reinterpret_cast<f32x4*>(at + 4 * c) = f32x4{w.v[0], w.v[1], w.v[2], w.v[3]};
+            *reinterpret_cast<f32x4*>(at + 4 * (eights + c)) = f32x4{w.v[4], w.v[5], w.v[6], w.v[7]};
+        }
+        const int f = 8 * eights + threadIdx.x;
+        if (f < features) at[f] = from ? from[f] : none;
+    }
+    // Of eight c (WIDE 8), or of feature c behind the last (WIDE 1).
+    template <int WIDE>
+    __device__ __forceinline__ Eight<Fp32> get(int c) const {
+        Eight<Fp32> w;
+        if constexpr (WIDE == 8) {
+            const f32x4 p = *reinterpret_cast<const f32x4*>(at + 4 * c), q = *reinterpret_cast<const f32x4*>(at + 4 * (eights + c));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { w.v[e] = p[e]; w.v[4 + e] = q[e]; }
+        } else {
+            w.v[0] = at[8 * eights + c];
+        }
+        return w;
+    }
+};
+
+// Mean and variance of a row over several waves by those of each wave's part: sums q of squares about a part's own mean m, of n values,
+// make one of sum (q + n (m - mean)^2).
+template <int TEAMS, int WAVES>
+struct Parts {
+    float size[WAVES], inverse[WAVES];
+    float sum[2][TEAMS][WAVES], squares[2][TEAMS][WAVES];
+};
 
 template <class X, class Y, int LANES, int N>
 __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a) {
-    constexpr int kTeams = norm_teams(LANES);
-    __shared__ float meet[2][16];
+    constexpr int kTeams = norm_teams(LANES), kWaves = LANES <= 64 ? 1 : LANES / 64;
+    using R = Row<X, LANES, N>;
+    __shared__ Parts<kTeams, kWaves> parts;
+    extern __shared__ __align__(16) float norm_weights[];
     const Chunk ch = norm_chunk(a, blockIdx.x, false);
     if (ch.group < 0) return;
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    const int n = (int)(ch.hi - ch.lo);
-    const float* gamma = a.gamma ? a.gamma + (size_t)ch.group * a.features : nullptr;
-    const float* beta = a.beta ? a.beta + (size_t)ch.group * a.features : nullptr;
-    for (int r0 = 0; r0 < n; r0 += kTeams) {
-        // a row behind the chunk's last is that one again
-        const bool mine = r0 + team < n;
-        const size_t row = (size_t)ch.lo + (mine ? r0 + team : n - 1);
-        Eight<X> x[N];
-        float sum = 0.0f, squares = 0.0f;
-#pragma unroll
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, wave = lane >> 6, n = (int)(ch.hi - ch.lo), features = a.features;
+    R x, next;
+    x.load(a.x, (size_t)(ch.lo + team) * a.ldx, lane, Extent(features, team < n));
+    Weights gamma, beta;
+    gamma.fill(norm_weights, a.gamma ? a.gamma + (size_t)ch.group * features : nullptr, features, 1.0f);
+    beta.fill(norm_weights + Weights::values(features), a.beta ? a.beta + (size_t)ch.group * features : nullptr, features, 0.0f);
+    if (kWaves > 1 && (int)threadIdx.x < kWaves) {
+        int size = threadIdx.x == 0 ? features & 7 : 0;
         for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            x[i].load(a.x, row * a.ldx + f, a.features - f);
+            const int left = (features >> 3) - (64 * (int)threadIdx.x + LANES * i);
+            size += 8 * (left < 0 ? 0 : left > 64 ? 64 : left);
         }
+        parts.size[threadIdx.x] = (float)size;
+        parts.inverse[threadIdx.x] = size ? 1.0f / (float)size : 0.0f;
+    }
+    __syncthreads();
+    const float own = kWaves > 1 ? parts.inverse[wave] : a.inverse;
+    auto step = [&](R& x, R& next, int r0, int turn) {
+        const Extent w(features, r0 + team < n);
+        next.load(a.x, (size_t)(ch.lo + r0 + kTeams + team) * a.ldx, lane, Extent(features, r0 + kTeams + team < n));
+        float sum = 0.0f, squares = 0.0f;
+        R::each(lane, w, [&](auto wide, int i) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+            for (int e = 0; e < wide; ++e) sum += x.at(i).get(e);
+        });
+        sum = lanes_sum<(LANES < 64 ? LANES : 64)>(sum);
+        float mean = sum * own;         // of the wave's part
+        R::each(lane, w, [&](auto wide, int i) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += x[i].get(e);
-        const float mean = row_sum<LANES>(sum, meet, 0) * a.inverse;
+            for (int e = 0; e < wide; ++e) {
+                const float d = x.at(i).get(e) - mean;
+                squares = __builtin_fmaf(d, d, squares);
+            }
+        });
+        squares = lanes_sum<(LANES < 64 ? LANES : 64)>(squares);
+        if constexpr (kWaves > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                parts.sum[turn][team][wave] = sum;
+                parts.squares[turn][team][wave] = squares;
+            }
+            __syncthreads();
+            sum = squares = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int left = a.features - 8 * (lane + LANES * i);
+            for (int k = 0; k < kWaves; ++k) sum += parts.sum[turn][team][k];
+            mean = sum * a.inverse;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = x[i].get(e) - mean;
-                squares += e < left ? d * d : 0.0f;
+            for (int k = 0; k < kWaves; ++k) {
+                const float d = __builtin_fmaf(parts.sum[turn][team][k], parts.inverse[k], -mean);
+                squares += __builtin_fmaf(parts.size[k] * d, d, parts.squares[turn][team][k]);
             }
         }
-        const float scale = 1.0f / sqrtf(row_sum<LANES>(squares, meet, 1) * a.inverse + a.eps);
-        if (!mine) continue;
-        if (a.stats && lane == 0) {
+        const float scale = __builtin_amdgcn_rsqf(squares * a.inverse + a.eps);
+        x.forget();
+        const size_t row = (size_t)(ch.lo + r0 + team);
+        if (a.stats && lane == 0 && r0 + team < n) {
             a.stats[2 * row] = mean;
             a.stats[2 * row + 1] = scale;
         }
+        Row<Y, LANES, N> y;
+        R::each(lane, w, [&](auto wide, int i) {
+            const int c = i < N ? lane + LANES * i : lane;
+            const Eight<Fp32> g = gamma.get<wide>(c), b = beta.get<wide>(c);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            if (f >= a.features) continue;
-            Eight<Fp32> w, b;
-            if (gamma) w.load(gamma, f, a.features - f);
-            if (beta) b.load(beta, f, a.features - f);
-            Eight<Y> y;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float h = (x[i].get(e) - mean) * scale;
-                y.set(e, __builtin_fmaf(gamma ? w.get(e) : 1.0f, h, beta ? b.get(e) : 0.0f));
-            }
-            y.store(a.y, row * a.ldy + f, a.features - f);
-        }
+            for (int e = 0; e < wide; ++e) y.at(i).set(e, __builtin_fmaf(g.v[e], (x.at(i).get(e) - mean) * scale, b.v[e]));
+            y.store(i, a.y, row * a.ldy, lane, w);
+        });
+    };
+    for (int r0 = 0; r0 < n; r0 += 2 * kTeams) {
+        step(x, next, r0, 0);
+        if (r0 + kTeams >= n) break;
+        step(next, x, r0 + kTeams, 1);
     }
 }
 
-// dx of rows.
+// The whole backward pass, every row read once: a lane has its features' sums in registers to the end of the chunk.
 template <class X, class Y, int LANES, int N>
-__global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_dx_kernel(Norm a) {
-    constexpr int kTeams = norm_teams(LANES);
-    __shared__ float meet[4][16];
-    const Chunk ch = norm_chunk(a, blockIdx.x, false);
-    if (ch.group < 0) return;
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    const int n = (int)(ch.hi - ch.lo);
-    const float* gamma = a.gamma ? a.gamma + (size_t)ch.group * a.features : nullptr;
-    int turn = 0;
-    for (int r0 = 0; r0 < n; r0 += kTeams, turn ^= 2) {
-        const bool mine = r0 + team < n;
-        const size_t row = (size_t)ch.lo + (mine ? r0 + team : n - 1);
-        const float mean = a.stats[2 * row], scale = a.stats[2 * row + 1];
-        Eight<X> x[N];
-        Eight<Y> dy[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            x[i].load(a.x, row * a.ldx + f, a.features - f);
-            dy[i].load(a.dy, row * a.lddy + f, a.features - f);
+__global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(Norm a) {
+    constexpr int kTeams = norm_teams(LANES), kWaves = LANES <= 64 ? 1 : LANES / 64;
+    using R = Row<X, LANES, N>;
+    __shared__ float meet[2][kTeams][2][kWaves];
+    extern __shared__ __align__(16) float norm_weights[];
+    const Chunk ch = norm_chunk(a, blockIdx.x, a.dgamma != nullptr);
+    if (ch.group < 0 || (a.dgamma && ch.count > 1 && ch.shared >= a.shared_max)) return;    // (the second only with offsets that fall)
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES, wave = lane >> 6, n = (int)(ch.hi - ch.lo), features = a.features;
+    struct Held {
+        R x;
+        Row<Y, LANES, N> dy;
+        float mean, scale;
+    } held, then;
+    auto load = [&](Held& h, int r) {
+        const Extent w(features, r < n);
+        const size_t row = (size_t)(ch.lo + r);
+        h.x.load(a.x, row * a.ldx, lane, w);
+        h.dy.load(a.dy, row * a.lddy, lane, w);
+        h.mean = h.scale = 0.0f;
+        if (r < n) {
+            h.mean = a.stats[2 * row];
+            h.scale = a.stats[2 * row + 1];
         }
+    };
+    load(held, team);
+    Weights gamma;
+    gamma.fill(norm_weights, a.gamma ? a.gamma + (size_t)ch.group * features : nullptr, features, 1.0f);
+    __syncthreads();
+    Row<Fp32, LANES, N> dg, db;         // the sums
+    dg.clear();
+    db.clear();
+    auto step = [&](Held& h, Held& next, int r0, int turn) {
+        const Extent w(features, r0 + team < n);
+        load(next, r0 + kTeams + team);
+        const float mean = h.mean, scale = h.scale;
         float s1 = 0.0f, s2 = 0.0f;
+        R::each(lane, w, [&](auto wide, int i) {
+            const Eight<Fp32> g = gamma.get<wide>(i < N ? lane + LANES * i : lane);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            Eight<Fp32> w;
-            if (gamma) w.load(gamma, f, a.features - f);
+            for (int e = 0; e < wide; ++e) {
+                const float d = h.dy.at(i).get(e), x = (h.x.at(i).get(e) - mean) * scale, u = d * g.v[e];
+                s1 += u;
+                s2 = __builtin_fmaf(u, x, s2);
+                dg.at(i).v[e] = __builtin_fmaf(d, x, dg.at(i).v[e]);
+                db.at(i).v[e] += d;
+            }
+        });
+        s1 = lanes_sum<(LANES < 64 ? LANES : 64)>(s1);
+        s2 = lanes_sum<(LANES < 64 ? LANES : 64)>(s2);
+        if constexpr (kWaves > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                meet[turn][team][0][wave] = s1;
+                meet[turn][team][1][wave] = s2;
+            }
+            __syncthreads();
+            s1 = s2 = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float u = dy[i].get(e) * (gamma ? w.get(e) : 1.0f), h = (x[i].get(e) - mean) * scale;
-                s1 += f + e < a.features ? u : 0.0f;
-                s2 += f + e < a.features ? u * h : 0.0f;
+            for (int k = 0; k < kWaves; ++k) {
+                s1 += meet[turn][team][0][k];
+                s2 += meet[turn][team][1][k];
             }
         }
-        s1 = row_sum<LANES>(s1, meet, turn) * a.inverse;
-        s2 = row_sum<LANES>(s2, meet, turn + 1) * a.inverse;
-        if (!mine) continue;
+        h.x.forget();
+        h.dy.forget();
+        if (a.y) {
+            // scale (u - m1 - (x - mean) scale m2)
+            const float m1 = -(scale * (s1 * a.inverse)), m2 = -(scale * scale * (s2 * a.inverse));
+            R dx;
+            R::each(lane, w, [&](auto wide, int i) {
+                const Eight<Fp32> g = gamma.get<wide>(i < N ? lane + LANES * i : lane);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            if (f >= a.features) continue;
-            Eight<Fp32> w;
-            if (gamma) w.load(gamma, f, a.features - f);
-            Eight<X> dx;
+                for (int e = 0; e < wide; ++e)
+                    dx.at(i).set(e, __builtin_fmaf(h.x.at(i).get(e) - mean, m2, __builtin_fmaf(h.dy.at(i).get(e) * g.v[e], scale, m1)));
+                dx.store(i, a.y, (size_t)(ch.lo + r0 + team) * a.ldy, lane, w);
+            });
+        }
+    };
+    for (int r0 = 0; r0 < n; r0 += 2 * kTeams) {
+        step(held, then, r0, 0);
+        if (r0 + kTeams >= n) break;
+        step(then, held, r0 + kTeams, 1);
+    }
+    if (!a.dgamma) return;
+    float* to = ch.count == 1 ? a.dgamma + (size_t)ch.group * features : a.partial + (size_t)ch.shared * 2 * features;
+    float* to_beta = ch.count == 1 ? a.dbeta + (size_t)ch.group * features : to + features;
+    const Extent all(features, true);
+    if constexpr (LANES >= 256) {
+        R::each(lane, all, [&](auto, int i) {
+            dg.store(i, to, 0, lane, all);
+            db.store(i, to_beta, 0, lane, all);
+        });
+    } else {
+        // the rows of a wave by exchanges, then those of the waves or teams, kShares of them, through LDS (where the weights were)
+        constexpr int kShares = LANES <= 64 ? 4 : kTeams;
+        const int share = LANES <= 64 ? threadIdx.x >> 6 : team;
+        if constexpr (LANES < 64) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float u = dy[i].get(e) * (gamma ? w.get(e) : 1.0f), h = (x[i].get(e) - mean) * scale;
-                dx.set(e, scale * (u - s1 - h * s2));
+            for (int i = 0; i <= N; ++i)
+#pragma unroll
+                for (int e = 0; e < (i < N ? 8 : 1); ++e) {
+                    dg.at(i).v[e] = groups_sum<LANES>(dg.at(i).v[e]);
+                    db.at(i).v[e] = groups_sum<LANES>(db.at(i).v[e]);
+                }
+        }
+        __syncthreads();
+        const int pitch = (int)Weights::values(features);
+        if (LANES >= 64 || (int)(threadIdx.x & 63) < LANES)
+            R::each(lane, all, [&](auto wide, int i) {
+                float* at = norm_weights + 2 * share * pitch + (i < N ? 8 * (lane + LANES * i) : 8 * all.eights + lane);
+#pragma unroll
+                for (int e = 0; e < wide; ++e) {
+                    at[e] = dg.at(i).v[e];
+                    at[pitch + e] = db.at(i).v[e];
+                }
+            });
+        __syncthreads();
+        for (int f = threadIdx.x; f < features; f += norm_threads(LANES)) {
+            float g = 0.0f, b = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kShares; ++k) {
+                g += norm_weights[2 * k * pitch + f];
+                b += norm_weights[2 * k * pitch + pitch + f];
             }
-            dx.store(a.y, row * a.ldy + f, a.features - f);
+            to[f] = g;
+            to_beta[f] = b;
         }
     }
 }
@@ -304,8 +444,10 @@ __global__ __launch_bounds__(256) void layer_norm_sums_kernel(Norm a) {
 }
 
 // Chunks' sums to those of their group, always in the same order.  A group of one chunk was written where it belongs.
-__global__ __launch_bounds__(256) void layer_norm_join_kernel(Norm a) {
-    __shared__ float slices[4][64];
+constexpr int kJoinThreads = 1024, kJoinSlices = kJoinThreads / 16;
+
+__global__ __launch_bounds__(kJoinThreads) void layer_norm_join_kernel(Norm a) {
+    __shared__ __align__(16) f32x4 slices[kJoinSlices][16];
     const int g = blockIdx.y, lane = threadIdx.x & 63;
     int64_t lo, hi;
     uint32_t count, first = 0;
@@ -324,20 +466,31 @@ __global__ __launch_bounds__(256) void layer_norm_join_kernel(Norm a) {
         if (count <= 1) return;
     }
     if (first + count > a.shared_max) return;
-    const int all = 2 * a.features, slice = threadIdx.x >> 6;
-    for (int e0 = 64 * blockIdx.x; e0 < all; e0 += 64 * gridDim.x) {
-        const int e = e0 + lane;
-        float s = 0.0f;
-        if (e < all) {
-            const float* from = a.partial + (size_t)first * all + e;
+    // 64 values a workgroup, four a thread; 64 slices of it have every 64th chunk
+    const int all = 2 * a.features, slice = threadIdx.x >> 4, e0 = 4 * (threadIdx.x & 15);
+    for (int b = 64 * blockIdx.x; b < all; b += 64 * gridDim.x) {
+        const int e = b + e0, left = all - e;
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float* from = a.partial + (size_t)first * all + e;
+        if (left >= 4) {
+            typedef f32x4 at_four __attribute__((aligned(4)));
 #pragma unroll 4
-            for (uint32_t c = slice; c < count; c += 4) s += from[(size_t)c * all];
+            for (uint32_t c = slice; c < count; c += kJoinSlices) s += *reinterpret_cast<const at_four*>(from + (size_t)c * all);
+        } else if (left > 0) {
+            for (uint32_t c = slice; c < count; c += kJoinSlices) {
+                s[0] += from[(size_t)c * all];
+                if (left > 1) s[1] += from[(size_t)c * all + 1];
+                if (left > 2) s[2] += from[(size_t)c * all + 2];
+            }
         }
-        slices[slice][lane] = s;
+        slices[slice][threadIdx.x & 15] = s;
         __syncthreads();
-        if (slice == 0 && e < all) {
-            s = slices[0][lane] + slices[1][lane] + slices[2][lane] + slices[3][lane];
-            (e < a.features ? a.dgamma + (size_t)g * a.features + e : a.dbeta + (size_t)g * a.features + (e - a.features))[0] = s;
+        if (threadIdx.x < 64) {
+            float sum = 0.0f;
+            for (int k = 0; k < kJoinSlices; ++k) sum += slices[k][threadIdx.x >> 2][threadIdx.x & 3];
+            const int f = b + threadIdx.x;
+            if (f < a.features) a.dgamma[(size_t)g * a.features + f] = sum;
+            else if (f < all) a.dbeta[(size_t)g * a.features + (f - a.features)] = sum;
         }
         __syncthreads();
     }

@@ -52,6 +52,64 @@ struct Eight {
     }
 };
 
+// A row that LANES lanes (8 at least) share: lane l has the eights l, l + LANES, ..., N of them at most, and of the up to seven features behind the last
+// whole eight the l-th.
+struct Extent {
+    int eights, rest;       // of a row; 0 for a row that is not there
+
+    __device__ __forceinline__ Extent(int features, bool there) : eights(there ? features >> 3 : 0), rest(there ? features & 7 : 0) {}
+};
+
+template <class T, int LANES, int N>
+struct Row {
+    static_assert(LANES >= 8, "the features behind the last eight have a lane each");
+    Eight<T> v[N];
+    Eight<T> tail;          // the first value
+
+    // f(i, eight) for the eights that are this lane's, then f(N, eight of one value) for its value of the rest.
+    template <class F>
+    static __device__ __forceinline__ void each(int lane, Extent w, F&& f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (lane + LANES * i < w.eights) f(std::integral_constant<int, 8>{}, i);
+        if (lane < w.rest) f(std::integral_constant<int, 1>{}, N);
+    }
+    __device__ __forceinline__ Eight<T>& at(int i) { return i < N ? v[i < N ? i : 0] : tail; }
+    __device__ __forceinline__ const Eight<T>& at(int i) const { return i < N ? v[i < N ? i : 0] : tail; }
+
+    __device__ __forceinline__ void load(const void* base, size_t at0, int lane, Extent w) {
+        const element_of<T>* from = static_cast<const element_of<T>*>(base) + at0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (lane + LANES * i < w.eights) __builtin_memcpy(v[i].v, from + 8 * (lane + LANES * i), sizeof(v[i].v));
+        if (lane < w.rest) tail.v[0] = from[8 * w.eights + lane];
+    }
+    __device__ __forceinline__ void store(int i, void* base, size_t at0, int lane, Extent w) const {
+        element_of<T>* to = static_cast<element_of<T>*>(base) + at0;
+        if (i < N) __builtin_memcpy(to + 8 * (lane + LANES * i), v[i < N ? i : 0].v, sizeof(v[0].v));
+        else to[8 * w.eights + lane] = tail.v[0];
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i].v[e] = element_of<T>{};
+        tail.v[0] = element_of<T>{};
+    }
+    // What was made of the values is made anew behind this, not kept: a value takes half a register as it came.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            constexpr int kWords = sizeof(v[0].v) / 16;
+            u32x4 words[kWords];
+            __builtin_memcpy(words, v[i].v, sizeof(words));
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) asm("" : "+v"(words[k]));
+            __builtin_memcpy(v[i].v, words, sizeof(words));
+        }
+    }
+};
+
 // Sums over groups of G neighbouring lanes (a power of two), the same in each of them: lanes exchange within quads, halves of a row of
 // 16 and rows by the vector ALU's own permutations, whole rows by swaps.  All lanes of a group have to be active.
 template <int CTRL>
