@@ -245,12 +245,15 @@ int pcc_route_grad(const float* d_dweight, const void* d_logits, size_t ldl, con
 
 namespace {
 
-// Segments of the sort: whole rounds of its waves, as many as there are workgroups of 1024 threads on the chip at most.
-uint32_t sort_segment(size_t entries) {
-    const size_t least = (entries + 255) / 256;
+// Segments of the sort: whole rounds of its waves, 256 of them at most, and with many experts fewer, since every workgroup sums all segments' counts.
+uint32_t sort_segment(size_t entries, int experts) {
+    const size_t most = std::min(256, std::max(64, 65536 / experts)), least = (entries + most - 1) / most;
     return (uint32_t)std::max<size_t>(4096, (least + 1023) / 1024 * 1024);
 }
-uint32_t sort_segments(size_t entries) { return (uint32_t)std::max<size_t>(1, (entries + sort_segment(entries) - 1) / sort_segment(entries)); }
+uint32_t sort_segments(size_t entries, int experts) {
+    const uint32_t segment = sort_segment(entries, experts);
+    return (uint32_t)std::max<size_t>(1, (entries + segment - 1) / segment);
+}
 
 // Rows of `features` values, their places and weights.
 bool rows_ok(size_t tokens, int k, size_t rows, int features, int type) {
@@ -263,6 +266,28 @@ int with_row_types(int type, int y_type, F&& f) {
     if (type == PCC_FP16) return y_type == PCC_FP16 ? f(Fp16{}, Fp16{}) : f(Fp16{}, Fp32{});
     return f(Fp32{}, Fp32{});
 }
+// How many lanes have a token's row, and how many eights of it at a time each.
+template <class F>
+int with_token_shape(int features, F&& f) {
+    const int eights = features / 8;
+    if (eights <= 8) return f(RowShape<8, 1>{});
+    if (eights <= 32) return f(RowShape<8, 4>{});
+    if (eights <= 64) return f(RowShape<16, 4>{});
+    if (eights <= 128) return f(RowShape<32, 4>{});
+    if (eights <= 256) return f(RowShape<64, 4>{});
+    return f(RowShape<256, 4>{});
+}
+// f(shape, workgroups), with the workgroups of each die in `a`.
+template <class F>
+int with_tokens(Experts& a, F&& f) {
+    return with_token_shape(a.features, [&](auto shape) {
+        constexpr int kTeams = kExpertThreads / decltype(shape)::kLanes;
+        const uint64_t each = ((a.tokens + kTeams - 1) / kTeams + 7) / 8;
+        if (!launchable(8 * each, kExpertThreads)) return PCC_E_ARG;
+        a.each = (uint32_t)each;
+        return f(shape, dim3((uint32_t)(8 * each)));
+    });
+}
 uint64_t chunk_blocks(uint64_t rows, uint32_t chunks, int threads) { return (rows * chunks + threads - 1) / threads; }
 
 }  // namespace
@@ -271,7 +296,7 @@ extern "C" {
 
 size_t pcc_expert_sort_workspace_bytes(size_t tokens, int k, int experts) {
     if (!choices_ok(tokens, k, experts)) return 0;
-    const uint32_t segments = sort_segments(tokens * k);
+    const uint32_t segments = sort_segments(tokens * k, experts);
     return segments > 1 ? (size_t)segments * experts * sizeof(uint32_t) : 0;
 }
 
@@ -288,7 +313,7 @@ int pcc_expert_sort(const int32_t* d_expert, size_t tokens, int k, int experts, 
     if (overlap(place, {expert, offsets, space}) || overlap(offsets, {expert, space}) || overlap(space, expert)) return PCC_E_ARG;
     Sort a = {};
     a.expert = d_expert; a.offsets = d_offsets; a.place = d_place; a.counts = (uint32_t*)d_workspace;
-    a.entries = (uint32_t)entries; a.segment = sort_segment(entries); a.segments = sort_segments(entries); a.experts = experts; a.bits = log2_of(experts) + 1;
+    a.entries = (uint32_t)entries; a.segment = sort_segment(entries, experts); a.segments = sort_segments(entries, experts); a.experts = experts; a.bits = log2_of(experts) + 1;
     hipStream_t st = (hipStream_t)hip_stream;
     if (a.segments > 1) {
         const int rc = launch([&] { hipLaunchKernelGGL(expert_count_kernel, dim3(a.segments), dim3(kSortThreads), (size_t)experts * sizeof(uint32_t), st, a); });
@@ -307,11 +332,11 @@ int pcc_expert_rows(const void* d_x, size_t ldx, const int32_t* d_place, size_t 
     if (overlap(matrix(d_rows, rows, ldr, features, type), {matrix(d_x, tokens, ldx, features, type), piece(d_place, tokens * k * 4)})) return PCC_E_ARG;
     Experts a = {};
     a.x = d_x; a.place = d_place; a.y = d_rows; a.ldx = ldx; a.ldy = ldr; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    a.chunks = (uint32_t)(features + 7) / 8;
-    const uint64_t blocks = chunk_blocks(tokens, a.chunks, kExpertThreads);
-    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
-    auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); }); };
-    return type == PCC_FP32 ? go(expert_rows_kernel<Fp32>) : go(expert_rows_kernel<Bf16>);      // bits are copied
+    return with_tokens(a, [&](auto shape, dim3 grid) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); }); };
+        return type == PCC_FP32 ? go(expert_rows_kernel<Fp32, L, N>) : go(expert_rows_kernel<Bf16, L, N>);      // bits are copied
+    });
 }
 
 int pcc_expert_join(const void* d_z, size_t ldz, const int32_t* d_place, const float* d_weight, size_t tokens, int k, size_t rows, int features, int type,
@@ -322,12 +347,10 @@ int pcc_expert_join(const void* d_z, size_t ldz, const int32_t* d_place, const f
     if (overlap(matrix(d_y, tokens, ldy, features, y_type), {matrix(d_z, rows, ldz, features, type), piece(d_place, tokens * k * 4), piece(d_weight, tokens * k * 4)})) return PCC_E_ARG;
     Experts a = {};
     a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_y; a.ldz = ldz; a.ldy = ldy; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    a.chunks = (uint32_t)(features + 7) / 8;
-    const uint64_t blocks = chunk_blocks(tokens, a.chunks, kExpertThreads);
-    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
-    return with_row_types(type, y_type, [&](auto t, auto ty) {
-        return launch([&] {
-            hipLaunchKernelGGL((expert_join_kernel<decltype(t), decltype(ty)>), dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a);
+    return with_tokens(a, [&](auto shape, dim3 grid) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        return with_row_types(type, y_type, [&](auto t, auto ty) {
+            return launch([&] { hipLaunchKernelGGL((expert_join_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
         });
     });
 }
@@ -345,11 +368,10 @@ int pcc_expert_join_grad(const void* d_dy, int y_type, size_t lddy, const void* 
     Experts a = {};
     a.x = d_dy; a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_dz; a.dweight = d_dweight;
     a.ldx = lddy; a.ldz = ldz; a.ldy = lddz; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    const uint64_t blocks = (tokens + kExpertThreads / 64 - 1) / (kExpertThreads / 64);
-    if (!launchable(blocks, kExpertThreads)) return PCC_E_ARG;
-    return with_row_types(type, y_type, [&](auto t, auto ty) {
-        return launch([&] {
-            hipLaunchKernelGGL((expert_join_grad_kernel<decltype(t), decltype(ty)>), dim3((uint32_t)blocks), dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a);
+    return with_tokens(a, [&](auto shape, dim3 grid) {
+        constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
+        return with_row_types(type, y_type, [&](auto t, auto ty) {
+            return launch([&] { hipLaunchKernelGGL((expert_join_grad_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
         });
     });
 }

@@ -52,12 +52,14 @@ __global__ __launch_bounds__(kDropoutThreads) void dropout_kernel(Dropout a) {
     x.load(a.x, row * a.ldx + f, a.features - f);
     if (a.residual) y.load(a.residual, row * a.ldr + f, a.features - f);
     const Philox bits = philox({{chunk | (uint32_t)(row >> 32) << 16, (uint32_t)row, (uint32_t)step, (uint32_t)(step >> 32)}}, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+    float out[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const bool kept = ((bits.c[e / 2] >> (16 * (e & 1))) & 0xFFFFu) >= a.border;
         const float v = kept ? x.get(e) * a.scale : 0.0f;
-        y.set(e, a.residual ? y.get(e) + v : v);
+        out[e] = a.residual ? y.get(e) + v : v;
     }
+    y.set(out);
     y.store(a.y, row * a.ldy + f, a.features - f);
 }
 

@@ -65,20 +65,29 @@ __global__ __launch_bounds__(kSortThreads) void expert_place_kernel(Sort a) {
     }
     __syncthreads();
     for (int e = threadIdx.x; e < experts; e += kSortThreads) {
+        uint32_t t = 0;
+        if (a.segments == 1)
+            for (int w = 0; w < kSortWaves; ++w) t += sort_shared[w * experts + e];
+        before[e] = 0;
+        total[e] = t;
+    }
+    __syncthreads();
+    if (a.segments > 1) {
+        // a thread has an expert and every so many-th segment
+        const int slices = kSortThreads / experts, e = threadIdx.x % experts, slice = threadIdx.x / experts;
         uint32_t b = 0, t = 0;
-        if (a.segments > 1) {
-            for (uint32_t s = 0; s < a.segments; ++s) {
+        if (slice < slices) {
+#pragma unroll 8
+            for (uint32_t s = slice; s < a.segments; s += slices) {
                 const uint32_t c = a.counts[(size_t)s * experts + e];
                 b += s < blockIdx.x ? c : 0;
                 t += c;
             }
-        } else {
-            for (int w = 0; w < kSortWaves; ++w) t += sort_shared[w * experts + e];
+            atomicAdd(&before[e], b);       // whole numbers: in any order
+            atomicAdd(&total[e], t);
         }
-        before[e] = b;
-        total[e] = t;
+        __syncthreads();
     }
-    __syncthreads();
     // sums of the experts in front; there are at most as many as threads
     uint32_t own = (int)threadIdx.x < experts ? total[threadIdx.x] : 0, sum = wave_prefix(own);
     if (lane == 63) sums[wave] = sum;
@@ -131,77 +140,138 @@ struct Experts {
     size_t ldx, ldz, ldy;
     uint64_t tokens, rows;
     int k, features;
-    uint32_t chunks;        // eights of a row
+    uint32_t each;          // workgroups for each of the chip's eight dies
 };
 constexpr int kExpertThreads = 256;
 
-// A thread has eight neighbours of a token's row.
-template <class T>
+// A token's row has LANES lanes, parts of LANES * N eights one after the other.  A die has neighbouring tokens, whose rows of one expert are neighbours
+// as well and share lines of its L2.
+template <int LANES>
+__device__ __forceinline__ uint64_t token_of(const Experts& a) {
+    constexpr int kTeams = kExpertThreads / LANES;
+    return ((uint64_t)(blockIdx.x % 8) * a.each + blockIdx.x / 8) * kTeams + threadIdx.x / LANES;
+}
+
+template <class T, int LANES, int N>
 __global__ __launch_bounds__(kExpertThreads) void expert_rows_kernel(Experts a) {
-    const uint64_t id = (uint64_t)blockIdx.x * kExpertThreads + threadIdx.x, token = id / a.chunks;
+    const uint64_t token = token_of<LANES>(a);
     if (token >= a.tokens) return;
-    const int f = 8 * (int)(id - token * a.chunks);
-    Eight<T> x;
-    x.load(a.x, token * a.ldx + f, a.features - f);
-    for (int j = 0; j < a.k; ++j) {
-        const uint32_t at = (uint32_t)a.place[token * a.k + j];
-        if (at < a.rows) x.store(a.y, at * a.ldy + f, a.features - f);
-    }
-}
-
-template <class T, class Y>
-__global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) {
-    const uint64_t id = (uint64_t)blockIdx.x * kExpertThreads + threadIdx.x, token = id / a.chunks;
-    if (token >= a.tokens) return;
-    const int f = 8 * (int)(id - token * a.chunks);
-    float sum[8] = {};
-    for (int j = 0; j < a.k; ++j) {
-        const uint32_t at = (uint32_t)a.place[token * a.k + j];
-        if (at >= a.rows) continue;
-        const float w = a.weight ? a.weight[token * a.k + j] : 1.0f;
-        Eight<T> z;
-        z.load(a.z, at * a.ldz + f, a.features - f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf(w, z.get(e), sum[e]);
-    }
-    Eight<Y> y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y.set(e, sum[e]);
-    y.store(a.y, token * a.ldy + f, a.features - f);
-}
-
-// A wave has a token.
-template <class T, class Y>
-__global__ __launch_bounds__(kExpertThreads) void expert_join_grad_kernel(Experts a) {
-    const uint64_t token = (uint64_t)blockIdx.x * (kExpertThreads / 64) + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (token >= a.tokens) return;
-    for (int j = 0; j < a.k; ++j) {
-        const uint32_t at = (uint32_t)a.place[token * a.k + j];
-        const bool there = at < a.rows;
-        const float w = a.weight ? a.weight[token * a.k + j] : 1.0f;
-        float dot = 0.0f;
-        if (there)
-            for (int f = 8 * lane; f < a.features; f += 512) {
-                Eight<Y> dy;
-                dy.load(a.x, token * a.ldx + f, a.features - f);
-                if (a.dweight) {
-                    Eight<T> z;
-                    z.load(a.z, at * a.ldz + f, a.features - f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(dy.get(e), z.get(e), dot);
-                }
-                if (a.y) {
-                    Eight<T> dz;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dz.set(e, w * dy.get(e));
-                    dz.store(a.y, at * a.ldy + f, a.features - f);
-                }
-            }
-        if (a.dweight) {
-            dot = lanes_sum<64>(dot);
-            if (lane == 0) a.dweight[token * a.k + j] = there ? dot : 0.0f;
+    const int lane = threadIdx.x % LANES;
+    const int32_t* place = a.place + token * a.k;
+    for (int c0 = 0; c0 == 0 || c0 < a.features >> 3; c0 += LANES * N) {
+        const Extent w(a.features, c0, LANES * N, true);
+        Row<T, LANES, N> x;
+        x.load(a.x, token * a.ldx + 8 * c0, lane, w);
+        for (int j = 0; j < a.k; ++j) {
+            const uint32_t at = (uint32_t)place[j];
+            if (at < a.rows) Row<T, LANES, N>::each(lane, w, [&](auto, auto i) { x.store(i, a.y, at * a.ldy + 8 * c0, lane, w); });
         }
+    }
+}
+
+template <class T, class Y, int LANES, int N>
+__global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) {
+    constexpr int kAtOnce = 2;          // rows on their way
+    using Z = Row<T, LANES, N>;
+    const uint64_t token = token_of<LANES>(a);
+    if (token >= a.tokens) return;
+    const int lane = threadIdx.x % LANES;
+    for (int c0 = 0; c0 == 0 || c0 < a.features >> 3; c0 += LANES * N) {
+        const Extent w(a.features, c0, LANES * N, true);
+        Sums<LANES, N> sum;
+        sum.clear();
+        for (int j0 = 0; j0 < a.k; j0 += kAtOnce) {
+            Z z[kAtOnce];
+            float weight[kAtOnce];
+            bool there[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const bool more = j0 + j < a.k;
+                const uint32_t at = more ? (uint32_t)a.place[token * a.k + j0 + j] : ~0u;
+                there[j] = at < a.rows;
+                weight[j] = more && a.weight ? a.weight[token * a.k + j0 + j] : 1.0f;
+                z[j].load(a.z, at * a.ldz + 8 * c0, lane, Extent(a.features, c0, LANES * N, there[j]));
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                Z::each(lane, Extent(a.features, c0, LANES * N, there[j]), [&](auto wide, auto i) {
+#pragma unroll
+                    for (int e = 0; e < wide; ++e) sum.at(i)[e] = __builtin_fmaf(weight[j], z[j].at(i).get(e), sum.at(i)[e]);
+                });
+        }
+        Row<Y, LANES, N> y;
+        Z::each(lane, w, [&](auto, auto i) {
+            y.at(i).set(sum.at(i));
+            y.store(i, a.y, token * a.ldy + 8 * c0, lane, w);
+        });
+    }
+}
+
+template <class T, class Y, int LANES, int N>
+__global__ __launch_bounds__(kExpertThreads) void expert_join_grad_kernel(Experts a) {
+    constexpr int kAtOnce = 2, kWaves = LANES <= 64 ? 1 : LANES / 64;
+    using Z = Row<T, LANES, N>;
+    __shared__ float meet[2][kAtOnce][kWaves];
+    const uint64_t token = token_of<LANES>(a);
+    const bool mine = token < a.tokens;
+    const int lane = threadIdx.x % LANES, k = mine ? a.k : 0, most = LANES * N;
+    const bool one = (a.features >> 3) <= most;         // the whole row at once: dy is read once
+    Row<Y, LANES, N> dy;
+    if (one) dy.load(a.x, token * a.ldx, lane, Extent(a.features, mine));
+    int turn = 0;
+    for (int j0 = 0; j0 < a.k; j0 += kAtOnce, turn ^= 1) {
+        uint32_t at[kAtOnce];
+        float weight[kAtOnce], dot[kAtOnce] = {};
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            at[j] = j0 + j < k ? (uint32_t)a.place[token * a.k + j0 + j] : ~0u;
+            weight[j] = j0 + j < k && a.weight ? a.weight[token * a.k + j0 + j] : 1.0f;
+        }
+        for (int c0 = 0; c0 == 0 || c0 < a.features >> 3; c0 += most) {
+            if (!one) dy.load(a.x, token * a.ldx + 8 * c0, lane, Extent(a.features, c0, most, mine));
+            Z z[kAtOnce];
+            if (a.dweight)
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) z[j].load(a.z, at[j] * a.ldz + 8 * c0, lane, Extent(a.features, c0, most, at[j] < a.rows));
+            if (a.y)
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    const Extent w(a.features, c0, most, at[j] < a.rows);
+                    Z dz;
+                    Z::each(lane, w, [&](auto wide, auto i) {
+                        float v[8] = {};
+#pragma unroll
+                        for (int e = 0; e < wide; ++e) v[e] = weight[j] * dy.at(i).get(e);
+                        dz.at(i).set(v);
+                        dz.store(i, a.y, at[j] * a.ldy + 8 * c0, lane, w);
+                    });
+                }
+            if (a.dweight)
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    Z::each(lane, Extent(a.features, c0, most, at[j] < a.rows), [&](auto wide, auto i) {
+#pragma unroll
+                        for (int e = 0; e < wide; ++e) dot[j] = __builtin_fmaf(dy.at(i).get(e), z[j].at(i).get(e), dot[j]);
+                    });
+        }
+        if (!a.dweight) continue;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            dot[j] = lanes_sum<(LANES < 64 ? LANES : 64)>(dot[j]);
+            if (kWaves > 1 && (threadIdx.x & 63) == 0) meet[turn][j][lane >> 6] = dot[j];
+        }
+        if constexpr (kWaves > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                dot[j] = 0.0f;
+#pragma unroll
+                for (int v = 0; v < kWaves; ++v) dot[j] += meet[turn][j][v];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (lane == j && j0 + j < k) a.dweight[token * a.k + j0 + j] = dot[j];
     }
 }
 

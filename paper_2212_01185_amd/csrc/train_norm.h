@@ -69,11 +69,11 @@ struct Weights {
         eights = features >> 3;
         for (int c = threadIdx.x; c < eights; c += blockDim.x) {
             Eight<Fp32> w;
-            if (from) __builtin_memcpy(w.v, from + 8 * c, sizeof(w.v));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w.v[e] = from ? w.v[e] : none;
-            *reinterpret_cast<f32x4*>(at + 4 * c) = f32x4{w.v[0], w.v[1], w.v[2], w.v[3]};
-            *reinterpret_cast<f32x4*>(at + 4 * (eights + c)) = f32x4{w.v[4], w.v[5], w.v[6], w.v[7]};
+            if (from) w.load8(from + 8 * c);
+            const uint32_t bits = as_bits(none);
+            if (!from) w.words[0] = w.words[1] = u32x4{bits, bits, bits, bits};
+            *reinterpret_cast<u32x4*>(at + 4 * c) = w.words[0];
+            *reinterpret_cast<u32x4*>(at + 4 * (eights + c)) = w.words[1];
         }
         const int f = 8 * eights + threadIdx.x;
         if (f < features) at[f] = from ? from[f] : none;
@@ -83,11 +83,10 @@ struct Weights {
     __device__ __forceinline__ Eight<Fp32> get(int c) const {
         Eight<Fp32> w;
         if constexpr (WIDE == 8) {
-            const f32x4 p = *reinterpret_cast<const f32x4*>(at + 4 * c), q = *reinterpret_cast<const f32x4*>(at + 4 * (eights + c));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { w.v[e] = p[e]; w.v[4 + e] = q[e]; }
+            w.words[0] = *reinterpret_cast<const u32x4*>(at + 4 * c);
+            w.words[1] = *reinterpret_cast<const u32x4*>(at + 4 * (eights + c));
         } else {
-            w.v[0] = at[8 * eights + c];
+            w.one(at[8 * eights + c]);
         }
         return w;
     }
@@ -130,13 +129,13 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
         const Extent w(features, r0 + team < n);
         next.load(a.x, (size_t)(ch.lo + r0 + kTeams + team) * a.ldx, lane, Extent(features, r0 + kTeams + team < n));
         float sum = 0.0f, squares = 0.0f;
-        R::each(lane, w, [&](auto wide, int i) {
+        R::each(lane, w, [&](auto wide, auto i) {
 #pragma unroll
             for (int e = 0; e < wide; ++e) sum += x.at(i).get(e);
         });
         sum = lanes_sum<(LANES < 64 ? LANES : 64)>(sum);
         float mean = sum * own;         // of the wave's part
-        R::each(lane, w, [&](auto wide, int i) {
+        R::each(lane, w, [&](auto wide, auto i) {
 #pragma unroll
             for (int e = 0; e < wide; ++e) {
                 const float d = x.at(i).get(e) - mean;
@@ -168,11 +167,13 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
             a.stats[2 * row + 1] = scale;
         }
         Row<Y, LANES, N> y;
-        R::each(lane, w, [&](auto wide, int i) {
+        R::each(lane, w, [&](auto wide, auto i) {
             const int c = i < N ? lane + LANES * i : lane;
             const Eight<Fp32> g = gamma.get<wide>(c), b = beta.get<wide>(c);
+            float v[8] = {};
 #pragma unroll
-            for (int e = 0; e < wide; ++e) y.at(i).set(e, __builtin_fmaf(g.v[e], (x.at(i).get(e) - mean) * scale, b.v[e]));
+            for (int e = 0; e < wide; ++e) v[e] = __builtin_fmaf(g.get(e), (x.at(i).get(e) - mean) * scale, b.get(e));
+            y.at(i).set(v);
             y.store(i, a.y, row * a.ldy, lane, w);
         });
     };
@@ -187,6 +188,8 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
 template <class X, class Y, int LANES, int N>
 __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(Norm a) {
     constexpr int kTeams = norm_teams(LANES), kWaves = LANES <= 64 ? 1 : LANES / 64;
+    // 512 threads have 256 registers each at most: rows of fp32 leave no room for the next row there
+    constexpr bool kAhead = LANES < 512 || !kIs32<Y>;
     using R = Row<X, LANES, N>;
     __shared__ float meet[2][kTeams][2][kWaves];
     extern __shared__ __align__(16) float norm_weights[];
@@ -213,23 +216,23 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(No
     Weights gamma;
     gamma.fill(norm_weights, a.gamma ? a.gamma + (size_t)ch.group * features : nullptr, features, 1.0f);
     __syncthreads();
-    Row<Fp32, LANES, N> dg, db;         // the sums
+    Sums<LANES, N> dg, db;
     dg.clear();
     db.clear();
     auto step = [&](Held& h, Held& next, int r0, int turn) {
         const Extent w(features, r0 + team < n);
-        load(next, r0 + kTeams + team);
+        if (kAhead) load(next, r0 + kTeams + team);
         const float mean = h.mean, scale = h.scale;
         float s1 = 0.0f, s2 = 0.0f;
-        R::each(lane, w, [&](auto wide, int i) {
+        R::each(lane, w, [&](auto wide, auto i) {
             const Eight<Fp32> g = gamma.get<wide>(i < N ? lane + LANES * i : lane);
 #pragma unroll
             for (int e = 0; e < wide; ++e) {
-                const float d = h.dy.at(i).get(e), x = (h.x.at(i).get(e) - mean) * scale, u = d * g.v[e];
+                const float d = h.dy.at(i).get(e), x = (h.x.at(i).get(e) - mean) * scale, u = d * g.get(e);
                 s1 += u;
                 s2 = __builtin_fmaf(u, x, s2);
-                dg.at(i).v[e] = __builtin_fmaf(d, x, dg.at(i).v[e]);
-                db.at(i).v[e] += d;
+                dg.at(i)[e] = __builtin_fmaf(d, x, dg.at(i)[e]);
+                db.at(i)[e] += d;
             }
         });
         s1 = lanes_sum<(LANES < 64 ? LANES : 64)>(s1);
@@ -253,51 +256,51 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(No
             // scale (u - m1 - (x - mean) scale m2)
             const float m1 = -(scale * (s1 * a.inverse)), m2 = -(scale * scale * (s2 * a.inverse));
             R dx;
-            R::each(lane, w, [&](auto wide, int i) {
+            R::each(lane, w, [&](auto wide, auto i) {
                 const Eight<Fp32> g = gamma.get<wide>(i < N ? lane + LANES * i : lane);
+                float v[8] = {};
 #pragma unroll
-                for (int e = 0; e < wide; ++e)
-                    dx.at(i).set(e, __builtin_fmaf(h.x.at(i).get(e) - mean, m2, __builtin_fmaf(h.dy.at(i).get(e) * g.v[e], scale, m1)));
+                for (int e = 0; e < wide; ++e) v[e] = __builtin_fmaf(h.x.at(i).get(e) - mean, m2, __builtin_fmaf(h.dy.at(i).get(e) * g.get(e), scale, m1));
+                dx.at(i).set(v);
                 dx.store(i, a.y, (size_t)(ch.lo + r0 + team) * a.ldy, lane, w);
             });
         }
+        if (!kAhead) load(next, r0 + kTeams + team);
     };
     for (int r0 = 0; r0 < n; r0 += 2 * kTeams) {
-        step(held, then, r0, 0);
+        step(held, kAhead ? then : held, r0, 0);
         if (r0 + kTeams >= n) break;
-        step(then, held, r0 + kTeams, 1);
+        step(kAhead ? then : held, held, r0 + kTeams, 1);
     }
     if (!a.dgamma) return;
     float* to = ch.count == 1 ? a.dgamma + (size_t)ch.group * features : a.partial + (size_t)ch.shared * 2 * features;
     float* to_beta = ch.count == 1 ? a.dbeta + (size_t)ch.group * features : to + features;
     const Extent all(features, true);
     if constexpr (LANES >= 256) {
-        R::each(lane, all, [&](auto, int i) {
-            dg.store(i, to, 0, lane, all);
-            db.store(i, to_beta, 0, lane, all);
+        R::each(lane, all, [&](auto, auto i) {
+            Row<Fp32, LANES, N> out;
+            out.at(i).set(dg.at(i));
+            out.store(i, to, 0, lane, all);
+            out.at(i).set(db.at(i));
+            out.store(i, to_beta, 0, lane, all);
         });
     } else {
         // the rows of a wave by exchanges, then those of the waves or teams, kShares of them, through LDS (where the weights were)
         constexpr int kShares = LANES <= 64 ? 4 : kTeams;
         const int share = LANES <= 64 ? threadIdx.x >> 6 : team;
         if constexpr (LANES < 64) {
-#pragma unroll
-            for (int i = 0; i <= N; ++i)
-#pragma unroll
-                for (int e = 0; e < (i < N ? 8 : 1); ++e) {
-                    dg.at(i).v[e] = groups_sum<LANES>(dg.at(i).v[e]);
-                    db.at(i).v[e] = groups_sum<LANES>(db.at(i).v[e]);
-                }
+            dg.sum_groups();
+            db.sum_groups();
         }
         __syncthreads();
         const int pitch = (int)Weights::values(features);
         if (LANES >= 64 || (int)(threadIdx.x & 63) < LANES)
-            R::each(lane, all, [&](auto wide, int i) {
+            R::each(lane, all, [&](auto wide, auto i) {
                 float* at = norm_weights + 2 * share * pitch + (i < N ? 8 * (lane + LANES * i) : 8 * all.eights + lane);
 #pragma unroll
                 for (int e = 0; e < wide; ++e) {
-                    at[e] = dg.at(i).v[e];
-                    at[pitch + e] = db.at(i).v[e];
+                    at[e] = dg.at(i)[e];
+                    at[pitch + e] = db.at(i)[e];
                 }
             });
         __syncthreads();
@@ -355,8 +358,10 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_long_kernel(Norm a) {
             x.load(a.x, at + f, a.features - f);
             if (gamma) w.load(gamma, f, a.features - f);
             if (beta) b.load(beta, f, a.features - f);
+            float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y.set(e, __builtin_fmaf(gamma ? w.get(e) : 1.0f, (x.get(e) - mean) * scale, beta ? b.get(e) : 0.0f));
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(gamma ? w.get(e) : 1.0f, (x.get(e) - mean) * scale, beta ? b.get(e) : 0.0f);
+            y.set(v);
             y.store(a.y, (size_t)row * a.ldy + f, a.features - f);
         }
     }
@@ -380,16 +385,17 @@ __global__ __launch_bounds__(kLongThreads) void layer_norm_long_dx_kernel(Norm a
                 x.load(a.x, (size_t)row * a.ldx + f, a.features - f);
                 dy.load(a.dy, (size_t)row * a.lddy + f, a.features - f);
                 if (gamma) w.load(gamma, f, a.features - f);
+                float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float u = dy.get(e) * (gamma ? w.get(e) : 1.0f), h = (x.get(e) - mean) * scale;
                     if (pass == 0) {
                         s1 += f + e < a.features ? u : 0.0f;
                         s2 += f + e < a.features ? u * h : 0.0f;
-                    } else {
-                        dx.set(e, scale * (u - s1 - h * s2));
                     }
+                    v[e] = scale * (u - s1 - h * s2);
                 }
+                dx.set(v);
                 if (pass == 1) dx.store(a.y, (size_t)row * a.ldy + f, a.features - f);
             }
             if (pass == 0) {

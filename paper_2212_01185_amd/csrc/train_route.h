@@ -143,8 +143,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
         const int f = 8 * (lane + LANES * i);
         if (f >= a.experts) continue;
         Eight<T> out;
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out.set(e, d[8 * i + e]);
+        for (int e = 0; e < 8; ++e) v[e] = d[8 * i + e];
+        out.set(v);
         out.store(a.dlogits, t * a.lddl + f, a.experts - f);
     }
 }

@@ -17,95 +17,89 @@ constexpr bool kIs32 = std::is_same_v<T, Fp32>;
 template <class T>
 using element_of = std::conditional_t<kIs32<T>, float, u16>;
 
-// Eight values of a row as memory has them: 16 or 32 bytes.
+// (Values, not elements of a vector: __builtin_bit_cast takes the first one's place of such.)
+__device__ __forceinline__ float as_float(uint32_t bits) { return __builtin_bit_cast(float, bits); }
+__device__ __forceinline__ uint32_t as_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+
+// 16 bytes at an address that an element of SIZE bytes may have.
+template <int SIZE>
+struct Anywhere;
+template <>
+struct Anywhere<2> {
+    typedef u32x4 type __attribute__((aligned(2)));
+};
+template <>
+struct Anywhere<4> {
+    typedef u32x4 type __attribute__((aligned(4)));
+};
+
+// Eight values of a row as memory has them: 16 or 32 bytes, at any address that an element may have.
 template <class T>
 struct Eight {
-    element_of<T> v[8];
+    static constexpr int kWords = kIs32<T> ? 2 : 1;
+    using Place = Anywhere<sizeof(element_of<T>)>;
+    u32x4 words[kWords];
 
-    // From the element `at` on, n of them (8 at most), and zeros.  Whole ones are one load (two of fp32) at any address.
+    __device__ __forceinline__ void load8(const element_of<T>* from) {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) words[k] = reinterpret_cast<const typename Place::type*>(from)[k];
+    }
+    __device__ __forceinline__ void store8(element_of<T>* to) const {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) reinterpret_cast<typename Place::type*>(to)[k] = words[k];
+    }
+    __device__ __forceinline__ element_of<T> element(int e) const {
+        if constexpr (kIs32<T>) return as_float(words[e / 4][e % 4]);
+        else return (u16)(words[0][e / 2] >> (16 * (e % 2)));
+    }
+    __device__ __forceinline__ void one(element_of<T> v) {      // the first, and zeros
+        clear();
+        if constexpr (kIs32<T>) words[0][0] = as_bits(v);
+        else words[0][0] = v;
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) words[k] = u32x4{0, 0, 0, 0};
+    }
+    // The n values from the element `at` on (8 at most), and zeros.
     __device__ __forceinline__ void load(const void* base, size_t at, int n) {
         const element_of<T>* from = static_cast<const element_of<T>*>(base) + at;
         if (n >= 8) {
-            __builtin_memcpy(v, from, sizeof(v));
+            load8(from);
         } else {
+            clear();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? from[e] : element_of<T>{};
+            for (int e = 0; e < 7; ++e) {
+                if (e >= n) continue;
+                if constexpr (kIs32<T>) words[e / 4][e % 4] = as_bits(from[e]);
+                else words[0][e / 2] |= (uint32_t)from[e] << (16 * (e % 2));
+            }
         }
     }
     __device__ __forceinline__ void store(void* base, size_t at, int n) const {
         element_of<T>* to = static_cast<element_of<T>*>(base) + at;
         if (n >= 8) {
-            __builtin_memcpy(to, v, sizeof(v));
+            store8(to);
         } else {
 #pragma unroll
             for (int e = 0; e < 7; ++e)
-                if (e < n) to[e] = v[e];
+                if (e < n) to[e] = element(e);
         }
     }
     __device__ __forceinline__ float get(int e) const {
-        if constexpr (kIs32<T>) return v[e];
-        else return from16<T>(v[e]);
+        if constexpr (kIs32<T>) return as_float(words[e / 4][e % 4]);
+        else if constexpr (std::is_same_v<T, Bf16>) return as_float(e % 2 ? words[0][e / 2] & 0xFFFF0000u : words[0][e / 2] << 16);
+        else return from16<T>((u16)(words[0][e / 2] >> (16 * (e % 2))));
     }
-    __device__ __forceinline__ void set(int e, float value) {       // to the nearest, ties to even
-        if constexpr (kIs32<T>) v[e] = value;
-        else v[e] = to16<T>(value);
-    }
-};
-
-// A row that LANES lanes (8 at least) share: lane l has the eights l, l + LANES, ..., N of them at most, and of the up to seven features behind the last
-// whole eight the l-th.
-struct Extent {
-    int eights, rest;       // of a row; 0 for a row that is not there
-
-    __device__ __forceinline__ Extent(int features, bool there) : eights(there ? features >> 3 : 0), rest(there ? features & 7 : 0) {}
-};
-
-template <class T, int LANES, int N>
-struct Row {
-    static_assert(LANES >= 8, "the features behind the last eight have a lane each");
-    Eight<T> v[N];
-    Eight<T> tail;          // the first value
-
-    // f(i, eight) for the eights that are this lane's, then f(N, eight of one value) for its value of the rest.
-    template <class F>
-    static __device__ __forceinline__ void each(int lane, Extent w, F&& f) {
+    // All eight, to the nearest, ties to even.
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        if constexpr (kIs32<T>) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (lane + LANES * i < w.eights) f(std::integral_constant<int, 8>{}, i);
-        if (lane < w.rest) f(std::integral_constant<int, 1>{}, N);
-    }
-    __device__ __forceinline__ Eight<T>& at(int i) { return i < N ? v[i < N ? i : 0] : tail; }
-    __device__ __forceinline__ const Eight<T>& at(int i) const { return i < N ? v[i < N ? i : 0] : tail; }
-
-    __device__ __forceinline__ void load(const void* base, size_t at0, int lane, Extent w) {
-        const element_of<T>* from = static_cast<const element_of<T>*>(base) + at0;
+            for (int e = 0; e < 8; ++e) words[e / 4][e % 4] = as_bits(v[e]);
+        } else {
+            typedef __attribute__((ext_vector_type(2))) typename T::value pair;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (lane + LANES * i < w.eights) __builtin_memcpy(v[i].v, from + 8 * (lane + LANES * i), sizeof(v[i].v));
-        if (lane < w.rest) tail.v[0] = from[8 * w.eights + lane];
-    }
-    __device__ __forceinline__ void store(int i, void* base, size_t at0, int lane, Extent w) const {
-        element_of<T>* to = static_cast<element_of<T>*>(base) + at0;
-        if (i < N) __builtin_memcpy(to + 8 * (lane + LANES * i), v[i < N ? i : 0].v, sizeof(v[0].v));
-        else to[8 * w.eights + lane] = tail.v[0];
-    }
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i].v[e] = element_of<T>{};
-        tail.v[0] = element_of<T>{};
-    }
-    // What was made of the values is made anew behind this, not kept: a value takes half a register as it came.
-    __device__ __forceinline__ void forget() {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            constexpr int kWords = sizeof(v[0].v) / 16;
-            u32x4 words[kWords];
-            __builtin_memcpy(words, v[i].v, sizeof(words));
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) asm("" : "+v"(words[k]));
-            __builtin_memcpy(v[i].v, words, sizeof(words));
+            for (int e = 0; e < 8; e += 2) words[0][e / 2] = __builtin_bit_cast(uint32_t, pair{(typename T::value)v[e], (typename T::value)v[e + 1]});
         }
     }
 };
@@ -158,5 +152,89 @@ __device__ __forceinline__ float groups_sum(float v) {
     }
     return v;
 }
+
+// A row that LANES lanes (8 at least) share: lane l has the eights l, l + LANES, ..., N of them at most, and of the up to seven features behind the last
+// whole eight the l-th.
+struct Extent {
+    int eights, rest;       // of a row; 0 for a row that is not there
+
+    __device__ __forceinline__ Extent(int features, bool there) : eights(there ? features >> 3 : 0), rest(there ? features & 7 : 0) {}
+    // Of a part of a row: `most` eights from eight c0 on, and in the last part the rest.
+    __device__ __forceinline__ Extent(int features, int c0, int most, bool there) {
+        const int left = (features >> 3) - c0;
+        eights = !there ? 0 : left < most ? left : most;
+        rest = there && left <= most ? features & 7 : 0;
+    }
+};
+
+template <class T, int LANES, int N>
+struct Row {
+    static_assert(LANES >= 8, "the features behind the last eight have a lane each");
+    Eight<T> v[N], tail;    // of the tail the first value
+
+    // f(8, i) for the eights that are this lane's, then f(1, N) for its value of the rest; both numbers are types.
+    template <int I = 0, class F>
+    static __device__ __forceinline__ void each(int lane, Extent w, F&& f) {
+        if constexpr (I < N) {
+            if (lane + LANES * I < w.eights) f(std::integral_constant<int, 8>{}, std::integral_constant<int, I>{});
+            each<I + 1>(lane, w, f);
+        } else {
+            if (lane < w.rest) f(std::integral_constant<int, 1>{}, std::integral_constant<int, N>{});
+        }
+    }
+    template <int I>
+    __device__ __forceinline__ Eight<T>& at(std::integral_constant<int, I>) {
+        if constexpr (I < N) return v[I];
+        else return tail;
+    }
+    __device__ __forceinline__ void load(const void* base, size_t at0, int lane, Extent w) {
+        const element_of<T>* from = static_cast<const element_of<T>*>(base) + at0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (lane + LANES * i < w.eights) v[i].load8(from + 8 * (lane + LANES * i));
+        if (lane < w.rest) tail.one(from[8 * w.eights + lane]);
+    }
+    template <int I>
+    __device__ __forceinline__ void store(std::integral_constant<int, I>, void* base, size_t at0, int lane, Extent w) const {
+        element_of<T>* to = static_cast<element_of<T>*>(base) + at0;
+        if constexpr (I < N) v[I].store8(to + 8 * (lane + LANES * I));
+        else to[8 * w.eights + lane] = tail.element(0);
+    }
+    // What was made of the values is made anew behind this, not kept: a value takes half a register as it came.
+    __device__ __forceinline__ void forget() {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int k = 0; k < Eight<T>::kWords; ++k) asm("" : "+v"(v[i].words[k]));
+    }
+};
+
+// Sums in fp32 of a row's features, as `Row` deals them out.
+template <int LANES, int N>
+struct Sums {
+    float v[N][8], tail[8];
+
+    template <int I>
+    __device__ __forceinline__ float (&at(std::integral_constant<int, I>))[8] {
+        if constexpr (I < N) return v[I];
+        else return tail;
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i][e] = 0.0f;
+            tail[e] = 0.0f;
+        }
+    }
+    // Over the rows of a wave.
+    __device__ __forceinline__ void sum_groups() {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = groups_sum<LANES>(v[i][e]);
+        tail[0] = groups_sum<LANES>(tail[0]);
+    }
+};
 
 }  // namespace pcc_train
