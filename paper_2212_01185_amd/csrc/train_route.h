@@ -22,13 +22,69 @@ struct Route {
 };
 constexpr int kRouteThreads = 256;
 
-// Bits that are ordered as the numbers are, a NaN last.
-__device__ __forceinline__ uint32_t ordered(float v) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
-    return v != v ? 0xFFFFFFFFu : b >> 31 ? ~b : b | 0x80000000u;
+// A logit and its expert as one whole number: larger for larger logits, and for lower experts where they are equal.  0: never to be chosen.
+template <class T>
+struct RouteKey {
+    static constexpr int kBits = kIs32<T> ? 32 : 16;
+    using type = std::conditional_t<kIs32<T>, uint64_t, uint32_t>;
+    static constexpr uint32_t kSign = 1u << (kBits - 1), kAll = kSign | (kSign - 1);
+
+    static __device__ __forceinline__ type of(element_of<T> element, float v, uint32_t expert) {
+        uint32_t b;
+        if constexpr (kIs32<T>) b = as_bits(v);
+        else b = element;
+        b = v != v ? kAll : b & kSign ? (0 - b) & kAll : b | kSign;      // both zeros are one
+        return v == -__builtin_inff() ? 0 : (type)b << kBits | (kAll ^ expert);
+    }
+    static __device__ __forceinline__ float logit(type key) {
+        const uint32_t b = (uint32_t)(key >> kBits), e = b & kSign ? b ^ kSign : (0 - b) & kAll;
+        if constexpr (kIs32<T>) return as_float(e);
+        else return from16<T>((u16)e);
+    }
+    static __device__ __forceinline__ int expert(type key) { return (int)((uint32_t)key & kAll ^ kAll); }
+};
+
+template <int G>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    return over_lanes<G>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
-__device__ __forceinline__ float unordered(uint32_t key) { return __builtin_bit_cast(float, key >> 31 ? key & 0x7FFFFFFFu : ~key); }
-constexpr uint32_t kNever = 0x007FFFFFu;        // ordered(-inf)
+template <int G>
+__device__ __forceinline__ uint64_t lanes_max(uint64_t v) {
+    auto step = [&](uint32_t low, uint32_t high) {
+        const uint64_t other = (uint64_t)high << 32 | low;
+        v = other > v ? other : v;
+    };
+    auto low = [&] { return (uint32_t)v; };
+    auto high = [&] { return (uint32_t)(v >> 32); };
+    if constexpr (G >= 2) step(moved<kSwapPairs>(low()), moved<kSwapPairs>(high()));
+    if constexpr (G >= 4) step(moved<kSwapTwos>(low()), moved<kSwapTwos>(high()));
+    if constexpr (G >= 8) step(moved<kMirrorEight>(low()), moved<kMirrorEight>(high()));
+    if constexpr (G >= 16) step(moved<kMirrorRow>(low()), moved<kMirrorRow>(high()));
+    if constexpr (G >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(low(), low(), false, false), q = __builtin_amdgcn_permlane16_swap(high(), high(), false, false);
+        v = (uint64_t)q[0] << 32 | p[0];
+        step(p[1], q[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(low(), low(), false, false), q = __builtin_amdgcn_permlane32_swap(high(), high(), false, false);
+        v = (uint64_t)q[0] << 32 | p[0];
+        step(p[1], q[1]);
+    }
+    return v;
+}
+
+// Eight keys, the largest first (merging by odd and even places, 19 comparisons).
+template <class K>
+__device__ __forceinline__ void sort_eight(K (&k)[8]) {
+    constexpr int kPairs[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                                   {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+    for (int i = 0; i < 19; ++i) {
+        const K a = k[kPairs[i][0]], b = k[kPairs[i][1]];
+        k[kPairs[i][0]] = a > b ? a : b;
+        k[kPairs[i][1]] = a > b ? b : a;
+    }
+}
 
 // e^v for v <= 0 (and NaN), with what the rounding of v log2(e) left out.
 __device__ __forceinline__ float exp_below(float v) {
@@ -37,116 +93,145 @@ __device__ __forceinline__ float exp_below(float v) {
     return __builtin_fmaf(e, __builtin_fmaf(b, 1.925962989e-8f, __builtin_fmaf(b, kLog2e, -t)) * kLn2, e);
 }
 
-// LANES lanes have a token, eight neighbouring logits each, N times.
+// LANES lanes have a token, eight neighbouring logits each, N times.  Each lane sorts its own; then the largest of all lanes' first ones is taken off
+// its list, k times, and choice j is kept by lane j % LANES.
 template <class T, int LANES, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
+    using Key = RouteKey<T>;
+    constexpr int kSlots = LANES >= PCC_MAX_CHOICES ? 1 : LANES == 1 ? 8 : PCC_MAX_CHOICES / LANES;    // (k is at most the number of experts)
     const uint64_t t0 = (uint64_t)blockIdx.x * (kRouteThreads / LANES) + threadIdx.x / LANES;
     const bool mine = t0 < a.tokens;
     const uint64_t t = mine ? t0 : a.tokens - 1;
     const int lane = threadIdx.x % LANES;
-    uint32_t key[8 * N];
-    float all = 0.0f, top = 0.0f, total = 0.0f;
+    Eight<T> l[N];
+    typename Key::type key[N][8], held[kSlots] = {}, top = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int f = 8 * (lane + LANES * i);
-        Eight<T> l;
-        l.load(a.logits, t * a.ldl + f, a.experts - f);
+        l[i].load(a.logits, t * a.ldl + f, a.experts - f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) key[8 * i + e] = f + e < a.experts ? ordered(l.get(e)) : 0u;
+        for (int e = 0; e < 8; ++e) key[i][e] = f + e < a.experts ? Key::of(l[i].element(e), l[i].get(e), (uint32_t)(f + e)) : 0;
+        sort_eight(key[i]);
     }
-    for (int j = 0; j < a.k; ++j) {
-        uint32_t best = 0;
 #pragma unroll
-        for (int i = 0; i < 8 * N; ++i) best = key[i] > best ? key[i] : best;
-        best = over_lanes<LANES>(best, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
-        uint32_t index = 0xFFFFFFFFu;
+    for (int s = 0; s < kSlots; ++s) {
+        for (int u = 0; u < LANES && s * LANES + u < a.k; ++u) {
+            typename Key::type best = key[0][0];
 #pragma unroll
-        for (int i = 8 * N - 1; i >= 0; --i) index = key[i] == best ? (uint32_t)(8 * (lane + LANES * (i / 8)) + i % 8) : index;
-        index = over_lanes<LANES>(index, [](uint32_t p, uint32_t q) { return p < q ? p : q; });
-        const bool taken = best > kNever;
-        if (j == 0) {
-            top = taken ? unordered(best) : 0.0f;
-            if (a.over_all) {
+            for (int i = 1; i < N; ++i) best = key[i][0] > best ? key[i][0] : best;
+            best = lanes_max<LANES>(best);
+            if (s == 0 && u == 0) top = best;
+            if (lane == u) held[s] = best;
 #pragma unroll
-                for (int i = 0; i < 8 * N; ++i) all += key[i] > kNever ? exp_below(unordered(key[i]) - top) : 0.0f;
-                all = lanes_sum<LANES>(all);
+            for (int i = 0; i < N; ++i) {
+                const bool taken = key[i][0] == best;
+#pragma unroll
+                for (int e = 0; e < 7; ++e) key[i][e] = taken ? key[i][e + 1] : key[i][e];
+                key[i][7] = taken ? 0 : key[i][7];
             }
         }
-        const float size = taken ? exp_below(unordered(best) - top) : 0.0f;
-        total += size;
-        if (mine && lane == 0) {
-            a.expert[t * a.k + j] = taken ? (int32_t)index : -1;
-            a.weight[t * a.k + j] = size;
-        }
-#pragma unroll
-        for (int i = 0; i < 8 * N; ++i)
-            if ((uint32_t)(8 * (lane + LANES * (i / 8)) + i % 8) == index) key[i] = 0;
     }
-    if (mine && lane == 0) {
-        const float by = a.over_all ? all : total;
-        for (int j = 0; j < a.k; ++j) {
-            const float size = a.weight[t * a.k + j];
-            a.weight[t * a.k + j] = a.expert[t * a.k + j] >= 0 ? size / by : 0.0f;
-        }
+    const float highest = top ? Key::logit(top) : 0.0f;
+    float total = 0.0f, size[kSlots];
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+        size[s] = held[s] ? exp_below(Key::logit(held[s]) - highest) : 0.0f;
+        total += size[s];
+    }
+    if (a.over_all) {
+        total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) total += 8 * (lane + LANES * i) + e < a.experts ? exp_below(l[i].get(e) - highest) : 0.0f;
+    }
+    total = lanes_sum<LANES>(total);
+    if (!mine) return;
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+        const int j = s * LANES + lane;
+        if (j >= a.k) continue;
+        a.expert[t * a.k + j] = held[s] ? Key::expert(held[s]) : -1;
+        a.weight[t * a.k + j] = held[s] ? size[s] / total : 0.0f;
     }
 }
 
+// A wave's tokens have a place in LDS for each logit: zeros, then what each choice brings is put in its expert's, by the lane that kept it.
 template <class T, int LANES, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
+    constexpr int kSlots = LANES >= PCC_MAX_CHOICES ? 1 : LANES == 1 ? 8 : PCC_MAX_CHOICES / LANES;
+    __shared__ __align__(16) float brought[kRouteThreads * 8 * N];
     const uint64_t t0 = (uint64_t)blockIdx.x * (kRouteThreads / LANES) + threadIdx.x / LANES;
     const bool mine = t0 < a.tokens;
     const uint64_t t = mine ? t0 : a.tokens - 1;
     const int lane = threadIdx.x % LANES;
-    float p[8 * N], along = 0.0f;
-    if (a.over_all) {
-        uint32_t best = 0;
-        float all = 0.0f;
+    float* own = brought + threadIdx.x / LANES * (LANES * 8 * N);
+    Eight<T> l[N];
+    int expert[kSlots];
+    float w[kSlots], dw[kSlots], along = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int f = 8 * (lane + LANES * i);
-            Eight<T> l;
-            l.load(a.logits, t * a.ldl + f, a.experts - f);
+    for (int s = 0; s < kSlots; ++s) {
+        const int j = s * LANES + lane;
+        const bool there = j < a.k;
+        expert[s] = there ? a.expert[t * a.k + j] : -1;
+        w[s] = there ? a.weight[t * a.k + j] : 0.0f;
+        dw[s] = there ? a.dweight[t * a.k + j] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int f = 8 * (lane + LANES * i);
+        if (a.over_all) l[i].load(a.logits, t * a.ldl + f, a.experts - f);
+        f32x4* zeros = reinterpret_cast<f32x4*>(own + f);
+        zeros[0] = zeros[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s) {
+        if ((uint32_t)expert[s] >= (uint32_t)a.experts) expert[s] = -1;
+        along += expert[s] >= 0 ? w[s] * dw[s] : 0.0f;
+    }
+    along = lanes_sum<LANES>(along);
+    __builtin_amdgcn_wave_barrier();        // a token's lanes are in one wave
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s)
+        if (expert[s] >= 0) own[expert[s]] = a.over_all ? dw[s] : w[s] * (dw[s] - along);
+    float top = -__builtin_inff(), all = 0.0f;
+    if (a.over_all) {
+        // (a NaN does not become the largest: it shows in the sum)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                p[8 * i + e] = f + e < a.experts ? l.get(e) : -__builtin_inff();
-                const uint32_t o = ordered(p[8 * i + e]);
-                best = o > best ? o : best;
+                const float v = 8 * (lane + LANES * i) + e < a.experts ? l[i].get(e) : -__builtin_inff();
+                top = v > top ? v : top;
             }
-        }
-        best = over_lanes<LANES>(best, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-        const float top = best > kNever ? unordered(best) : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8 * N; ++i) {
-            p[i] = p[i] == -__builtin_inff() ? 0.0f : exp_below(p[i] - top);
-            all += p[i];
-        }
-        all = lanes_sum<LANES>(all);
-        const float inverse = all == 0.0f ? 0.0f : 1.0f / all;
-#pragma unroll
-        for (int i = 0; i < 8 * N; ++i) p[i] *= inverse;
+        top = over_lanes<LANES>(top, [](float x, float y) { return x > y ? x : y; });
+        top = top == -__builtin_inff() ? 0.0f : top;
     }
-    for (int j = 0; j < a.k; ++j)
-        if (a.expert[t * a.k + j] >= 0) along += a.weight[t * a.k + j] * a.dweight[t * a.k + j];
-    float d[8 * N];
+    float p[N][8];
 #pragma unroll
-    for (int i = 0; i < 8 * N; ++i) d[i] = a.over_all ? -along * p[i] : 0.0f;
-    for (int j = 0; j < a.k; ++j) {
-        const int expert = a.expert[t * a.k + j];
-        const float w = a.weight[t * a.k + j], dw = a.dweight[t * a.k + j];
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int i = 0; i < 8 * N; ++i)
-            if (8 * (lane + LANES * (i / 8)) + i % 8 == expert) d[i] = a.over_all ? p[i] * (dw - along) : w * (dw - along);
-    }
+        for (int e = 0; e < 8; ++e) {
+            p[i][e] = a.over_all && 8 * (lane + LANES * i) + e < a.experts ? exp_below(l[i].get(e) - top) : 0.0f;
+            all += p[i][e];
+        }
+    all = lanes_sum<LANES>(all);
+    const float inverse = all == 0.0f ? 0.0f : 1.0f / all;
+    __builtin_amdgcn_wave_barrier();
     if (!mine) return;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int f = 8 * (lane + LANES * i);
         if (f >= a.experts) continue;
-        Eight<T> out;
-        float v[8];
+        const f32x4 low = *reinterpret_cast<const f32x4*>(own + f), high = *reinterpret_cast<const f32x4*>(own + f + 4);
+        float d[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = d[8 * i + e];
-        out.set(v);
+        for (int e = 0; e < 8; ++e) {
+            const float g = e < 4 ? low[e] : high[e - 4];
+            d[e] = a.over_all ? p[i][e] * inverse * (g - along) : g;
+        }
+        Eight<T> out;
+        out.set(d);
         out.store(a.dlogits, t * a.lddl + f, a.experts - f);
     }
 }

@@ -234,6 +234,14 @@ def test_route(experts, k, over_all):
         assert (full[:, experts:] == 5).all() and (got[l == -float("inf")] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [FP32, BF16, FP16])
+def test_route_zeros_of_both_signs_are_equal(dtype):
+    l = torch.zeros(3, 9, dtype=dtype)
+    l[0, ::2], l[1, :5], l[2, 4:] = -0.0, -0.0, -0.0
+    expert, weight = binding.pcc_route(l.cuda(), 4)
+    assert expert.tolist() == [[0, 1, 2, 3]] * 3 and (weight == 0.25).all()
+
+
 def test_route_nan_and_infinity():
     l = torch.zeros(4, 12)
     l[0, 7], l[1, 3], l[1, 9], l[2, 5] = float("nan"), float("inf"), -float("nan"), float("inf")
