@@ -54,16 +54,17 @@ int log2_of(int v) { return v <= 1 ? 0 : 1 + log2_of(v / 2); }
 
 // Chunks of whole turns of a workgroup's teams, `want` of them at most if there are not too many groups for that: as many as run at once, for a
 // workgroup's start (weights) and end (sums) are worth some rows.
-void norm_chunks(size_t rows, int groups, int want, int lanes, int& log2, uint32_t& mult) {
+void norm_chunks(size_t rows, int groups, int want, int teams, int& log2, uint32_t& mult) {
     const size_t whole = groups == 1 ? want : want > 2 * groups ? want - groups : want / 2 + 1, least = (rows + whole - 1) / whole;
-    log2 = log2_of(norm_teams(lanes));
+    log2 = log2_of(teams);
     while (log2 < 24 && ((size_t)64 << log2) < least) ++log2;
     mult = (uint32_t)std::min<size_t>(std::max<size_t>((least + ((size_t)1 << log2) - 1) >> log2, 1), 64);
 }
-// Chunks whose sums are joined: two workgroups of 256 threads a compute unit by their registers.
+// Chunks whose sums are joined: as many workgroups as run at once by their registers.
 void sums_chunks(size_t rows, int groups, int features, int& log2, uint32_t& mult) {
-    const int lanes = with_row_shape(features, [](auto shape) { return decltype(shape)::kLanes; });
-    norm_chunks(rows, groups, features < 72 ? 1280 : lanes <= 256 ? 512 : 256, lanes, log2, mult);
+    const int threads = with_row_shape(features, [](auto shape) { return norm_grad_threads(decltype(shape)::kLanes, decltype(shape)::kChunks); });
+    const int teams = with_row_shape(features, [](auto shape) { return std::max(1, norm_grad_teams(decltype(shape)::kLanes, decltype(shape)::kChunks)); });
+    norm_chunks(rows, groups, threads == 256 ? 1280 : 256, teams, log2, mult);
 }
 
 }  // namespace
@@ -85,7 +86,7 @@ int pcc_layer_norm(const void* d_x, size_t ldx, const float* d_gamma, const floa
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.eps = eps; a.inverse = 1.0f / (float)features;
     return with_row_shape(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        norm_chunks(rows, groups, L <= 64 ? 2048 : L == 128 ? 1024 : L == 256 ? 512 : 256, L, a.log2, a.mult);
+        norm_chunks(rows, groups, L <= 64 ? 2048 : L == 128 ? 1024 : L == 256 ? 512 : 256, norm_teams(L), a.log2, a.mult);
         const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
         if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
         return with_norm_types(type, y_type, [&](auto tx, auto ty) {
@@ -137,7 +138,7 @@ int pcc_layer_norm_grad(const void* d_dy, int y_type, size_t lddy, const void* d
             using Y = decltype(ty);
             if constexpr (N == 0) {
                 if (d_dx && rows) {
-                    norm_chunks(rows, groups, 2048, kLongThreads, a.log2, a.mult);
+                    norm_chunks(rows, groups, 2048, 1, a.log2, a.mult);
                     const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
                     if (!launchable(blocks, kLongThreads)) return PCC_E_ARG;
                     const int rc = launch([&] {
@@ -155,11 +156,11 @@ int pcc_layer_norm_grad(const void* d_dy, int y_type, size_t lddy, const void* d
             } else {
                 sums_chunks(rows, groups, features, a.log2, a.mult);
                 const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
-                if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
-                const size_t lds = Weights::values(features) * sizeof(float) * (L <= 64 ? 8 : L < 256 ? 2 * norm_teams(L) : 1);    // sums take the weights' place
+                if (!launchable(blocks, norm_grad_threads(L, N))) return PCC_E_ARG;
+                const size_t lds = Weights::values(features) * sizeof(float) * 2 * norm_grad_shares(L, N);     // sums take the weights' place
                 if (!allow_lds(layer_norm_grad_kernel<X, Y, L, N>, lds)) { (void)hipGetLastError(); return PCC_E_HIP; }
                 return launch([&] {
-                    hipLaunchKernelGGL((layer_norm_grad_kernel<X, Y, L, N>), dim3((uint32_t)((blocks + 7) / 8 * 8)), dim3(norm_threads(L)), lds, st, a);
+                    hipLaunchKernelGGL((layer_norm_grad_kernel<X, Y, L, N>), dim3((uint32_t)((blocks + 7) / 8 * 8)), dim3(norm_grad_threads(L, N)), lds, st, a);
                 });
             }
         });
@@ -247,7 +248,7 @@ namespace {
 
 // Segments of the sort: whole rounds of its waves, 256 of them at most, and with many experts fewer, since every workgroup sums all segments' counts.
 uint32_t sort_segment(size_t entries, int experts) {
-    const size_t most = std::min(256, std::max(64, 65536 / experts)), least = (entries + most - 1) / most;
+    const size_t most = std::min(256, std::max(64, 32768 / experts)), least = (entries + most - 1) / most;
     return (uint32_t)std::max<size_t>(4096, (least + 1023) / 1024 * 1024);
 }
 uint32_t sort_segments(size_t entries, int experts) {
@@ -266,27 +267,35 @@ int with_row_types(int type, int y_type, F&& f) {
     if (type == PCC_FP16) return y_type == PCC_FP16 ? f(Fp16{}, Fp16{}) : f(Fp16{}, Fp32{});
     return f(Fp32{}, Fp32{});
 }
-// How many lanes have a token's row, and how many eights of it at a time each.
+// How many lanes have a token's row, and how many eights of it at a time each: where it is copied, as many as it has eights, so that it
+// leaves in one piece.
+template <class F>
+int with_copy_shape(int features, F&& f) {
+    const int eights = features / 8;
+    if (eights <= 8) return f(RowShape<8, 1>{});
+    if (eights <= 16) return f(RowShape<16, 1>{});
+    if (eights <= 32) return f(RowShape<32, 1>{});
+    if (eights <= 64) return f(RowShape<64, 1>{});
+    if (eights <= 128) return f(RowShape<64, 2>{});
+    return f(RowShape<256, 1>{});
+}
 template <class F>
 int with_token_shape(int features, F&& f) {
     const int eights = features / 8;
     if (eights <= 8) return f(RowShape<8, 1>{});
-    if (eights <= 32) return f(RowShape<8, 4>{});
+    if (eights <= 32) return f(RowShape<16, 2>{});
     if (eights <= 64) return f(RowShape<16, 4>{});
     if (eights <= 128) return f(RowShape<32, 4>{});
     if (eights <= 256) return f(RowShape<64, 4>{});
     return f(RowShape<256, 4>{});
 }
-// f(shape, workgroups), with the workgroups of each die in `a`.
+// f(workgroups) for a token's row in LANES lanes, with the workgroups of each die in `a`.
 template <class F>
-int with_tokens(Experts& a, F&& f) {
-    return with_token_shape(a.features, [&](auto shape) {
-        constexpr int kTeams = kExpertThreads / decltype(shape)::kLanes;
-        const uint64_t each = ((a.tokens + kTeams - 1) / kTeams + 7) / 8;
-        if (!launchable(8 * each, kExpertThreads)) return PCC_E_ARG;
-        a.each = (uint32_t)each;
-        return f(shape, dim3((uint32_t)(8 * each)));
-    });
+int with_tokens(Experts& a, int lanes, F&& f) {
+    const uint64_t teams = kExpertThreads / lanes, each = ((a.tokens + teams - 1) / teams + 7) / 8;
+    if (!launchable(8 * each, kExpertThreads)) return PCC_E_ARG;
+    a.each = (uint32_t)each;
+    return f(dim3((uint32_t)(8 * each)));
 }
 uint64_t chunk_blocks(uint64_t rows, uint32_t chunks, int threads) { return (rows * chunks + threads - 1) / threads; }
 
@@ -332,10 +341,16 @@ int pcc_expert_rows(const void* d_x, size_t ldx, const int32_t* d_place, size_t 
     if (overlap(matrix(d_rows, rows, ldr, features, type), {matrix(d_x, tokens, ldx, features, type), piece(d_place, tokens * k * 4)})) return PCC_E_ARG;
     Experts a = {};
     a.x = d_x; a.place = d_place; a.y = d_rows; a.ldx = ldx; a.ldy = ldr; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    return with_tokens(a, [&](auto shape, dim3 grid) {
+    // Rows of whole lines go past the caches.  us, so and not: 500,000 tokens to 2 rows of 128 bytes 41 and 52, 65,536 to 2 of 1,024 40 and 53, but
+    // 393,216 to 2 of 320 (half of a line is another row's) 84 and 82.
+    const bool past = features * size_of(type) % 128 == 0 && ldr * size_of(type) % 128 == 0 && aligned(d_rows, 128);
+    return with_copy_shape(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); }); };
-        return type == PCC_FP32 ? go(expert_rows_kernel<Fp32, L, N>) : go(expert_rows_kernel<Bf16, L, N>);      // bits are copied
+        return with_tokens(a, L, [&](dim3 grid) {
+            auto go = [&](auto kernel) { return launch([&] { hipLaunchKernelGGL(kernel, grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); }); };
+            if (type == PCC_FP32) return past ? go(expert_rows_kernel<Fp32, L, N, true>) : go(expert_rows_kernel<Fp32, L, N, false>);
+            return past ? go(expert_rows_kernel<Bf16, L, N, true>) : go(expert_rows_kernel<Bf16, L, N, false>);     // bits are copied
+        });
     });
 }
 
@@ -347,10 +362,12 @@ int pcc_expert_join(const void* d_z, size_t ldz, const int32_t* d_place, const f
     if (overlap(matrix(d_y, tokens, ldy, features, y_type), {matrix(d_z, rows, ldz, features, type), piece(d_place, tokens * k * 4), piece(d_weight, tokens * k * 4)})) return PCC_E_ARG;
     Experts a = {};
     a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_y; a.ldz = ldz; a.ldy = ldy; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    return with_tokens(a, [&](auto shape, dim3 grid) {
+    return with_token_shape(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        return with_row_types(type, y_type, [&](auto t, auto ty) {
-            return launch([&] { hipLaunchKernelGGL((expert_join_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
+        return with_tokens(a, L, [&](dim3 grid) {
+            return with_row_types(type, y_type, [&](auto t, auto ty) {
+                return launch([&] { hipLaunchKernelGGL((expert_join_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
+            });
         });
     });
 }
@@ -368,10 +385,12 @@ int pcc_expert_join_grad(const void* d_dy, int y_type, size_t lddy, const void* 
     Experts a = {};
     a.x = d_dy; a.z = d_z; a.place = d_place; a.weight = d_weight; a.y = d_dz; a.dweight = d_dweight;
     a.ldx = lddy; a.ldz = ldz; a.ldy = lddz; a.tokens = tokens; a.rows = rows; a.k = k; a.features = features;
-    return with_tokens(a, [&](auto shape, dim3 grid) {
+    return with_token_shape(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        return with_row_types(type, y_type, [&](auto t, auto ty) {
-            return launch([&] { hipLaunchKernelGGL((expert_join_grad_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
+        return with_tokens(a, L, [&](dim3 grid) {
+            return with_row_types(type, y_type, [&](auto t, auto ty) {
+                return launch([&] { hipLaunchKernelGGL((expert_join_grad_kernel<decltype(t), decltype(ty), L, N>), grid, dim3(kExpertThreads), 0, (hipStream_t)hip_stream, a); });
+            });
         });
     });
 }

@@ -152,7 +152,7 @@ __device__ __forceinline__ uint64_t token_of(const Experts& a) {
     return ((uint64_t)(blockIdx.x % 8) * a.each + blockIdx.x / 8) * kTeams + threadIdx.x / LANES;
 }
 
-template <class T, int LANES, int N>
+template <class T, int LANES, int N, bool PAST>
 __global__ __launch_bounds__(kExpertThreads) void expert_rows_kernel(Experts a) {
     const uint64_t token = token_of<LANES>(a);
     if (token >= a.tokens) return;
@@ -164,14 +164,18 @@ __global__ __launch_bounds__(kExpertThreads) void expert_rows_kernel(Experts a) 
         x.load(a.x, token * a.ldx + 8 * c0, lane, w);
         for (int j = 0; j < a.k; ++j) {
             const uint32_t at = (uint32_t)place[j];
-            if (at < a.rows) Row<T, LANES, N>::each(lane, w, [&](auto, auto i) { x.store(i, a.y, at * a.ldy + 8 * c0, lane, w); });
+            if (at < a.rows)
+                Row<T, LANES, N>::each(lane, w, [&](auto, auto i) {
+                    if constexpr (PAST) x.store_past(i, a.y, at * a.ldy + 8 * c0, lane, w);
+                    else x.store(i, a.y, at * a.ldy + 8 * c0, lane, w);
+                });
         }
     }
 }
 
 template <class T, class Y, int LANES, int N>
 __global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) {
-    constexpr int kAtOnce = 2;          // rows on their way
+    constexpr int kAtOnce = N == 1 ? 4 : 2;         // rows on their way
     using Z = Row<T, LANES, N>;
     const uint64_t token = token_of<LANES>(a);
     if (token >= a.tokens) return;
@@ -202,14 +206,16 @@ __global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) 
         Row<Y, LANES, N> y;
         Z::each(lane, w, [&](auto, auto i) {
             y.at(i).set(sum.at(i));
-            y.store(i, a.y, token * a.ldy + 8 * c0, lane, w);
+            // past the caches where neighbouring lanes write neighbouring 16 bytes: 393,216 rows of 160 in bf16 72 us and 76, but 8,192 of 2,048 in fp32 44 and 40
+            if constexpr (!kIs32<Y>) y.store_past(i, a.y, token * a.ldy + 8 * c0, lane, w);
+            else y.store(i, a.y, token * a.ldy + 8 * c0, lane, w);
         });
     }
 }
 
 template <class T, class Y, int LANES, int N>
 __global__ __launch_bounds__(kExpertThreads) void expert_join_grad_kernel(Experts a) {
-    constexpr int kAtOnce = 2, kWaves = LANES <= 64 ? 1 : LANES / 64;
+    constexpr int kAtOnce = N == 1 ? 4 : 2, kWaves = LANES <= 64 ? 1 : LANES / 64;
     using Z = Row<T, LANES, N>;
     __shared__ float meet[2][kAtOnce][kWaves];
     const uint64_t token = token_of<LANES>(a);

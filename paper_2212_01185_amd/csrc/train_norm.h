@@ -5,7 +5,7 @@
 //
 // A row is read once: LANES lanes have it in registers, eight neighbours at a time, so the variance is that of the distances from the
 // mean and not a difference of two large sums.  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
-// forward 62 us, 4.3 TB/s (a large copy has 5.2); backward 393,216 rows of 160 87 us, 4.4 TB/s, of which 5 join the chunks' sums, and the vector ALU
+// forward 62 us, 4.3 TB/s (a large copy has 5.2); backward 393,216 rows of 160 86 us, 4.4 TB/s, of which 5 join the chunks' sums, and the vector ALU
 // is busy for about half of it.
 #pragma once
 
@@ -44,6 +44,12 @@ __device__ __forceinline__ Chunk norm_chunk(const Norm& a, uint32_t b, bool empt
 // Threads of a workgroup, and rows that it has at a time.
 constexpr int norm_threads(int lanes) { return lanes <= 256 ? 256 : lanes; }
 constexpr int norm_teams(int lanes) { return norm_threads(lanes) / lanes; }
+// The same for the backward pass with its sums: the fewer workgroups, the fewer sums to join.  us with 512 threads and 256: 32,768 rows of 1,024 51 and 55,
+// 8,192 of 4,096 56 and 60, 393,216 of 160 86 and 87; but 786,432 of 36 55 and 51.
+constexpr int norm_grad_threads(int lanes, int eights) { return eights == 1 ? 256 : 512; }
+constexpr int norm_grad_teams(int lanes, int eights) { return norm_grad_threads(lanes, eights) / lanes; }
+// Sums of a workgroup's features that meet in LDS: those of each wave, or of each team of several waves.
+constexpr int norm_grad_shares(int lanes, int eights) { return lanes <= 64 ? norm_grad_threads(lanes, eights) / 64 : norm_grad_teams(lanes, eights); }
 
 // Sums over a row's lanes, the same in all of them, of a workgroup with one row.
 template <int LANES>
@@ -186,10 +192,10 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
 
 // The whole backward pass, every row read once: a lane has its features' sums in registers to the end of the chunk.
 template <class X, class Y, int LANES, int N>
-__global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(Norm a) {
-    constexpr int kTeams = norm_teams(LANES), kWaves = LANES <= 64 ? 1 : LANES / 64;
-    // 512 threads have 256 registers each at most: rows of fp32 leave no room for the next row there
-    constexpr bool kAhead = LANES < 512 || !kIs32<Y>;
+__global__ __launch_bounds__(norm_grad_threads(LANES, N)) void layer_norm_grad_kernel(Norm a) {
+    constexpr int kTeams = norm_grad_teams(LANES, N), kWaves = LANES <= 64 ? 1 : LANES / 64;
+    // 512 threads have 256 registers each at most: where more than one wave's sums are kept as well, rows of fp32 leave no room for the next row
+    constexpr bool kAhead = LANES < 256 || !kIs32<Y>;
     using R = Row<X, LANES, N>;
     __shared__ float meet[2][kTeams][2][kWaves];
     extern __shared__ __align__(16) float norm_weights[];
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(No
     float* to = ch.count == 1 ? a.dgamma + (size_t)ch.group * features : a.partial + (size_t)ch.shared * 2 * features;
     float* to_beta = ch.count == 1 ? a.dbeta + (size_t)ch.group * features : to + features;
     const Extent all(features, true);
-    if constexpr (LANES >= 256) {
+    if constexpr (LANES > 64 && kTeams == 1) {
         R::each(lane, all, [&](auto, auto i) {
             Row<Fp32, LANES, N> out;
             out.at(i).set(dg.at(i));
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(No
         });
     } else {
         // the rows of a wave by exchanges, then those of the waves or teams, kShares of them, through LDS (where the weights were)
-        constexpr int kShares = LANES <= 64 ? 4 : kTeams;
+        constexpr int kShares = norm_grad_shares(LANES, N);
         const int share = LANES <= 64 ? threadIdx.x >> 6 : team;
         if constexpr (LANES < 64) {
             dg.sum_groups();
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_grad_kernel(No
                 }
             });
         __syncthreads();
-        for (int f = threadIdx.x; f < features; f += norm_threads(LANES)) {
+        for (int f = threadIdx.x; f < features; f += norm_grad_threads(LANES, N)) {
             float g = 0.0f, b = 0.0f;
 #pragma unroll
             for (int k = 0; k < kShares; ++k) {

@@ -22,26 +22,29 @@ struct Route {
 };
 constexpr int kRouteThreads = 256;
 
-// A logit and its expert as one whole number: larger for larger logits, and for lower experts where they are equal.  0: never to be chosen.
+// A logit and its expert as one whole number: larger for larger logits, and for lower experts where they are equal.  A logit of 16 bits leaves the
+// last ten bits of its fp32 form free, which take the expert; one of fp32 takes 32 more.  0 is less than any.
 template <class T>
 struct RouteKey {
-    static constexpr int kBits = kIs32<T> ? 32 : 16;
     using type = std::conditional_t<kIs32<T>, uint64_t, uint32_t>;
-    static constexpr uint32_t kSign = 1u << (kBits - 1), kAll = kSign | (kSign - 1);
+    static constexpr uint32_t kLow = 0x3FF;
+    static_assert(PCC_MAX_EXPERTS <= kLow + 1, "an expert's number has ten bits");
+    // What is not above is -inf.
+    static constexpr type kNever = kIs32<T> ? 0x007FFFFFFFFFFFFFull : 0x007FFFFFu;
 
-    static __device__ __forceinline__ type of(element_of<T> element, float v, uint32_t expert) {
-        uint32_t b;
-        if constexpr (kIs32<T>) b = as_bits(v);
-        else b = element;
-        b = v != v ? kAll : b & kSign ? (0 - b) & kAll : b | kSign;      // both zeros are one
-        return v == -__builtin_inff() ? 0 : (type)b << kBits | (kAll ^ expert);
+    // Bits that are ordered as the numbers are: both zeros are one, a NaN is the last.
+    static __device__ __forceinline__ type of(float v, uint32_t expert) {
+        const uint32_t b = as_bits(v != v ? __builtin_nanf("") : v + 0.0f), o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+        if constexpr (kIs32<T>) return (type)o << 32 | ~expert;
+        else return (o & ~kLow) | (kLow ^ expert);
     }
     static __device__ __forceinline__ float logit(type key) {
-        const uint32_t b = (uint32_t)(key >> kBits), e = b & kSign ? b ^ kSign : (0 - b) & kAll;
-        if constexpr (kIs32<T>) return as_float(e);
-        else return from16<T>((u16)e);
+        uint32_t o;
+        if constexpr (kIs32<T>) o = (uint32_t)(key >> 32);
+        else o = key >> 31 ? key & ~kLow : key | kLow;
+        return as_float(o >> 31 ? o ^ 0x80000000u : ~o);
     }
-    static __device__ __forceinline__ int expert(type key) { return (int)((uint32_t)key & kAll ^ kAll); }
+    static __device__ __forceinline__ int expert(type key) { return (int)(kIs32<T> ? ~(uint32_t)key : kLow ^ ((uint32_t)key & kLow)); }
 };
 
 template <int G>
@@ -86,56 +89,78 @@ __device__ __forceinline__ void sort_eight(K (&k)[8]) {
     }
 }
 
-// e^v for v <= 0 (and NaN), with what the rounding of v log2(e) left out.
-__device__ __forceinline__ float exp_below(float v) {
-    constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-    const float b = v < -120.0f ? -120.0f : v, t = b * kLog2e, e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, __builtin_fmaf(b, 1.925962989e-8f, __builtin_fmaf(b, kLog2e, -t)) * kLn2, e);
+// e^v for v <= 0, rounded as v log2(e) is.  A NaN stays one.
+__device__ __forceinline__ float exp_below(float v) { return __builtin_amdgcn_exp2f((v < -120.0f ? -120.0f : v) * 1.44269504088896341f); }
+
+// Takes `best` off the lists that it is the first of; NEEDED entries of a list behind it are.
+template <int NEEDED, class K, int N>
+__device__ __forceinline__ void take_off(K (&key)[N][8], K best) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bool taken = key[i][0] == best;
+#pragma unroll
+        for (int e = 0; e < (NEEDED < 8 ? NEEDED : 8); ++e) key[i][e] = taken ? (e < 7 ? key[i][e < 7 ? e + 1 : 7] : K{0}) : key[i][e];
+    }
+}
+template <int LANES, class K, int N>
+__device__ __forceinline__ K first_of(const K (&key)[N][8]) {
+    K best = key[0][0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) best = key[i][0] > best ? key[i][0] : best;
+    return lanes_max<LANES>(best);
+}
+// Choices J, J + 1, ... of eight at most.
+template <int LANES, int SLOTS, int J = 0, class K, int N>
+__device__ __forceinline__ void choose_eight(K (&key)[N][8], K (&held)[SLOTS], K& top, int k, int lane) {
+    if constexpr (J < 8) {
+        if (J >= k) return;
+        const K best = first_of<LANES>(key);
+        if (J == 0) top = best;
+        if (lane == J % LANES) held[J / LANES] = best;
+        take_off<7 - J>(key, best);
+        choose_eight<LANES, SLOTS, J + 1>(key, held, top, k, lane);
+    }
 }
 
 // LANES lanes have a token, eight neighbouring logits each, N times.  Each lane sorts its own; then the largest of all lanes' first ones is taken off
-// its list, k times, and choice j is kept by lane j % LANES.
+// its list, k times, and choice j is kept by lane j % LANES.  393,216 tokens, 8 of 64: bound by the vector ALU, not by the bytes.
 template <class T, int LANES, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
     using Key = RouteKey<T>;
+    using K = typename Key::type;
     constexpr int kSlots = LANES >= PCC_MAX_CHOICES ? 1 : LANES == 1 ? 8 : PCC_MAX_CHOICES / LANES;    // (k is at most the number of experts)
     const uint64_t t0 = (uint64_t)blockIdx.x * (kRouteThreads / LANES) + threadIdx.x / LANES;
     const bool mine = t0 < a.tokens;
     const uint64_t t = mine ? t0 : a.tokens - 1;
     const int lane = threadIdx.x % LANES;
     Eight<T> l[N];
-    typename Key::type key[N][8], held[kSlots] = {}, top = 0;
+    K key[N][8], held[kSlots] = {}, top = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int f = 8 * (lane + LANES * i);
         l[i].load(a.logits, t * a.ldl + f, a.experts - f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) key[i][e] = f + e < a.experts ? Key::of(l[i].element(e), l[i].get(e), (uint32_t)(f + e)) : 0;
+        for (int e = 0; e < 8; ++e) key[i][e] = f + e < a.experts ? Key::of(l[i].get(e), (uint32_t)(f + e)) : 0;
         sort_eight(key[i]);
     }
+    if (LANES == 1 || a.k <= 8) {
+        choose_eight<LANES, kSlots>(key, held, top, a.k, lane);
+    } else {
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-        for (int u = 0; u < LANES && s * LANES + u < a.k; ++u) {
-            typename Key::type best = key[0][0];
-#pragma unroll
-            for (int i = 1; i < N; ++i) best = key[i][0] > best ? key[i][0] : best;
-            best = lanes_max<LANES>(best);
-            if (s == 0 && u == 0) top = best;
-            if (lane == u) held[s] = best;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const bool taken = key[i][0] == best;
-#pragma unroll
-                for (int e = 0; e < 7; ++e) key[i][e] = taken ? key[i][e + 1] : key[i][e];
-                key[i][7] = taken ? 0 : key[i][7];
+        for (int s = 0; s < kSlots; ++s)
+            for (int u = 0; u < LANES && s * LANES + u < a.k; ++u) {
+                const K best = first_of<LANES>(key);
+                if (s == 0 && u == 0) top = best;
+                if (lane == u) held[s] = best;
+                take_off<8>(key, best);
             }
-        }
     }
-    const float highest = top ? Key::logit(top) : 0.0f;
+    const bool some = top > Key::kNever;
+    const float highest = some ? Key::logit(top) : 0.0f;
     float total = 0.0f, size[kSlots];
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
-        size[s] = held[s] ? exp_below(Key::logit(held[s]) - highest) : 0.0f;
+        size[s] = held[s] > Key::kNever ? exp_below(Key::logit(held[s]) - highest) : 0.0f;
         total += size[s];
     }
     if (a.over_all) {
@@ -151,8 +176,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
     for (int s = 0; s < kSlots; ++s) {
         const int j = s * LANES + lane;
         if (j >= a.k) continue;
-        a.expert[t * a.k + j] = held[s] ? Key::expert(held[s]) : -1;
-        a.weight[t * a.k + j] = held[s] ? size[s] / total : 0.0f;
+        a.expert[t * a.k + j] = held[s] > Key::kNever ? Key::expert(held[s]) : -1;
+        a.weight[t * a.k + j] = held[s] > Key::kNever ? size[s] / total : 0.0f;
     }
 }
 
@@ -196,13 +221,12 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
         if (expert[s] >= 0) own[expert[s]] = a.over_all ? dw[s] : w[s] * (dw[s] - along);
     float top = -__builtin_inff(), all = 0.0f;
     if (a.over_all) {
-        // (a NaN does not become the largest: it shows in the sum)
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = 8 * (lane + LANES * i) + e < a.experts ? l[i].get(e) : -__builtin_inff();
-                top = v > top ? v : top;
+                top = v > top ? v : top;        // (a NaN does not become the largest: it shows in the sum)
             }
         top = over_lanes<LANES>(top, [](float x, float y) { return x > y ? x : y; });
         top = top == -__builtin_inff() ? 0.0f : top;

@@ -48,6 +48,11 @@ struct Eight {
 #pragma unroll
         for (int k = 0; k < kWords; ++k) reinterpret_cast<typename Place::type*>(to)[k] = words[k];
     }
+    // Past the caches.
+    __device__ __forceinline__ void store8_past(element_of<T>* to) const {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) __builtin_nontemporal_store(words[k], reinterpret_cast<typename Place::type*>(to) + k);
+    }
     __device__ __forceinline__ element_of<T> element(int e) const {
         if constexpr (kIs32<T>) return as_float(words[e / 4][e % 4]);
         else return (u16)(words[0][e / 2] >> (16 * (e % 2)));
@@ -199,6 +204,11 @@ struct Row {
         element_of<T>* to = static_cast<element_of<T>*>(base) + at0;
         if constexpr (I < N) v[I].store8(to + 8 * (lane + LANES * I));
         else to[8 * w.eights + lane] = tail.element(0);
+    }
+    template <int I>
+    __device__ __forceinline__ void store_past(std::integral_constant<int, I> i, void* base, size_t at0, int lane, Extent w) const {
+        if constexpr (I < N) v[I].store8_past(static_cast<element_of<T>*>(base) + at0 + 8 * (lane + LANES * I));
+        else store(i, base, at0, lane, w);
     }
     // What was made of the values is made anew behind this, not kept: a value takes half a register as it came.
     __device__ __forceinline__ void forget() {
