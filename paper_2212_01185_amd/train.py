@@ -41,16 +41,21 @@ def parse_blob(blob: bytes):
 
 
 class Trainer:
-    """Networks of one shape under training.  ``blobs``: the weight blobs they start from, one a network."""
+    """Networks of one shape under training.  ``blobs``: the weight blobs they start from, one a network.  ``dropout``: the share of each hidden layer's
+    results that a step leaves out (the others are scaled up; a blob is the whole network), with masks fixed by ``seed``, the step's number
+    and a pixel's place among all of the step's."""
 
     def __init__(self, blobs, device: int = 0, lr: float = 1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
-                 state_bits: int = 32, lr_tensor=None):
+                 state_bits: int = 32, lr_tensor=None, dropout: float = 0.0, seed: int = 0):
         blobs = [blobs] if isinstance(blobs, (bytes, bytearray)) else list(blobs)
         parsed = [parse_blob(bytes(b)) for b in blobs]
         if not parsed or any(p[1:] != parsed[0][1:] or [w.shape for w, _ in p[0]] != [w.shape for w, _ in parsed[0][0]] for p in parsed):
             raise ValueError("blobs must be one or more networks of one shape")
         if not eps > 0:
             raise ValueError("eps must be above 0: padded inputs and networks without pictures have moments of 0")
+        if not 0 <= dropout < 1:
+            raise ValueError("dropout must be in [0, 1)")
+        self.dropout, self.seed = float(dropout), int(seed)
         self.k, self.nbhd, self.delay, self.act, self.dist = parsed[0][1:]
         self.groups, self.device = len(parsed), torch.device("cuda", device)
         self.dims = [parsed[0][0][0][0].shape[1]] + [w.shape[0] for w, _ in parsed[0][0]]
@@ -81,6 +86,12 @@ class Trainer:
         self.optimizer = binding.AdamW(lists[0], lists[1], copies=lists[2], state_bits=state_bits, lr=lr, betas=betas, eps=eps,
                                        weight_decay=weight_decay, lr_tensor=lr_tensor)
 
+    def _drop(self, layer: int, t: torch.Tensor) -> torch.Tensor:
+        """A hidden layer's results, or the gradients of its sums, with this step's mask, in place."""
+        if self.dropout:
+            binding.pcc_dropout(t, self.dropout, (self.seed + layer) % (1 << 64), step=self.optimizer.step, out=t)
+        return t
+
     def gradients(self, pictures) -> torch.Tensor:
         """Forward and backward pass; the gradients of each network's mean code length are left in ``dw`` and ``db``.
 
@@ -109,11 +120,16 @@ class Trainer:
             last = layer + 1 == layers
             h.append(binding.pcc_grouped_linear(h[-1], self.w16[layer], self.b[layer], offsets, binding.PCC_ACT_NONE if last else self.act,
                                                 out_dtype=torch.float32 if last else torch.bfloat16))
+            if not last:
+                self._drop(layer, h[-1])
         weight = torch.repeat_interleave(1.0 / counts.clamp_min(1).to(torch.float32), counts, output_size=rows) if self.groups > 1 else None
         bits, dz = binding.pcc_mixture_loss(h.pop(), rgb, self.dist, 1.0 if self.groups > 1 else 1.0 / rows, weight=weight, grad_dtype=torch.bfloat16)
         for layer in reversed(range(layers)):
             dz, _, _ = binding.pcc_grouped_linear_grad(dz, h.pop(), self.w16[layer], offsets, self.act if layer else binding.PCC_ACT_NONE,
                                                        want_dx=layer > 0, dw=self.dw[layer], db=self.db[layer])
+            # the activation's derivative was told by the sign of what the mask had left, and is dropped where that is 0
+            if layer:
+                self._drop(layer - 1, dz)
         total = torch.segment_reduce(bits.double(), "sum", lengths=counts)
         return total / (3 * counts.clamp_min(1))
 
@@ -143,6 +159,7 @@ def main(argv=None) -> None:
     p.add_argument("--crop", type=int, default=64, help="their height and width at most")
     p.add_argument("--lr", type=float, default=1e-3)
     p.add_argument("--state-bits", type=int, choices=[8, 32], default=32)
+    p.add_argument("--dropout", type=float, default=0.0, help="share of each hidden layer's results that a step leaves out")
     p.add_argument("--seed", type=int, default=0)
     a = p.parse_args(argv)
     pictures = np.load(a.pictures, allow_pickle=False)
@@ -153,7 +170,7 @@ def main(argv=None) -> None:
             start = f.read()
     else:
         start = {"workload": synth.make_blob, "paper": synth.make_paper_blob, "diagonal": synth.make_diagonal_blob}[a.network](a.seed)
-    trainer = Trainer(start, lr=a.lr, state_bits=a.state_bits)
+    trainer = Trainer(start, lr=a.lr, state_bits=a.state_bits, dropout=a.dropout, seed=a.seed % (1 << 64))
     rng = np.random.default_rng(a.seed)
     n, h, w, _ = pictures.shape
     ch, cw = min(a.crop, h), min(a.crop, w)
