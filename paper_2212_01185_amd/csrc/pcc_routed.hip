@@ -24,8 +24,9 @@ template <int LANES, int N>
 struct RowShape {
     static constexpr int kLanes = LANES, kChunks = N;
 };
-// How many lanes have a row, and how many eights of it each.
-template <class F>
+// How many lanes have a row, and how many eights of it each.  us, four and two eights a lane: rows of several waves, 16,384 of 4,096 forward 62 and 58,
+// 8,192 of 4,096 backward 83 and 80, 8,192 of 8,192 forward 60 and 57; of one wave 65,536 of 1,024 forward 58 and 60.
+template <bool FORWARD, class F>
 int with_row_shape(int features, F&& f) {
     const int eights = features / 8;
     if (eights <= 8) return f(RowShape<8, 1>{});
@@ -34,9 +35,12 @@ int with_row_shape(int features, F&& f) {
     if (eights <= 64) return f(RowShape<16, 4>{});
     if (eights <= 128) return f(RowShape<32, 4>{});
     if (eights <= 256) return f(RowShape<64, 4>{});
-    if (eights <= 512) return f(RowShape<128, 4>{});
-    if (eights <= 1024) return f(RowShape<256, 4>{});
-    if (eights <= 2048) return f(RowShape<512, 4>{});
+    if (eights <= 512) return f(RowShape<256, 2>{});
+    if (eights <= 1024) return f(RowShape<512, 2>{});
+    if (eights <= 2048) {       // (without sums to keep, a thread needs few enough registers for 1024 of them: 4,096 rows of 16,384 62 us, else 64)
+        if constexpr (FORWARD) return f(RowShape<1024, 2>{});
+        else return f(RowShape<512, 4>{});
+    }
     return f(RowShape<kLongThreads, 0>{});      // read again for each sum
 }
 // x and y have one type, or x is fp32 and y a 16-bit one.
@@ -62,8 +66,8 @@ void norm_chunks(size_t rows, int groups, int want, int teams, int& log2, uint32
 }
 // Chunks whose sums are joined: as many workgroups as run at once by their registers.
 void sums_chunks(size_t rows, int groups, int features, int& log2, uint32_t& mult) {
-    const int threads = with_row_shape(features, [](auto shape) { return norm_grad_threads(decltype(shape)::kLanes, decltype(shape)::kChunks); });
-    const int teams = with_row_shape(features, [](auto shape) { return std::max(1, norm_grad_teams(decltype(shape)::kLanes, decltype(shape)::kChunks)); });
+    const int threads = with_row_shape<false>(features, [](auto shape) { return norm_grad_threads(decltype(shape)::kLanes, decltype(shape)::kChunks); });
+    const int teams = with_row_shape<false>(features, [](auto shape) { return std::max(1, norm_grad_teams(decltype(shape)::kLanes, decltype(shape)::kChunks)); });
     norm_chunks(rows, groups, threads == 256 ? 1280 : 256, teams, log2, mult);
 }
 
@@ -84,9 +88,9 @@ int pcc_layer_norm(const void* d_x, size_t ldx, const float* d_gamma, const floa
     Norm a = {};
     a.x = d_x; a.gamma = d_gamma; a.beta = d_beta; a.off = d_offsets; a.y = d_y; a.stats = d_stats;
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.eps = eps; a.inverse = 1.0f / (float)features;
-    return with_row_shape(features, [&](auto shape) {
+    return with_row_shape<true>(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-        norm_chunks(rows, groups, L <= 64 ? 2048 : L == 128 ? 1024 : L == 256 ? 512 : 256, norm_teams(L), a.log2, a.mult);
+                norm_chunks(rows, groups, L <= 64 ? 2048 : L <= 512 ? 512 : 256, norm_teams(L), a.log2, a.mult);
         const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
         if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
         return with_norm_types(type, y_type, [&](auto tx, auto ty) {
@@ -131,7 +135,7 @@ int pcc_layer_norm_grad(const void* d_dy, int y_type, size_t lddy, const void* d
     a.ldx = ldx; a.lddy = lddy; a.ldy = lddx; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.inverse = 1.0f / (float)features;
     a.shared_max = (uint32_t)std::min<size_t>(need / (2 * features * sizeof(float)), 0xFFFFFFFFu);
     hipStream_t st = (hipStream_t)hip_stream;
-    const int rc = with_row_shape(features, [&](auto shape) {
+    const int rc = with_row_shape<false>(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
         return with_norm_types(type, y_type, [&](auto tx, auto ty) {
             using X = decltype(tx);

@@ -5,7 +5,7 @@
 //
 // A row is read once: LANES lanes have it in registers, eight neighbours at a time, so the variance is that of the distances from the
 // mean and not a difference of two large sums.  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
-// forward 62 us, 4.3 TB/s (a large copy has 5.2); backward 393,216 rows of 160 86 us, 4.4 TB/s, of which 5 join the chunks' sums, and the vector ALU
+// forward 57 us, 4.7 TB/s (a large copy has 5.2); backward 393,216 rows of 160 85 us, 4.5 TB/s, of which 5 join the chunks' sums, and the vector ALU
 // is busy for about half of it.
 #pragma once
 
@@ -70,6 +70,11 @@ struct Weights {
     int eights;
 
     static __host__ __device__ constexpr size_t values(int features) { return (size_t)features / 8 * 8 + 8; }
+    // Where feature f stands.
+    static __device__ __forceinline__ int place(int f, int eights) {
+        const int c = f >> 3;
+        return c == eights ? f : 4 * (f & 4 ? eights + c : c) + (f & 3);
+    }
     __device__ __forceinline__ void fill(float* lds, const float* from, int features, float none) {
         at = lds;
         eights = features >> 3;
@@ -194,8 +199,8 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
 template <class X, class Y, int LANES, int N>
 __global__ __launch_bounds__(norm_grad_threads(LANES, N)) void layer_norm_grad_kernel(Norm a) {
     constexpr int kTeams = norm_grad_teams(LANES, N), kWaves = LANES <= 64 ? 1 : LANES / 64;
-    // 512 threads have 256 registers each at most: where more than one wave's sums are kept as well, rows of fp32 leave no room for the next row
-    constexpr bool kAhead = LANES < 256 || !kIs32<Y>;
+    // 512 threads have 256 registers each at most: four eights a lane of fp32, with the sums, leave no room for the next row
+    constexpr bool kAhead = LANES < 512 || N < 4 || !kIs32<Y>;
     using R = Row<X, LANES, N>;
     __shared__ float meet[2][kTeams][2][kWaves];
     extern __shared__ __align__(16) float norm_weights[];
@@ -302,20 +307,27 @@ __global__ __launch_bounds__(norm_grad_threads(LANES, N)) void layer_norm_grad_k
         const int pitch = (int)Weights::values(features);
         if (LANES >= 64 || (int)(threadIdx.x & 63) < LANES)
             R::each(lane, all, [&](auto wide, auto i) {
-                float* at = norm_weights + 2 * share * pitch + (i < N ? 8 * (lane + LANES * i) : 8 * all.eights + lane);
-#pragma unroll
-                for (int e = 0; e < wide; ++e) {
-                    at[e] = dg.at(i)[e];
-                    at[pitch + e] = db.at(i)[e];
+                float* at = norm_weights + 2 * share * pitch;
+                const float (&g)[8] = dg.at(i), (&b)[8] = db.at(i);
+                if constexpr (wide == 8) {
+                    const int c = lane + LANES * i;
+                    *reinterpret_cast<f32x4*>(at + 4 * c) = f32x4{g[0], g[1], g[2], g[3]};
+                    *reinterpret_cast<f32x4*>(at + 4 * (all.eights + c)) = f32x4{g[4], g[5], g[6], g[7]};
+                    *reinterpret_cast<f32x4*>(at + pitch + 4 * c) = f32x4{b[0], b[1], b[2], b[3]};
+                    *reinterpret_cast<f32x4*>(at + pitch + 4 * (all.eights + c)) = f32x4{b[4], b[5], b[6], b[7]};
+                } else {
+                    at[8 * all.eights + lane] = g[0];
+                    at[pitch + 8 * all.eights + lane] = b[0];
                 }
             });
         __syncthreads();
         for (int f = threadIdx.x; f < features; f += norm_grad_threads(LANES, N)) {
+            const int at = Weights::place(f, all.eights);
             float g = 0.0f, b = 0.0f;
 #pragma unroll
             for (int k = 0; k < kShares; ++k) {
-                g += norm_weights[2 * k * pitch + f];
-                b += norm_weights[2 * k * pitch + pitch + f];
+                g += norm_weights[2 * k * pitch + at];
+                b += norm_weights[2 * k * pitch + pitch + at];
             }
             to[f] = g;
             to_beta[f] = b;

@@ -89,8 +89,21 @@ __device__ __forceinline__ void sort_eight(K (&k)[8]) {
     }
 }
 
-// e^v for v <= 0, rounded as v log2(e) is.  A NaN stays one.
-__device__ __forceinline__ float exp_below(float v) { return __builtin_amdgcn_exp2f((v < -120.0f ? -120.0f : v) * 1.44269504088896341f); }
+// e^v for v <= 0 (-inf gives 0), rounded as v log2(e) is.  A NaN stays one.
+__device__ __forceinline__ float exp_below(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896341f); }
+
+// Eight logits of a token from expert f on; what lies behind the last expert is -inf.
+template <class T>
+__device__ __forceinline__ void load_logits(Eight<T>& l, const Route& a, uint64_t t, int f, bool whole) {
+    l.load(a.logits, t * a.ldl + f, a.experts - f);
+    if (whole) return;
+    constexpr uint32_t kBelow = kIs32<T> ? 0xFF800000u : std::is_same_v<T, Bf16> ? 0xFF80u : 0xFC00u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (kIs32<T>) l.words[e / 4][e % 4] = f + e < a.experts ? l.words[e / 4][e % 4] : kBelow;
+        else l.words[0][e / 2] |= f + e < a.experts ? 0u : kBelow << (16 * (e % 2));     // (zeros until then)
+    }
+}
 
 // Takes `best` off the lists that it is the first of; NEEDED entries of a list behind it are.
 template <int NEEDED, class K, int N>
@@ -133,14 +146,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
     const bool mine = t0 < a.tokens;
     const uint64_t t = mine ? t0 : a.tokens - 1;
     const int lane = threadIdx.x % LANES;
+    const bool whole = a.experts == 8 * LANES * N;
     Eight<T> l[N];
     K key[N][8], held[kSlots] = {}, top = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int f = 8 * (lane + LANES * i);
-        l[i].load(a.logits, t * a.ldl + f, a.experts - f);
+        load_logits(l[i], a, t, f, whole);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) key[i][e] = f + e < a.experts ? Key::of(l[i].get(e), (uint32_t)(f + e)) : 0;
+        for (int e = 0; e < 8; ++e) key[i][e] = Key::of(l[i].get(e), (uint32_t)(f + e));
         sort_eight(key[i]);
     }
     if (LANES == 1 || a.k <= 8) {
@@ -168,7 +182,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) total += 8 * (lane + LANES * i) + e < a.experts ? exp_below(l[i].get(e) - highest) : 0.0f;
+            for (int e = 0; e < 8; ++e) total += exp_below(l[i].get(e) - highest);
     }
     total = lanes_sum<LANES>(total);
     if (!mine) return;
@@ -190,6 +204,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
     const bool mine = t0 < a.tokens;
     const uint64_t t = mine ? t0 : a.tokens - 1;
     const int lane = threadIdx.x % LANES;
+    const bool whole = a.experts == 8 * LANES * N;
     float* own = brought + threadIdx.x / LANES * (LANES * 8 * N);
     Eight<T> l[N];
     int expert[kSlots];
@@ -205,7 +220,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int f = 8 * (lane + LANES * i);
-        if (a.over_all) l[i].load(a.logits, t * a.ldl + f, a.experts - f);
+        if (a.over_all) load_logits(l[i], a, t, f, whole);
         f32x4* zeros = reinterpret_cast<f32x4*>(own + f);
         zeros[0] = zeros[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -225,7 +240,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float v = 8 * (lane + LANES * i) + e < a.experts ? l[i].get(e) : -__builtin_inff();
+                const float v = l[i].get(e);
                 top = v > top ? v : top;        // (a NaN does not become the largest: it shows in the sum)
             }
         top = over_lanes<LANES>(top, [](float x, float y) { return x > y ? x : y; });
@@ -236,7 +251,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            p[i][e] = a.over_all && 8 * (lane + LANES * i) + e < a.experts ? exp_below(l[i].get(e) - top) : 0.0f;
+            p[i][e] = a.over_all ? exp_below(l[i].get(e) - top) : 0.0f;
             all += p[i][e];
         }
     all = lanes_sum<LANES>(all);
