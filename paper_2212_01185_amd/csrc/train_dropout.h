@@ -39,7 +39,8 @@ __device__ __forceinline__ Philox philox(Philox s, uint32_t k0, uint32_t k1) {
 
 constexpr int kDropoutThreads = 256;
 
-// A thread has eight neighbours of a row.
+// A thread has eight neighbours of a row: their bits are one turn of the generator.  With 16 bits an element its multiplications fit beside the loads:
+// 16,384 rows of 4,096 in bf16 with a residual 70 us, 5.7 TB/s, the vector ALU busy for 58 % of it (bits of 32 would take twice as many turns).
 template <class X, class Y>
 __global__ __launch_bounds__(kDropoutThreads) void dropout_kernel(Dropout a) {
     const uint64_t id = (uint64_t)blockIdx.x * kDropoutThreads + threadIdx.x, row = id / a.chunks;

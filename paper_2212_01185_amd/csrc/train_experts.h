@@ -13,7 +13,8 @@ namespace pcc_train {
 // ---------------------------------------------------------------------------
 // Sort by counting.  A workgroup of 16 waves has a segment of the entries, a wave a sixteenth of it.  The first kernel counts each segment's
 // experts; in the second a workgroup finds by those counts where its entries of each expert go, then its waves deal the places out
-// 64 entries at a time: equal experts of a wave are found by ballots over the bits of their numbers.
+// 64 entries at a time: equal experts of a wave are found by ballots over the bits of their numbers.  One segment (4,096 entries) takes the second kernel alone.
+// 786,432 entries of 16 experts: 5 and 7 us, of which the entries' bytes are one (a thread an expert for the sum over segments: 36 instead of 7).
 // ---------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 
@@ -144,6 +145,8 @@ struct Experts {
 };
 constexpr int kExpertThreads = 256;
 
+// Memory bounds all of these.  us, 393,216 tokens with 2 rows of 160 in bf16 each: rows 69 (5.4 TB/s), join 72 (5.3), its gradient 124 (5.1); 8,192 tokens with
+// four of 2,048, join to fp32, 40 (5.0).
 // A token's row has LANES lanes, parts of LANES * N eights one after the other.  A die has neighbouring tokens, whose rows of one expert are neighbours
 // as well and share lines of its L2.
 template <int LANES>
