@@ -602,7 +602,7 @@ def pcc_dropout(x: torch.Tensor, p: float, seed: int, step: torch.Tensor | None 
     nearest 1/65536.  The result has x's type, or one of the two is fp32; residual has the result's.  `out` may be x or residual."""
     _unrecorded(x, residual, out)
     ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
-    shape = (int(x.shape[0]), int(x.shape[1]))
+    shape, seed = (int(x.shape[0]), int(x.shape[1])), int(seed)
     if not 0 <= seed < 1 << 64:
         raise ValueError("seed must be a whole number of 64 bits")
     if step is not None:

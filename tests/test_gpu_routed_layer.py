@@ -214,6 +214,72 @@ def test_more_than_2_to_the_32_elements():
     assert_near(out[-2:], wanted, limit, "dropout")
 
 
+# ---------------------------------------------------------------------------------------------------- as many groups as there may be, any address
+
+@pytest.mark.parametrize("groups,features", [(65535, 24), (65535, 9), (3000, 200)])
+def test_layer_norm_of_as_many_groups_as_there_may_be(groups, features):
+    gen = torch.Generator().manual_seed(groups)
+    lengths = torch.randint(0, 3, (groups,), generator=gen)
+    lengths[[0, 64, 65, groups - 2]] = torch.tensor([900, 0, 1500, 700])
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), lengths.cumsum(0)])
+    rows = int(off[-1])
+    x, dy = torch.randn(rows, features, generator=gen), torch.randn(rows, features, generator=gen)
+    gamma, beta = torch.randn(groups, features, generator=gen), torch.randn(groups, features, generator=gen)
+    g = torch.repeat_interleave(torch.arange(groups), lengths)
+    y, stats = binding.pcc_layer_norm(x.cuda(), gamma.cuda(), beta.cuda(), off.cuda())
+    dx, dgamma, dbeta = binding.pcc_layer_norm_grad(dy.cuda(), x.cuda(), stats, gamma.cuda(), off.cuda())
+    # one group of all rows with each row's own weights: h and the sums of a row do not hang on the group
+    (h, e_h), _ = ref.layer_norm(x, None, None, [0, rows], 1e-5)
+    want = gamma.double()[g] * h + beta.double()[g]
+    assert_near(y, want, gamma.double()[g].abs() * e_h + 2 * ref.U * (want.abs() + (gamma.double()[g] * h).abs()), "y")
+    (value, limit), _, _ = ref.layer_norm_grad(dy.double() * gamma.double()[g], x, stats, None, [0, rows])
+    assert_near(dx, value, limit * (1 + 2 * ref.U), "dx")       # (the product with gamma is rounded in the kernel: in the reference's bound of u)
+    s = stats.double().cpu()
+    part = dy.double() * ((x.double() - s[:, :1]) * s[:, 1:])
+    for name, got, p in (("dgamma", dgamma, part), ("dbeta", dbeta, dy.double())):
+        sums, sizes = (torch.zeros(groups, features, dtype=torch.float64).index_add_(0, g, t) for t in (p, p.abs()))
+        assert_near(got, sums, (lengths[:, None].double() + 8) * ref.U * sizes, name)
+        assert (got.cpu()[lengths == 0] == 0).all()
+
+
+def _shifted(t):
+    """The same values one element behind the start of an allocation."""
+    full = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+    full[1:] = t.reshape(-1)
+    return full[1:].view(t.shape)
+
+
+@pytest.mark.parametrize("features", [40, 37, 4100])
+def test_weights_statistics_and_places_at_any_address(features):
+    gen = torch.Generator().manual_seed(features)
+    x, dy = torch.randn(2100, features, generator=gen).to(BF16).cuda(), torch.randn(2100, features, generator=gen).to(BF16).cuda()
+    gamma, beta, off = torch.randn(2, features, generator=gen).cuda(), torch.randn(2, features, generator=gen).cuda(), torch.tensor([0, 1999, 2100]).cuda()
+    y, stats = binding.pcc_layer_norm(x, gamma, beta, off)
+    y2, stats2 = binding.pcc_layer_norm(_shifted(x), _shifted(gamma), _shifted(beta), off, out=_shifted(torch.zeros_like(x)), stats=_shifted(torch.zeros_like(stats)))
+    assert torch.equal(y, y2) and torch.equal(stats, stats2)
+    want = binding.pcc_layer_norm_grad(dy, x, stats, gamma, off)
+    got = binding.pcc_layer_norm_grad(_shifted(dy), _shifted(x), _shifted(stats), _shifted(gamma), off, dx=_shifted(torch.zeros_like(x)),
+                                      dgamma=_shifted(torch.zeros_like(gamma)), dbeta=_shifted(torch.zeros_like(gamma)))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    logits, dweight = torch.randn(300, 21, generator=gen).cuda(), torch.randn(300, 3, generator=gen).cuda()
+    expert, weight = binding.pcc_route(logits, 3)
+    again = binding.pcc_route(_shifted(logits), 3, expert=_shifted(torch.zeros_like(expert)), weight=_shifted(torch.zeros_like(weight)))
+    assert torch.equal(expert, again[0]) and torch.equal(weight, again[1])
+    assert torch.equal(binding.pcc_route_grad(dweight, logits, expert, weight),
+                       binding.pcc_route_grad(_shifted(dweight), _shifted(logits), _shifted(expert), _shifted(weight), dlogits=_shifted(torch.zeros_like(logits))))
+    offsets, place = binding.pcc_expert_sort(expert, 21)
+    again = binding.pcc_expert_sort(_shifted(expert), 21, offsets=_shifted(torch.zeros_like(offsets)), place=_shifted(torch.zeros_like(place)))
+    assert torch.equal(offsets, again[0]) and torch.equal(place, again[1])
+    rows = binding.pcc_expert_rows(x[:300], place)
+    assert torch.equal(rows, binding.pcc_expert_rows(_shifted(x[:300]), _shifted(place), out=_shifted(torch.zeros_like(rows))))
+    assert torch.equal(binding.pcc_expert_join(rows, place, weight),
+                       binding.pcc_expert_join(_shifted(rows), _shifted(place), _shifted(weight), out=_shifted(torch.zeros(300, features, dtype=BF16, device="cuda"))))
+    want = binding.pcc_expert_join_grad(dy[:300], rows, place, weight)
+    got = binding.pcc_expert_join_grad(_shifted(dy[:300]), _shifted(rows), _shifted(place), _shifted(weight), dz=_shifted(torch.zeros_like(rows)),
+                                       dweight=_shifted(torch.zeros_like(weight)))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
 # ---------------------------------------------------------------------------------------------------- dropout in the trainer
 
 def _picture(h, w):
