@@ -31,6 +31,7 @@ EXPORTS = (
 )
 PCC_BF16, PCC_FP16, PCC_FP32 = 0, 1, 2
 PCC_ACT_RELU, PCC_ACT_LEAKY, PCC_ACT_NONE = 0, 1, 2
+PCC_MAX_EXPERTS, PCC_MAX_CHOICES = 1024, 16
 STATE_BLOCK = 256          # elements of an 8-bit optimizer state that share a scale
 TIMING_NAMES = ("encode_pixels", "encode_rans", "encode_scan", "encode_compact", "decode")
 
@@ -419,9 +420,20 @@ def pcc_mixture_loss(params: torch.Tensor, rgb: torch.Tensor, dist: int = 0, sca
 
 # Layers round the grouped products.
 
+_ANY = tuple(_TYPES)
+
+
+def _made_or_checked(what: str, t, dtype, shape, device):
+    """A contiguous result: a new tensor, or the one that was given."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _check(what, t, (dtype,), shape, device)
+    return t
+
+
 def _norm_groups(x, gamma, offsets):
     """(distance of x's rows, groups) of a layer norm; gamma and offsets may be None."""
-    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    ldx = _check("x", x, _ANY, (None, None), rows=True)
     if offsets is not None:
         _check("offsets", offsets, (torch.int64,), (None,), x.device)
         groups = int(offsets.shape[0]) - 1
@@ -443,16 +455,18 @@ def pcc_layer_norm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: tor
     rows, features = int(x.shape[0]), int(x.shape[1])
     if beta is not None:
         _check("beta", beta, (torch.float32,), (groups, features), x.device)
+    ldy = features
     if out is None:
         out = torch.empty((rows, features), dtype=out_dtype or x.dtype, device=x.device)
-    ldy = _check("out", out, (tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype,)) if out_dtype is None else (out_dtype,), (rows, features), x.device,
-                 rows=True)
-    if stats is None and want_stats:
-        stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
+    else:
+        ldy = _check("out", out, (_ANY if x.dtype == torch.float32 else (x.dtype,)) if out_dtype is None else (out_dtype,), (rows, features), x.device,
+                     rows=True)
     if stats is not None:
         _check("stats", stats, (torch.float32,), (rows, 2), x.device)
+    elif want_stats:
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
     _call("pcc_layer_norm", x.device, x.data_ptr(), ldx, _ptr(gamma), _ptr(beta), _ptr(offsets), groups, rows, features, eps, _TYPES[x.dtype],
-          out.data_ptr(), _TYPES[out.dtype], ldy, _ptr(stats))
+          out.data_ptr(), _TYPES.get(out.dtype, -1), ldy, _ptr(stats))
     return out, stats
 
 
@@ -464,16 +478,16 @@ def pcc_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, 
     _unrecorded(dy, x, stats, gamma, dx, dgamma, dbeta)
     ldx, groups = _norm_groups(x, gamma, offsets)
     rows, features = int(x.shape[0]), int(x.shape[1])
-    lddy = _check("dy", dy, tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype,), (rows, features), x.device, rows=True)
+    lddy = _check("dy", dy, _ANY if x.dtype == torch.float32 else (x.dtype,), (rows, features), x.device, rows=True)
     _check("stats", stats, (torch.float32,), (rows, 2), x.device)
+    lddx = features
     if want_dx and dx is None:
         dx = torch.empty((rows, features), dtype=x.dtype, device=x.device)
-    lddx = _check("dx", dx, (x.dtype,), (rows, features), x.device, rows=True) if want_dx else features
+    elif want_dx:
+        lddx = _check("dx", dx, (x.dtype,), (rows, features), x.device, rows=True)
     if want_weights:
-        dgamma = torch.empty((groups, features), dtype=torch.float32, device=x.device) if dgamma is None else dgamma
-        dbeta = torch.empty((groups, features), dtype=torch.float32, device=x.device) if dbeta is None else dbeta
-        _check("dgamma", dgamma, (torch.float32,), (groups, features), x.device)
-        _check("dbeta", dbeta, (torch.float32,), (groups, features), x.device)
+        dgamma = _made_or_checked("dgamma", dgamma, torch.float32, (groups, features), x.device)
+        dbeta = _made_or_checked("dbeta", dbeta, torch.float32, (groups, features), x.device)
         if workspace is None:
             need = int((_lib or load()).pcc_layer_norm_grad_workspace_bytes(rows, groups, features))
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
@@ -491,12 +505,10 @@ def pcc_route(logits: torch.Tensor, k: int, over_all: bool = False, expert: torc
     """(expert int32 [tokens, k], weight fp32 [tokens, k]): the experts with the k largest logits [tokens, experts] of each token, the largest first, and
     the softmax over them, or with over_all their part of the softmax over all.  A logit of -inf is never chosen: the choice is -1 then, its weight 0."""
     _unrecorded(logits, weight)
-    ldl = _check("logits", logits, tuple(_TYPES), (None, None), rows=True)
+    ldl = _check("logits", logits, _ANY, (None, None), rows=True)
     tokens, experts = int(logits.shape[0]), int(logits.shape[1])
-    expert = torch.empty((tokens, k), dtype=torch.int32, device=logits.device) if expert is None else expert
-    weight = torch.empty((tokens, k), dtype=torch.float32, device=logits.device) if weight is None else weight
-    _check("expert", expert, (torch.int32,), (tokens, k), logits.device)
-    _check("weight", weight, (torch.float32,), (tokens, k), logits.device)
+    expert = _made_or_checked("expert", expert, torch.int32, (tokens, k), logits.device)
+    weight = _made_or_checked("weight", weight, torch.float32, (tokens, k), logits.device)
     _call("pcc_route", logits.device, logits.data_ptr(), ldl, tokens, experts, k, _TYPES[logits.dtype], int(over_all), expert.data_ptr(), weight.data_ptr())
     return expert, weight
 
@@ -505,14 +517,17 @@ def pcc_route_grad(dweight: torch.Tensor, logits: torch.Tensor, expert: torch.Te
                    dlogits: torch.Tensor | None = None) -> torch.Tensor:
     """The logits' gradient, of their type, from that of the weights fp32 [tokens, k] and what pcc_route gave."""
     _unrecorded(dweight, logits, weight, dlogits)
-    ldl = _check("logits", logits, tuple(_TYPES), (None, None), rows=True)
+    ldl = _check("logits", logits, _ANY, (None, None), rows=True)
     tokens, experts = int(logits.shape[0]), int(logits.shape[1])
     _check("expert", expert, (torch.int32,), (tokens, None), logits.device)
     k = int(expert.shape[1])
     _check("weight", weight, (torch.float32,), (tokens, k), logits.device)
     _check("dweight", dweight, (torch.float32,), (tokens, k), logits.device)
-    dlogits = torch.empty((tokens, experts), dtype=logits.dtype, device=logits.device) if dlogits is None else dlogits
-    lddl = _check("dlogits", dlogits, (logits.dtype,), (tokens, experts), logits.device, rows=True)
+    lddl = experts
+    if dlogits is None:
+        dlogits = torch.empty((tokens, experts), dtype=logits.dtype, device=logits.device)
+    else:
+        lddl = _check("dlogits", dlogits, (logits.dtype,), (tokens, experts), logits.device, rows=True)
     _call("pcc_route_grad", logits.device, dweight.data_ptr(), logits.data_ptr(), ldl, expert.data_ptr(), weight.data_ptr(), tokens, experts, k,
           _TYPES[logits.dtype], int(over_all), dlogits.data_ptr(), lddl)
     return dlogits
@@ -524,10 +539,10 @@ def pcc_expert_sort(expert: torch.Tensor, experts: int, offsets: torch.Tensor | 
     token.  A choice outside 0..experts - 1 has place -1."""
     _check("expert", expert, (torch.int32,), (None, None))
     tokens, k = int(expert.shape[0]), int(expert.shape[1])
-    offsets = torch.empty(experts + 1, dtype=torch.int64, device=expert.device) if offsets is None else offsets
-    place = torch.empty((tokens, k), dtype=torch.int32, device=expert.device) if place is None else place
-    _check("offsets", offsets, (torch.int64,), (experts + 1,), expert.device)
-    _check("place", place, (torch.int32,), (tokens, k), expert.device)
+    if not 0 < experts <= PCC_MAX_EXPERTS:
+        raise ValueError("experts must be 1 to %d" % PCC_MAX_EXPERTS)
+    offsets = _made_or_checked("offsets", offsets, torch.int64, (experts + 1,), expert.device)
+    place = _made_or_checked("place", place, torch.int32, (tokens, k), expert.device)
     if workspace is None:
         need = int((_lib or load()).pcc_expert_sort_workspace_bytes(tokens, k, experts))
         workspace = torch.empty(need, dtype=torch.uint8, device=expert.device) if need else None
@@ -547,13 +562,16 @@ def pcc_expert_rows(x: torch.Tensor, place: torch.Tensor, out: torch.Tensor | No
     """Rows of each expert, one behind the other: out[place[t, j]] = x[t].  out [rows, features] has tokens * k rows by default; rows that no choice has
     are left as they are in `out`, and undefined in a new tensor.  (The gradient is pcc_expert_join without weights.)"""
     _unrecorded(x, out)
-    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    ldx = _check("x", x, _ANY, (None, None), rows=True)
     tokens, k = _check_place(place, x.device)
     features = int(x.shape[1])
     if int(x.shape[0]) != tokens:
         raise ValueError("x and place must have one row for each token")
-    out = torch.empty((tokens * k, features), dtype=x.dtype, device=x.device) if out is None else out
-    ldr = _check("out", out, (x.dtype,), (None, features), x.device, rows=True)
+    ldr = features
+    if out is None:
+        out = torch.empty((tokens * k, features), dtype=x.dtype, device=x.device)
+    else:
+        ldr = _check("out", out, (x.dtype,), (None, features), x.device, rows=True)
     _call("pcc_expert_rows", x.device, x.data_ptr(), ldx, place.data_ptr(), tokens, k, out.shape[0], features, _TYPES[x.dtype], out.data_ptr(), ldr)
     return out
 
@@ -562,15 +580,18 @@ def pcc_expert_join(z: torch.Tensor, place: torch.Tensor, weight: torch.Tensor |
                     out_dtype: torch.dtype | None = None) -> torch.Tensor:
     """y[t] = sum over j of weight[t, j] z[place[t, j]] (None: weights of 1), summed in fp32.  z [rows, features]; y has its type or fp32."""
     _unrecorded(z, weight, out)
-    ldz = _check("z", z, tuple(_TYPES), (None, None), rows=True)
+    ldz = _check("z", z, _ANY, (None, None), rows=True)
     tokens, k = _check_place(place, z.device)
     rows, features = int(z.shape[0]), int(z.shape[1])
     if weight is not None:
         _check("weight", weight, (torch.float32,), (tokens, k), z.device)
-    out = torch.empty((tokens, features), dtype=out_dtype or z.dtype, device=z.device) if out is None else out
-    ldy = _check("out", out, (z.dtype, torch.float32) if out_dtype is None else (out_dtype,), (tokens, features), z.device, rows=True)
+    ldy = features
+    if out is None:
+        out = torch.empty((tokens, features), dtype=out_dtype or z.dtype, device=z.device)
+    else:
+        ldy = _check("out", out, (z.dtype, torch.float32) if out_dtype is None else (out_dtype,), (tokens, features), z.device, rows=True)
     _call("pcc_expert_join", z.device, z.data_ptr(), ldz, place.data_ptr(), _ptr(weight), tokens, k, rows, features, _TYPES[z.dtype], out.data_ptr(),
-          _TYPES[out.dtype], ldy)
+          _TYPES.get(out.dtype, -1), ldy)
     return out
 
 
@@ -579,17 +600,19 @@ def pcc_expert_join_grad(dy: torch.Tensor, z: torch.Tensor, place: torch.Tensor,
     """(dz, dweight) of pcc_expert_join: dz has z's type, dweight fp32 [tokens, k] (None without want_dweight).  Rows that no choice has are left as they are
     in `dz`, and undefined in a new tensor."""
     _unrecorded(dy, z, weight, dz, dweight)
-    ldz = _check("z", z, tuple(_TYPES), (None, None), rows=True)
+    ldz = _check("z", z, _ANY, (None, None), rows=True)
     tokens, k = _check_place(place, z.device)
     rows, features = int(z.shape[0]), int(z.shape[1])
     lddy = _check("dy", dy, (z.dtype, torch.float32), (tokens, features), z.device, rows=True)
     if weight is not None:
         _check("weight", weight, (torch.float32,), (tokens, k), z.device)
-    dz = torch.empty((rows, features), dtype=z.dtype, device=z.device) if dz is None else dz
-    lddz = _check("dz", dz, (z.dtype,), (rows, features), z.device, rows=True)
+    lddz = features
+    if dz is None:
+        dz = torch.empty((rows, features), dtype=z.dtype, device=z.device)
+    else:
+        lddz = _check("dz", dz, (z.dtype,), (rows, features), z.device, rows=True)
     if want_dweight:
-        dweight = torch.empty((tokens, k), dtype=torch.float32, device=z.device) if dweight is None else dweight
-        _check("dweight", dweight, (torch.float32,), (tokens, k), z.device)
+        dweight = _made_or_checked("dweight", dweight, torch.float32, (tokens, k), z.device)
     _call("pcc_expert_join_grad", z.device, dy.data_ptr(), _TYPES[dy.dtype], lddy, z.data_ptr(), ldz, place.data_ptr(), _ptr(weight), tokens, k, rows, features,
           _TYPES[z.dtype], dz.data_ptr(), lddz, dweight.data_ptr() if want_dweight else None)
     return dz, (dweight if want_dweight else None)
@@ -601,17 +624,20 @@ def pcc_dropout(x: torch.Tensor, p: float, seed: int, step: torch.Tensor | None 
     (64 bits), step (int64 [1] on the device, None: 0), row and column alone: the same call on the gradient is the backward pass.  p is taken to the
     nearest 1/65536.  The result has x's type, or one of the two is fp32; residual has the result's.  `out` may be x or residual."""
     _unrecorded(x, residual, out)
-    ldx = _check("x", x, tuple(_TYPES), (None, None), rows=True)
+    ldx = _check("x", x, _ANY, (None, None), rows=True)
     shape, seed = (int(x.shape[0]), int(x.shape[1])), int(seed)
     if not 0 <= seed < 1 << 64:
         raise ValueError("seed must be a whole number of 64 bits")
     if step is not None:
         _check("step", step, (torch.int64,), (1,), x.device)
-    out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device) if out is None else out
-    ldy = _check("out", out, (tuple(_TYPES) if x.dtype == torch.float32 else (x.dtype, torch.float32)) if out_dtype is None else (out_dtype,), shape, x.device, rows=True)
+    ldy = shape[1]
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype or x.dtype, device=x.device)
+    else:
+        ldy = _check("out", out, (_ANY if x.dtype == torch.float32 else (x.dtype, torch.float32)) if out_dtype is None else (out_dtype,), shape, x.device, rows=True)
     ldr = _check("residual", residual, (out.dtype,), shape, x.device, rows=True) if residual is not None else shape[1]
     _call("pcc_dropout", x.device, x.data_ptr(), ldx, _ptr(residual), ldr, shape[0], shape[1], _TYPES[x.dtype], p, seed, _ptr(step), out.data_ptr(),
-          _TYPES[out.dtype], ldy)
+          _TYPES.get(out.dtype, -1), ldy)
     return out
 
 

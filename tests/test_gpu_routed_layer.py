@@ -280,6 +280,22 @@ def test_weights_statistics_and_places_at_any_address(features):
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_types_that_no_operator_has_are_refused():
+    x, place = torch.zeros(4, 8, dtype=BF16, device="cuda"), torch.zeros(4, 1, dtype=torch.int32, device="cuda")
+    for bad in (lambda: binding.pcc_layer_norm(x, out_dtype=torch.float64), lambda: binding.pcc_layer_norm(x, out_dtype=FP16), lambda: binding.pcc_layer_norm(x, out_dtype=FP32),
+                lambda: binding.pcc_dropout(x, 0.1, 1, out_dtype=FP16), lambda: binding.pcc_dropout(x, 0.1, 1, out_dtype=torch.float64),
+                lambda: binding.pcc_expert_join(x, place, out_dtype=FP16), lambda: binding.pcc_route(x, 9), lambda: binding.pcc_route(x, 0), lambda: binding.pcc_dropout(x, 1.5, 1)):
+        with pytest.raises(binding.PccError):
+            bad()
+    for bad in (lambda: binding.pcc_layer_norm(x.double()), lambda: binding.pcc_layer_norm(x.t()), lambda: binding.pcc_layer_norm(x[:1].expand(4, 8)),
+                lambda: binding.pcc_layer_norm(x, torch.ones(2, 8, device="cuda")), lambda: binding.pcc_layer_norm(x, torch.ones(1, 8)),
+                lambda: binding.pcc_expert_sort(place, 0), lambda: binding.pcc_expert_sort(place, 1025), lambda: binding.pcc_expert_sort(place.long(), 4),
+                lambda: binding.pcc_expert_rows(x[:3], place), lambda: binding.pcc_dropout(x, 0.1, -1), lambda: binding.pcc_dropout(x, 0.1, 1 << 64),
+                lambda: binding.pcc_dropout(x, 0.1, 1, residual=x.float())):
+        with pytest.raises(ValueError):
+            bad()
+
+
 # ---------------------------------------------------------------------------------------------------- dropout in the trainer
 
 def _picture(h, w):
