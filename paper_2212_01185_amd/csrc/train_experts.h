@@ -146,7 +146,7 @@ struct Experts {
 constexpr int kExpertThreads = 256;
 
 // Memory bounds all of these.  us, 393,216 tokens with 2 rows of 160 in bf16 each: rows 69 (5.4 TB/s), join 72 (5.3), its gradient 124 (5.1); 8,192 tokens with
-// four of 2,048, join to fp32, 40 (5.0).
+// four of 2,048, join to fp32, 43 (4.6).
 // A token's row has LANES lanes, parts of LANES * N eights one after the other.  A die has neighbouring tokens, whose rows of one expert are neighbours
 // as well and share lines of its L2.
 template <int LANES>
@@ -209,9 +209,9 @@ __global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) 
         Row<Y, LANES, N> y;
         Z::each(lane, w, [&](auto, auto i) {
             y.at(i).set(sum.at(i));
-            // past the caches where neighbouring lanes write neighbouring 16 bytes: 393,216 rows of 160 in bf16 72 us and 76, but 8,192 of 2,048 in fp32 44 and 40
-            if constexpr (!kIs32<Y>) y.store_past(i, a.y, token * a.ldy + 8 * c0, lane, w);
-            else y.store(i, a.y, token * a.ldy + 8 * c0, lane, w);
+            // past the caches, us so and not: 393,216 rows of 160 in bf16 72 and 76, 8,192 of 2,048 in fp32 43 and 46 (but 44 and 40 where three sets of
+            // inputs and results are all there is, and the last results still lie in the caches when they are written again)
+            y.store_past(i, a.y, token * a.ldy + 8 * c0, lane, w);
         });
     }
 }

@@ -115,7 +115,7 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t moved(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true);
 }
-constexpr int kSwapPairs = 0xB1, kSwapTwos = 0x4E, kMirrorEight = 0x141, kMirrorRow = 0x140, kTurnFour = 0x124, kTurnEight = 0x128;
+constexpr int kSwapPairs = 0xB1, kSwapTwos = 0x4E, kMirrorEight = 0x141, kMirrorRow = 0x140, kTurnEight = 0x128;
 
 template <int G, class V, class F>
 __device__ __forceinline__ V over_lanes(V v, F&& join) {
@@ -145,7 +145,7 @@ template <int G>
 __device__ __forceinline__ float groups_sum(float v) {
     auto bits = [](float x) { return __builtin_bit_cast(uint32_t, x); };
     auto value = [](uint32_t x) { return __builtin_bit_cast(float, x); };
-    if constexpr (G <= 4) v += value(moved<kTurnFour>(bits(v)));
+    static_assert(G >= 8, "a row has eight lanes at least");
     if constexpr (G <= 8) v += value(moved<kTurnEight>(bits(v)));
     if constexpr (G <= 16) {
         const auto p = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
