@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import routed_reference as ref
-from paper_2212_01185_amd import binding
+from paper_2212_01185_amd import binding, synth, train
 
 ARG, SCRATCH, OK = binding.PCC_E_ARG, binding.PCC_E_SCRATCH, binding.PCC_OK
 # stand for device pointers, far from each other: a refused call never follows them
@@ -158,6 +158,12 @@ def test_python_arguments():
                 lambda: binding.pcc_dropout(x, 0.1, 1, residual=asks(x))):
         with pytest.raises(ValueError, match="autograd"):
             bad()
+
+
+@pytest.mark.parametrize("dropout", [1.0, -0.5, float("nan"), 2])
+def test_trainer_wants_a_share_below_one(dropout):
+    with pytest.raises(ValueError, match="dropout"):
+        train.Trainer(synth.make_blob(0), dropout=dropout)
 
 
 def test_the_reference_makes_philox_published_outputs():
