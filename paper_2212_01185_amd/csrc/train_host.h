@@ -58,10 +58,12 @@ inline bool overlap(const Span& a, std::initializer_list<Span> others) {
 }
 inline bool ld_ok(size_t ld, int features) { return ld >= (size_t)features && ld <= kMaxLd; }
 
-// More LDS than 64 KB has to be asked for; per device and kernel, and cheap enough to do at every launch.
+// More LDS than 64 KB, a kernel's static variables among it, has to be asked for; per device and kernel, and cheap enough to do at every launch.
+// No kernel that comes here has more than this of static ones (the norm's forward pass of 1024 lanes has 384 bytes).
+constexpr size_t kStaticLds = 1024;
 template <class K>
 bool allow_lds(K kernel, size_t bytes) {
-    return bytes <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+    return bytes <= 64 * 1024 - kStaticLds || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
 }
 
 // Chunks of mult * 2^log2 rows: about rows / want rows, in steps of 1/4 to 1/8 of a power of two, and a multiple of `unit` (a power of two).  The
