@@ -264,14 +264,14 @@ __global__ __launch_bounds__(norm_grad_threads(LANES, N)) void layer_norm_grad_k
         h.x.forget();
         h.dy.forget();
         if (a.y) {
-            // scale (u - m1 - (x - mean) scale m2)
-            const float m1 = -(scale * (s1 * a.inverse)), m2 = -(scale * scale * (s2 * a.inverse));
+            // in the formula's order: with scale taken into the means, its square would leave fp32's range long before dx does (scale is up to 2^63)
+            const float m1 = -(s1 * a.inverse), m2 = -(s2 * a.inverse);
             R dx;
             R::each(lane, w, [&](auto wide, auto i) {
                 const Eight<Fp32> g = gamma.get<wide>(i < N ? lane + LANES * i : lane);
                 float v[8] = {};
 #pragma unroll
-                for (int e = 0; e < wide; ++e) v[e] = __builtin_fmaf(h.x.at(i).get(e) - mean, m2, __builtin_fmaf(h.dy.at(i).get(e) * g.get(e), scale, m1));
+                for (int e = 0; e < wide; ++e) v[e] = scale * __builtin_fmaf((h.x.at(i).get(e) - mean) * scale, m2, __builtin_fmaf(h.dy.at(i).get(e), g.get(e), m1));
                 dx.at(i).set(v);
                 dx.store(i, a.y, (size_t)(ch.lo + r0 + team) * a.ldy, lane, w);
             });
