@@ -4,7 +4,8 @@
 //   with u = gamma dy:  dx = s (u - mean(u) - h mean(u h)),  dgamma = sum over rows of dy h,  dbeta = sum of dy
 //
 // A row is read once: LANES lanes have it in registers, eight neighbours at a time, so the variance is that of the distances from the
-// mean and not a difference of two large sums.  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
+// mean and not a difference of two large sums.  The mean is a sum's first, which is off by the roundings of a sum as large as the values, and the mean of the
+// distances from it: a row of one value has that mean exactly, and distances and a variance of 0 (see `centred`).  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
 // forward 57 us, 4.7 TB/s (a large copy has 5.2); backward 393,216 rows of 160 85 us, 4.5 TB/s, of which 5 join the chunks' sums, and the vector ALU
 // is busy for about half of it.
 #pragma once
@@ -108,8 +109,23 @@ struct Weights {
 template <int TEAMS, int WAVES>
 struct Parts {
     float size[WAVES], inverse[WAVES];
-    float sum[2][TEAMS][WAVES], squares[2][TEAMS][WAVES];
+    float mean[2][TEAMS][WAVES], squares[2][TEAMS][WAVES];
 };
+
+// The mean of n values and the sum of their squares about it, from a first mean, the sum `rest` of the distances from it and the sum of those' squares: the
+// mean is off by rest / n, which adds rest^2 / n to the squares.  Where that is not a small part of them (rows whose values are nearly one
+// value, far from 0), what would be left of the squares is their rounding: they are summed again, by again(mean), which every lane of the wave calls.
+template <class F>
+__device__ __forceinline__ void centred(float& mean, float& squares, float rest, float inverse, F&& again) {
+    const float off = rest * inverse;
+    const bool anew = !(64.0f * off * rest < squares);      // (also where squares about the first mean are infinite)
+    mean += off;
+    squares -= rest * off;
+    if (__any(anew)) {
+        const float s = again(mean);
+        squares = anew ? s : squares;       // a row's result does not hang on those beside it
+    }
+}
 
 template <class X, class Y, int LANES, int N>
 __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a) {
@@ -139,34 +155,48 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
     auto step = [&](R& x, R& next, int r0, int turn) {
         const Extent w(features, r0 + team < n);
         next.load(a.x, (size_t)(ch.lo + r0 + kTeams + team) * a.ldx, lane, Extent(features, r0 + kTeams + team < n));
-        float sum = 0.0f, squares = 0.0f;
+        constexpr int kGroup = LANES < 64 ? LANES : 64;
+        float sum = 0.0f, rest = 0.0f, squares = 0.0f;
         R::each(lane, w, [&](auto wide, auto i) {
 #pragma unroll
             for (int e = 0; e < wide; ++e) sum += x.at(i).get(e);
         });
-        sum = lanes_sum<(LANES < 64 ? LANES : 64)>(sum);
-        float mean = sum * own;         // of the wave's part
+        float mean = lanes_sum<kGroup>(sum) * own;         // of the wave's part
         R::each(lane, w, [&](auto wide, auto i) {
 #pragma unroll
             for (int e = 0; e < wide; ++e) {
                 const float d = x.at(i).get(e) - mean;
+                rest += d;
                 squares = __builtin_fmaf(d, d, squares);
             }
         });
-        squares = lanes_sum<(LANES < 64 ? LANES : 64)>(squares);
+        squares = lanes_sum<kGroup>(squares);
+        centred(mean, squares, lanes_sum<kGroup>(rest), own, [&](float mean) {
+            float s = 0.0f;
+            R::each(lane, w, [&](auto wide, auto i) {
+#pragma unroll
+                for (int e = 0; e < wide; ++e) {
+                    const float d = x.at(i).get(e) - mean;
+                    s = __builtin_fmaf(d, d, s);
+                }
+            });
+            return lanes_sum<kGroup>(s);
+        });
         if constexpr (kWaves > 1) {
             if ((threadIdx.x & 63) == 0) {
-                parts.sum[turn][team][wave] = sum;
+                parts.mean[turn][team][wave] = mean;
                 parts.squares[turn][team][wave] = squares;
             }
             __syncthreads();
-            sum = squares = 0.0f;
+            // the mean by the parts' distances from the first one's: of equal ones it is that one
+            const float first = parts.mean[turn][team][0];
+            rest = squares = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) sum += parts.sum[turn][team][k];
-            mean = sum * a.inverse;
+            for (int k = 1; k < kWaves; ++k) rest = __builtin_fmaf(parts.size[k], parts.mean[turn][team][k] - first, rest);
+            mean = __builtin_fmaf(rest, a.inverse, first);
 #pragma unroll
             for (int k = 0; k < kWaves; ++k) {
-                const float d = __builtin_fmaf(parts.sum[turn][team][k], parts.inverse[k], -mean);
+                const float d = parts.mean[turn][team][k] - mean;
                 squares += __builtin_fmaf(parts.size[k] * d, d, parts.squares[turn][team][k]);
             }
         }
@@ -341,31 +371,40 @@ constexpr int kLongThreads = 1024;
 
 template <class X, class Y>
 __global__ __launch_bounds__(kLongThreads) void layer_norm_long_kernel(Norm a) {
-    __shared__ float meet[2][16];
+    __shared__ float meet[4][16];
     const Chunk ch = norm_chunk(a, blockIdx.x, false);
     if (ch.group < 0) return;
     const float* gamma = a.gamma ? a.gamma + (size_t)ch.group * a.features : nullptr;
     const float* beta = a.beta ? a.beta + (size_t)ch.group * a.features : nullptr;
     for (int64_t row = ch.lo; row < ch.hi; ++row) {
         const size_t at = (size_t)row * a.ldx;
-        float sum = 0.0f, squares = 0.0f;
-        for (int f = 8 * threadIdx.x; f < a.features; f += 8 * kLongThreads) {
-            Eight<X> x;
-            x.load(a.x, at + f, a.features - f);
+        float sum = 0.0f, rest = 0.0f, squares = 0.0f;
+        auto each = [&](auto f) {
+            for (int c = 8 * threadIdx.x; c < a.features; c += 8 * kLongThreads) {
+                Eight<X> x;
+                x.load(a.x, at + c, a.features - c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += x.get(e);
-        }
-        const float mean = row_sum<kLongThreads>(sum, meet, 0) * a.inverse;
-        for (int f = 8 * threadIdx.x; f < a.features; f += 8 * kLongThreads) {
-            Eight<X> x;
-            x.load(a.x, at + f, a.features - f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = x.get(e) - mean;
-                squares += f + e < a.features ? d * d : 0.0f;
+                for (int e = 0; e < 8; ++e) f(x.get(e), c + e < a.features);
             }
-        }
-        const float scale = 1.0f / sqrtf(row_sum<kLongThreads>(squares, meet, 1) * a.inverse + a.eps);
+        };
+        each([&](float v, bool) { sum += v; });     // zeros behind the last
+        float mean = row_sum<kLongThreads>(sum, meet, 0) * a.inverse;
+        each([&](float v, bool there) {
+            const float d = there ? v - mean : 0.0f;
+            rest += d;
+            squares = __builtin_fmaf(d, d, squares);
+        });
+        rest = row_sum<kLongThreads>(rest, meet, 1);
+        squares = row_sum<kLongThreads>(squares, meet, 2);
+        centred(mean, squares, rest, a.inverse, [&](float mean) {       // the same sums in all waves
+            float s = 0.0f;
+            each([&](float v, bool there) {
+                const float d = there ? v - mean : 0.0f;
+                s = __builtin_fmaf(d, d, s);
+            });
+            return row_sum<kLongThreads>(s, meet, 3);
+        });
+        const float scale = 1.0f / sqrtf(squares * a.inverse + a.eps);
         if (a.stats && threadIdx.x == 0) {
             a.stats[2 * row] = mean;
             a.stats[2 * row + 1] = scale;

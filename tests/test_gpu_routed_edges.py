@@ -36,3 +36,63 @@ def test_layer_norm_gradient_of_rows_of_any_size(features, size, dsize, eps):
         for name, t, (value, limit) in zip(("dx", "dgamma", "dbeta"), got, ref.layer_norm_grad(dy, x, stats, gamma, [0, 6])):
             assert value.abs().max() < 1e38
             assert_near(t, value, limit, (name, x_type, y_type))
+
+
+SHAPES = [5, 8, 30, 120, 160, 240, 513, 960, 1000, 2056, 3000, 4096, 8193, 12301, 16384, 20000, 40001, 65536]
+
+
+@pytest.mark.parametrize("features", SHAPES)
+def test_layer_norm_of_rows_of_one_value_is_beta(features):
+    """Whatever the value, the mean is it: no distance, and a width of the root of eps."""
+    gen = torch.Generator().manual_seed(features)
+    wild = (1 + torch.rand(40, generator=gen)) * 10.0 ** torch.randint(-18, 19, (40,), generator=gen) * (torch.randint(0, 2, (40,), generator=gen) * 2 - 1)
+    values = torch.cat([torch.tensor([0.0, 1.0, -3.0, 12032.0, 12345.678, 1e-20, 1e15, 0.1, 1e30]), wild])
+    gamma, beta = torch.randn(1, features, generator=gen).cuda(), torch.randn(1, features, generator=gen).cuda()
+    for dtype, eps in ((BF16, 1e-5), (FP16, 1e-5), (FP32, 1e-5), (FP32, 1e-30)):
+        x = values.to(dtype)
+        x = x[torch.isfinite(x)][:, None].expand(-1, features).contiguous().cuda()
+        y, stats = binding.pcc_layer_norm(x, gamma, beta, eps=eps, out_dtype=dtype)
+        assert torch.equal(stats[:, 0], x[:, 0].float())
+        assert ((stats[:, 1].double() * eps ** 0.5 - 1).abs() <= 4 * ref.U).all()      # eps in fp32 (a half), 1 / sqrt of the hardware (one step)
+        assert torch.equal(y, beta.to(dtype).expand(len(x), -1))
+
+
+def _norm_bounds(x, gamma, beta, eps):
+    """y, the statistics and their bounds where a mean may be far from 0 against the width: the mean is right but for its own rounding and those of
+    the sum of the distances from a first mean, which is off by a sum's roundings."""
+    x = x.double().cpu()
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    var = (d * d).mean(1, keepdim=True)
+    s = (var + eps) ** -0.5
+    h = d * s
+    away = d.abs().mean(1, keepdim=True)
+    first = (ref.DEPTH + 2) * ref.U * x.abs().mean(1, keepdim=True)
+    # a wave's mean and the row's are rounded to fp32; distances from the first mean are as large as d and its error
+    e_mean = 2 * ref.U * mean.abs() + (ref.DEPTH + 4) * ref.U * (away + first)
+    # squares about the first mean, of which what its error adds is taken off: 1/64 of them at most, else they are summed anew
+    e_var = (ref.DEPTH + 8) * ref.U * var * (1 + 1 / 32) + 2 * away * e_mean + e_mean ** 2
+    low = (var + eps - e_var).clamp_min(eps / 2)
+    e_s = s * (e_var / (2 * low) + 5 * ref.U)
+    e_h = s * e_mean + 3 * ref.U * h.abs() + (d.abs() + e_mean) * e_s
+    g, b = gamma.double().cpu(), beta.double().cpu()
+    return (g * h + b, g.abs() * e_h + 2 * ref.U * ((g * h + b).abs() + (g * h).abs())), (torch.cat([mean, s], 1), torch.cat([e_mean, e_s], 1))
+
+
+@pytest.mark.parametrize("features", SHAPES)
+def test_layer_norm_of_rows_far_from_0(features):
+    """Means of up to a million widths, and rows with one value that is far larger than all others, first, last or between."""
+    gen = torch.Generator().manual_seed(features + 1)
+    x = torch.randn(40, features, generator=gen)
+    x[:20] = x[:20] * 10.0 ** torch.linspace(-6, 0, 20)[:, None] + torch.randn(20, 1, generator=gen) + 1
+    for i, at in enumerate((0, features - 1, features // 2)):
+        x[20 + i, at], x[24 + i, at] = 1e4, -1e7
+    gamma, beta = torch.randn(1, features, generator=gen), torch.randn(1, features, generator=gen)
+    for eps in (1e-5, 1e-14):
+        y, stats = binding.pcc_layer_norm(x.cuda(), gamma.cuda(), beta.cuda(), eps=eps)
+        (want, bound), (want_stats, stats_bound) = _norm_bounds(x, gamma, beta, eps)
+        assert_near(stats, want_stats, stats_bound, ("stats", eps))
+        assert_near(y, want, bound, ("y", eps))
+    # a row's bits do not hang on its neighbours
+    alone = torch.cat([binding.pcc_layer_norm(x[i:i + 1].cuda(), gamma.cuda(), beta.cuda(), eps=1e-14)[0] for i in range(40)])
+    assert torch.equal(alone, y)
