@@ -274,7 +274,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float g = e < 4 ? low[e] : high[e - 4];
-            d[e] = a.over_all ? p[i][e] * inverse * (g - along) : g;
+            // (a masked logit's 0 is no product: along or the sum may be infinite or NaN)
+            d[e] = !a.over_all ? g : l[i].get(e) == -__builtin_inff() ? 0.0f : p[i][e] * inverse * (g - along);
         }
         Eight<T> out;
         out.set(d);

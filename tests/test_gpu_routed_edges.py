@@ -96,3 +96,27 @@ def test_layer_norm_of_rows_far_from_0(features):
     # a row's bits do not hang on its neighbours
     alone = torch.cat([binding.pcc_layer_norm(x[i:i + 1].cuda(), gamma.cuda(), beta.cuda(), eps=1e-14)[0] for i in range(40)])
     assert torch.equal(alone, y)
+
+
+@pytest.mark.parametrize("experts,k", [(3, 2), (8, 2), (12, 2), (64, 8), (65, 3), (200, 16), (1000, 4)])
+@pytest.mark.parametrize("dtype", [FP32, BF16, FP16])
+def test_route_gradient_of_a_masked_logit_is_0_beside_what_is_not_a_number(dtype, experts, k):
+    """Experts that may not be taken keep a gradient of 0 where the token's other gradients are NaN or infinite."""
+    gen = torch.Generator().manual_seed(experts)
+    logits = torch.randn(70, experts, generator=gen)
+    dweight = torch.randn(70, k, generator=gen)
+    logits[::7, 0], logits[1::7, 0] = float("nan"), float("inf")
+    dweight[2::7, 0], dweight[3::7, 1], dweight[4::7, 0] = float("nan"), float("inf"), -float("inf")
+    plain = torch.zeros(70, dtype=torch.bool)
+    plain[5::7] = plain[6::7] = True
+    logits[:, experts // 2::2] = -float("inf")
+    logits = logits.to(dtype)
+    masked = logits == -float("inf")
+    for over_all in (False, True):
+        expert, weight = binding.pcc_route(logits.cuda(), k, over_all=over_all)
+        got = binding.pcc_route_grad(dweight.cuda(), logits.cuda(), expert, weight, over_all=over_all).cpu()
+        assert (got[masked] == 0).all()
+        if over_all:                                # each open one's gradient hangs on all of them: p (0 - sum w dw) at least is not finite
+            assert not torch.isfinite(got[~plain][~masked[~plain]]).any()
+        value, limit = ref.route_grad(torch.where(expert.cpu() >= 0, dweight, torch.zeros(())), logits, expert.cpu(), k, over_all)
+        assert_near(got[plain], value[plain], limit[plain], (dtype, over_all))
