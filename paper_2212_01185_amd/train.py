@@ -53,8 +53,9 @@ class Trainer:
             raise ValueError("blobs must be one or more networks of one shape")
         if not eps > 0:
             raise ValueError("eps must be above 0: padded inputs and networks without pictures have moments of 0")
-        if not 0 <= dropout < 1:
-            raise ValueError("dropout must be in [0, 1)")
+        # (the operator takes the share to the nearest 1/65536: one that it would round to 1 drops everything)
+        if not (0 <= dropout < 1 and int(dropout * 65536 + 0.5) < 65536):
+            raise ValueError("dropout must be in [0, 1 - 2^-17)")
         self.dropout, self.seed = float(dropout), int(seed)
         self.k, self.nbhd, self.delay, self.act, self.dist = parsed[0][1:]
         self.groups, self.device = len(parsed), torch.device("cuda", device)
