@@ -40,10 +40,17 @@ def parse_blob(blob: bytes):
     return (layers,) + tuple(words[11:16])
 
 
+def mask_seed(number: int) -> int:
+    """A seed of dropout's masks for the run of this number (any whole number): those of the first 2^32 runs, and of as many below 0, are more than
+    2^20 apart, modulo 2^64."""
+    return number * 0x9E3779B97F4A7C15 % (1 << 64)      # odd, and far from every fraction of 2^64 with a small denominator
+
+
 class Trainer:
     """Networks of one shape under training.  ``blobs``: the weight blobs they start from, one a network.  ``dropout``: the share of each hidden layer's
     results that a step leaves out (the others are scaled up; a blob is the whole network), with masks fixed by ``seed``, the step's number
-    and a pixel's place among all of the step's."""
+    and a pixel's place among all of the step's.  Layer l's masks have the key seed + l, modulo 2^64: trainers that shall not share masks take seeds
+    at least as far apart as there are hidden layers, as `mask_seed` makes them."""
 
     def __init__(self, blobs, device: int = 0, lr: float = 1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                  state_bits: int = 32, lr_tensor=None, dropout: float = 0.0, seed: int = 0):
@@ -171,7 +178,7 @@ def main(argv=None) -> None:
             start = f.read()
     else:
         start = {"workload": synth.make_blob, "paper": synth.make_paper_blob, "diagonal": synth.make_diagonal_blob}[a.network](a.seed)
-    trainer = Trainer(start, lr=a.lr, state_bits=a.state_bits, dropout=a.dropout, seed=a.seed % (1 << 64))
+    trainer = Trainer(start, lr=a.lr, state_bits=a.state_bits, dropout=a.dropout, seed=mask_seed(a.seed))
     rng = np.random.default_rng(a.seed)
     n, h, w, _ = pictures.shape
     ch, cw = min(a.crop, h), min(a.crop, w)
