@@ -506,6 +506,8 @@ def pcc_route(logits: torch.Tensor, k: int, over_all: bool = False, expert: torc
     the softmax over them, or with over_all their part of the softmax over all.  A logit of -inf is never chosen: the choice is -1 then, its weight 0."""
     _unrecorded(logits, weight)
     ldl = _check("logits", logits, _ANY, (None, None), rows=True)
+    if not 0 < k <= PCC_MAX_CHOICES:                # before results of k columns are made
+        raise PccError(PCC_E_ARG, "pcc_route")
     tokens, experts = int(logits.shape[0]), int(logits.shape[1])
     expert = _made_or_checked("expert", expert, torch.int32, (tokens, k), logits.device)
     weight = _made_or_checked("weight", weight, torch.float32, (tokens, k), logits.device)

@@ -120,3 +120,9 @@ def test_route_gradient_of_a_masked_logit_is_0_beside_what_is_not_a_number(dtype
             assert not torch.isfinite(got[~plain][~masked[~plain]]).any()
         value, limit = ref.route_grad(torch.where(expert.cpu() >= 0, dweight, torch.zeros(())), logits, expert.cpu(), k, over_all)
         assert_near(got[plain], value[plain], limit[plain], (dtype, over_all))
+
+
+@pytest.mark.parametrize("k", [-1, 0, 17, 1 << 50])
+def test_route_refuses_a_number_of_choices_before_it_makes_room_for_them(k):
+    with pytest.raises(binding.PccError):
+        binding.pcc_route(torch.zeros(4, 32, device="cuda"), k)
