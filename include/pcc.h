@@ -348,7 +348,11 @@ int pcc_adamw_step(pcc_adamw *plan, const pcc_adamw_hyper *h_hyper, int64_t *d_s
  *   d_offsets [groups + 1] as above, or NULL for one group of all rows.  d_stats
  *   [rows][2] fp32 or NULL: each row's mean and 1 / sqrt(...), which the backward
  *   pass takes.  Rows of no group are neither read nor written.  eps is at least
- *   2^-126. */
+ *   2^-126.
+ * The mean is right to its rounding to fp32, also far from 0: a row of one value
+ * has y = beta.  Squares of distances from it are summed in fp32: a finite row for
+ * which that sum is infinite (distances beyond 2^64 / sqrt(features)) has
+ * 1 / sqrt(...) = 0. */
 int pcc_layer_norm(const void *d_x, size_t ldx, const float *d_gamma, const float *d_beta,
                    const int64_t *d_offsets, int groups, size_t rows, int features, float eps,
                    int type, void *d_y, int y_type, size_t ldy, float *d_stats, void *hip_stream);
@@ -379,7 +383,7 @@ int pcc_route(const void *d_logits, size_t ldl, size_t tokens, int experts, int 
 /* Its gradient d_dlogits [tokens][experts] of `type`, all of it written: from
  * d_dweight [tokens][k] fp32 (not looked at where the choice is -1) and what the
  * call above was given and wrote.  d_logits may be NULL where over_all is 0.  A
- * logit of -inf has gradient 0. */
+ * logit of -inf has gradient 0, whatever the token's other values are. */
 int pcc_route_grad(const float *d_dweight, const void *d_logits, size_t ldl, const int32_t *d_expert,
                    const float *d_weight, size_t tokens, int experts, int k, int type, int over_all,
                    void *d_dlogits, size_t lddl, void *hip_stream);

@@ -24,8 +24,8 @@ template <int LANES, int N>
 struct RowShape {
     static constexpr int kLanes = LANES, kChunks = N;
 };
-// How many lanes have a row, and how many eights of it each.  us, four and two eights a lane: rows of several waves, 16,384 of 4,096 forward 62 and 58,
-// 8,192 of 4,096 backward 83 and 80, 8,192 of 8,192 forward 60 and 57; of one wave 65,536 of 1,024 forward 58 and 60.
+// How many lanes have a row, and how many eights of it each.  us, four and two eights a lane: rows of several waves, 16,384 of 4,096 forward 58.6 and 58.4
+// (8,192 in fp32 57.9 and 57.2), 8,192 of 4,096 backward 83 and 80, 8,192 of 8,192 forward 60 and 57; of one wave 65,536 of 1,024 forward 59 and 64.
 template <bool FORWARD, class F>
 int with_row_shape(int features, F&& f) {
     const int eights = features / 8;
@@ -37,7 +37,7 @@ int with_row_shape(int features, F&& f) {
     if (eights <= 256) return f(RowShape<64, 4>{});
     if (eights <= 512) return f(RowShape<256, 2>{});
     if (eights <= 1024) return f(RowShape<512, 2>{});
-    if (eights <= 2048) {       // (without sums to keep, a thread needs few enough registers for 1024 of them: 4,096 rows of 16,384 62 us, else 64)
+    if (eights <= 2048) {       // (without sums to keep, a thread needs few enough registers for 1024 of them: 4,096 rows of 16,384 62 us, else 67)
         if constexpr (FORWARD) return f(RowShape<1024, 2>{});
         else return f(RowShape<512, 4>{});
     }
@@ -64,7 +64,10 @@ void norm_chunks(size_t rows, int groups, int want, int teams, int& log2, uint32
     while (log2 < 24 && ((size_t)64 << log2) < least) ++log2;
     mult = (uint32_t)std::min<size_t>(std::max<size_t>((least + ((size_t)1 << log2) - 1) >> log2, 1), 64);
 }
-// Chunks whose sums are joined: as many workgroups as run at once by their registers.
+// Chunks whose sums are joined: a workgroup of 512 threads for each compute unit, five of 256 threads, whose rows are short and sums few.  us with 128, 256, 512,
+// 1,024 and 1,280 chunks: 786,432 rows of 36 171, 94, 59, 49, 51, of 64 168, 95, 71, 72, 74 (256 threads); 393,216 of 160 107, 86, 90, 97, 98, 32,768 of 1,024 57, 50, 57,
+// 69, 69, 8,192 of 4,096 67, 51, 57, 61, 61, 2,048 of 16,384 71, 63, 75, 102, 102 (512 threads; where registers and LDS would let two workgroups run at once, too:
+// 16,384 of 2,560 103, 63, 61, 64, 67).
 void sums_chunks(size_t rows, int groups, int features, int& log2, uint32_t& mult) {
     const int threads = with_row_shape<false>(features, [](auto shape) { return norm_grad_threads(decltype(shape)::kLanes, decltype(shape)::kChunks); });
     const int teams = with_row_shape<false>(features, [](auto shape) { return std::max(1, norm_grad_teams(decltype(shape)::kLanes, decltype(shape)::kChunks)); });
@@ -90,7 +93,7 @@ int pcc_layer_norm(const void* d_x, size_t ldx, const float* d_gamma, const floa
     a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)rows; a.groups = groups; a.features = features; a.eps = eps; a.inverse = 1.0f / (float)features;
     return with_row_shape<true>(features, [&](auto shape) {
         constexpr int L = decltype(shape)::kLanes, N = decltype(shape)::kChunks;
-                norm_chunks(rows, groups, L <= 64 ? 2048 : L <= 512 ? 512 : 256, norm_teams(L), a.log2, a.mult);
+        norm_chunks(rows, groups, L <= 64 ? 2048 : L <= 512 ? 512 : 256, norm_teams(L), a.log2, a.mult);
         const uint64_t blocks = chunk_count(a.rows, groups, a.log2, a.mult);
         if (!launchable(blocks, norm_threads(L))) return PCC_E_ARG;
         return with_norm_types(type, y_type, [&](auto tx, auto ty) {
@@ -272,7 +275,8 @@ int with_row_types(int type, int y_type, F&& f) {
     return f(Fp32{}, Fp32{});
 }
 // How many lanes have a token's row, and how many eights of it at a time each: where it is copied, as many as it has eights, so that it
-// leaves in one piece.
+// leaves in one piece.  us, 63 million values of bf16 in rows of so many features, two rows a token, by the shape before, the rule's and the one behind it: 64 features
+// -, 29, 29; 136 44, 40, 64; 256 29, 28, 28; 264 41, 40, 40; 520 40, 39, 63; 1,024 28, 29, 28; 1,032 42, 41, -; 2,056 45, 39, -; 8,192 30, 29, -.
 template <class F>
 int with_copy_shape(int features, F&& f) {
     const int eights = features / 8;
@@ -283,6 +287,10 @@ int with_copy_shape(int features, F&& f) {
     if (eights <= 128) return f(RowShape<64, 2>{});
     return f(RowShape<256, 1>{});
 }
+// Where rows are read and joined.  us as above, join / its gradient: 64 features -, 39 / 72, 52 / 96; 136 69 / 106, 41 / 68, 55 / 86; 256 39 / 68, 37 / 63, 39 / 64; 264 48 / 70,
+// 42 / 68, 55 / 87; 512 38 / 65, 37 / 65, 38 / 64; 520 47 / 70, 40 / 66, 54 / 86; 1,024 37 / 66, 37 / 65, 38 / 63; 1,032 44 / 68, 39 / 65, 83 / 137; 2,048 45 / 68, 37 / 65, 50 / 81;
+// 4,096 38 / 66, 37 / 63, -; 8,192 38 / 68, 37 / 65, -.  From 2,056 to about 3,000 features the shape before would be the better one: 2,056 40 / 67, 53 / 83, -; 2,500
+// 44 / 73, 51 / 90, -; 3,000 40 / 69, 42 / 67, -.
 template <class F>
 int with_token_shape(int features, F&& f) {
     const int eights = features / 8;

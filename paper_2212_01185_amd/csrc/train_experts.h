@@ -210,7 +210,8 @@ __global__ __launch_bounds__(kExpertThreads) void expert_join_kernel(Experts a) 
         Z::each(lane, w, [&](auto, auto i) {
             y.at(i).set(sum.at(i));
             // past the caches, us so and not: 393,216 rows of 160 in bf16 72 and 76, 8,192 of 2,048 in fp32 43 and 46 (but 44 and 40 where three sets of
-            // inputs and results are all there is, and the last results still lie in the caches when they are written again)
+            // inputs and results are all there is, and the last results still lie in the caches when they are written again).  With dropout and its residual
+            // behind it, in a graph: 300 of 160 in bf16 4.9 and 4.7, 393,216 of 160 141 and 137, 1,024 of 2,048 in fp32 12.9 and 13.9, 8,192 of them 74 and 74
             y.store_past(i, a.y, token * a.ldy + 8 * c0, lane, w);
         });
     }

@@ -6,7 +6,7 @@
 // A row is read once: LANES lanes have it in registers, eight neighbours at a time, so the variance is that of the distances from the
 // mean and not a difference of two large sums.  The mean is a sum's first, which is off by the roundings of a sum as large as the values, and the mean of the
 // distances from it: a row of one value has that mean exactly, and distances and a variance of 0 (see `centred`).  The next row's loads are on their way while a row is summed.  Memory bounds both passes: 16,384 rows of 4,096 in bf16
-// forward 57 us, 4.7 TB/s (a large copy has 5.2); backward 393,216 rows of 160 85 us, 4.5 TB/s, of which 5 join the chunks' sums, and the vector ALU
+// forward 58 us, 4.6 TB/s (a large copy has 5.2); backward 393,216 rows of 160 85 us, 4.5 TB/s, of which 5 join the chunks' sums, and the vector ALU
 // is busy for about half of it.
 #pragma once
 
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_kernel(Norm a)
                 squares += __builtin_fmaf(parts.size[k] * d, d, parts.squares[turn][team][k]);
             }
         }
-        const float scale = __builtin_amdgcn_rsqf(squares * a.inverse + a.eps);
+        const float scale = __builtin_amdgcn_rsqf(squares * a.inverse + a.eps);     // the hardware's: within a step of fp32
         x.forget();
         const size_t row = (size_t)(ch.lo + r0 + team);
         if (a.stats && lane == 0 && r0 + team < n) {
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(norm_grad_threads(LANES, N)) void layer_norm_grad_k
 }
 
 // Rows that do not fit the registers of a workgroup (more than 16,391 features) are read again for each sum, from L2 or behind it: 1024 threads a row.  2,048 rows of
-// 30,000 in bf16: 85 us forward, 2.9 TB/s; 1,024 of them backward 106 us with the sums, which read them once more.
+// 30,000 in bf16: 87 us forward, 2.8 TB/s; 1,024 of them backward 106 us with the sums, which read them once more.
 constexpr int kLongThreads = 1024;
 
 template <class X, class Y>

@@ -89,7 +89,7 @@ __device__ __forceinline__ void sort_eight(K (&k)[8]) {
     }
 }
 
-// e^v for v <= 0 (-inf gives 0), rounded as v log2(e) is.  A NaN stays one.
+// e^v for v <= 0 (-inf gives 0), rounded as v log2(e) is: off by |v| half steps of fp32 beside its own.  A NaN stays one.
 __device__ __forceinline__ float exp_below(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504088896341f); }
 
 // Eight logits of a token from expert f on; what lies behind the last expert is -inf.
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) total += exp_below(l[i].get(e) - highest);
     }
-    const float inverse = 1.0f / lanes_sum<LANES>(total);
+    const float inverse = 1.0f / lanes_sum<LANES>(total);      // (a weight is a product with it: two roundings where a quotient has one)
     if (!mine) return;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(Route a) {
 }
 
 // A wave's tokens have a place in LDS for each logit: zeros, then what each choice brings is put in its expert's, by the lane that kept it.  393,216 tokens of
-// 64 in bf16, 8 chosen, softmax over all: 21 us, 6.5 TB/s with what the caches hold (each lane comparing its logits' numbers with every choice: 53).
+// 64 in bf16, 8 chosen, softmax over all: 22 us, 6.2 TB/s with what the caches hold (each lane comparing its logits' numbers with every choice: 53).
 template <class T, int LANES, int N>
 __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(Route a) {
     constexpr int kSlots = LANES >= PCC_MAX_CHOICES ? 1 : LANES == 1 ? 8 : PCC_MAX_CHOICES / LANES;

@@ -126,3 +126,14 @@ def test_route_gradient_of_a_masked_logit_is_0_beside_what_is_not_a_number(dtype
 def test_route_refuses_a_number_of_choices_before_it_makes_room_for_them(k):
     with pytest.raises(binding.PccError):
         binding.pcc_route(torch.zeros(4, 32, device="cuda"), k)
+
+
+@pytest.mark.parametrize("features", [8, 160, 4096, 16384, 20000])
+def test_layer_norm_of_finite_rows_whose_squares_are_not(features):
+    x = torch.full((3, features), 1e25)
+    x[:, ::2] *= -1
+    x[1] = 1e25 * (torch.randn(features, generator=torch.Generator().manual_seed(2)) + 3)
+    beta = torch.randn(1, features, generator=torch.Generator().manual_seed(1)).cuda()
+    for dtype in (FP32, BF16):
+        y, stats = binding.pcc_layer_norm(x.to(dtype).cuda(), None, beta, out_dtype=dtype)
+        assert (stats[:, 1] == 0).all() and torch.isfinite(stats).all() and torch.equal(y, beta.to(dtype).expand(3, -1))
